@@ -282,6 +282,98 @@ int obc_reconstruct_workspace_bytes(int R, int d, int max_pruned, size_t *bytes)
 int obc_reconstruct_rows(obc_ctx *ctx, const float *W, const float *Hinv, const uint8_t *mask, int R, int d,
                          int max_pruned, float *W_out, void *ws, size_t ws_bytes);
 
+/* ---- Running compressed layers of language models -----------------------------------------
+ * A layer's codes on a grid of at most 16 values, packed to 4 bits with a step and an offset per row
+ * and group of `group` consecutive columns, and the operators around it: its product with activations
+ * (single tokens to prompts), the gradient of its inputs, the root-mean-square norm before it, and the
+ * loss against the dense model's answers by which what stays uncompressed is tuned.  All asynchronous.
+ * Element types of activations, gradients and logits: */
+#define OBC_F32 0
+#define OBC_F16 1
+#define OBC_BF16 2
+#define OBC_I8 3   /* 8-bit integers with an fp32 scale per row */
+
+/* Flags of obc_group_grid. */
+#define OBC_GRID_SYMMETRIC 1 /* symmetric about zero: offset = -max|w|, delta = 2 max|w| / maxq */
+#define OBC_GRID_ZERO 2      /* zero is one of the grid's values (layers that are pruned and quantized) */
+
+/* Grid of every row and group over its live weights (live nullable = all live): min-max, or as `flags`
+ * say; 1 <= maxq <= 15.  group: 32, 64 or a multiple of 128; 0 or >= d: one group per row.
+ *   delta, offset   R x ceil(d / group) out; values of half precision, rounded so that the grid still
+ *                   covers the weights, as obc_pack4 keeps them.  With one group per row they are what
+ *                   obc_quant_rows takes.  delta = 1 where the range is empty.
+ * A group whose weights half precision cannot hold latches OBC_ERR_NUMERIC. */
+int obc_group_grid(obc_ctx *ctx, const float *W, const uint8_t *live, int R, int d, int group, int maxq,
+                   int flags, float *delta, float *offset);
+
+/* Pack R x d codes (int32, 0 .. 15, as obc_quant_rows writes them) with their grid for the products:
+ * weight = offset + delta * code.  delta and offset (R x ceil(d / group)) are rounded to half precision
+ * (obc_group_grid's already are).  A code of -1 is a pruned weight: it takes the code whose value is
+ * exactly 0.  A code out of range, or of -1 on a grid without a zero, latches OBC_ERR_BAD_ARG; a step or
+ * offset beyond half precision or not finite latches OBC_ERR_NUMERIC.  `packed` (obc_pack4_bytes, aligned
+ * to 16 bytes) is opaque: codes in the order of the matrix instructions' operands. */
+int obc_pack4_bytes(int R, int d, int group, size_t *bytes);
+int obc_pack4(obc_ctx *ctx, const int32_t *codes, const float *delta, const float *offset, int R, int d,
+              int group, void *packed);
+
+/* y = x W^T for T tokens: y[t, r] = sum_c x[t, c] (offset + delta code)[r, c], T x R.
+ *   x   T x d, leading dimension ldx >= d, of x_type; OBC_I8: x stands for x_scale[t] * x[t, c]
+ *       (x_scale: T fp32; null for the other types)
+ *   y   T x R, leading dimension ldy >= R, of y_type (OBC_F32, OBC_F16 or OBC_BF16)
+ * Products and sums have the precision of fp32 (OBC_I8: integer sums, exact) and are rounded once, to y's
+ * type.  Rows need no alignment beyond their elements'.  Fixed summation order for a given T, R, d and group.
+ * A non-finite input makes its token's outputs non-finite (inf or NaN).  y may not overlap x. */
+int obc_product4_workspace_bytes(int T, int R, int d, int group, int x_type, size_t *bytes);
+int obc_product4(obc_ctx *ctx, const void *packed, int R, int d, int group, const void *x, int x_type,
+                 const float *x_scale, int T, int64_t ldx, void *y, int y_type, int64_t ldy, void *ws,
+                 size_t ws_bytes);
+
+/* dx = dy W for T tokens, the gradient of obc_product4's inputs: dx[t, c] = sum_r dy[t, r] W[r, c].
+ *   dy  T x R, leading dimension lddy >= R;  dx  T x d, leading dimension lddx >= d; both of `type`
+ *       (OBC_F32, OBC_F16 or OBC_BF16)
+ * 16-bit types: weights rounded to the type (the steps differ along the sum, so they cannot be taken out of
+ * it), products and sums fp32, one rounding of the result.  OBC_F32: the precision of fp32 throughout. */
+int obc_product4_grad_workspace_bytes(int T, int R, int d, int group, int type, size_t *bytes);
+int obc_product4_grad(obc_ctx *ctx, const void *packed, int R, int d, int group, const void *dy, int type, int T,
+                      int64_t lddy, void *dx, int64_t lddx, void *ws, size_t ws_bytes);
+
+/* Root-mean-square norm of T rows with the residual's addition:
+ *   h = x + residual,  y = h / sqrt(mean(h^2) + eps) * gain
+ *   x, residual, h   T x d, contiguous, of x_type (OBC_F32, OBC_F16, OBC_BF16); residual nullable (h = x); h
+ *            nullable (not written), h == x or h == residual allowed.  The norm is of the unrounded sum.
+ *   gain     d, fp32
+ *   y        T x d of y_type: x_type or OBC_I8; OBC_I8: y stands for y_scale[t] * y[t, c], y_scale[t] =
+ *            max|y| / 127 (1 for a row of zeros; NaN, and codes 0, for a row with a NaN or an infinity)
+ *   y_scale  T fp32 out, with OBC_I8;  rstd  nullable, T fp32 out: 1 / sqrt(mean(h^2) + eps)
+ * 1 <= d <= 65536. */
+int obc_rmsnorm(obc_ctx *ctx, const void *x, const void *residual, int x_type, const float *gain, float eps, int T,
+                int d, void *h, void *y, int y_type, float *y_scale, float *rstd);
+
+/* Its backward pass (8-bit outputs: straight through the rounding), from the saved sum h and rstd:
+ *   dx = dh + rstd (gain dy - xhat mean(gain dy xhat)),  dgain = sum_t dy xhat,   xhat = h rstd
+ *   h, dy, dh, dx   T x d, contiguous, of `type`; dh: the gradient that reaches h on the residual path, nullable.
+ *                   dx is the gradient of x and of residual alike; dx == dy or dx == dh allowed
+ *   dgain    d fp32 out
+ * Fixed summation order. */
+int obc_rmsnorm_grad_workspace_bytes(int T, int d, size_t *bytes);
+int obc_rmsnorm_grad(obc_ctx *ctx, const void *h, const float *gain, const float *rstd, const void *dy, const void *dh,
+                     int type, int T, int d, void *dx, float *dgain, void *ws, size_t ws_bytes);
+
+/* Distillation from a teacher's top logits.  For every row t with its valid entries j (top_index >= 0)
+ *   p_j = softmax over the valid entries of top_logit / temperature,  q = softmax over the row of z / temperature
+ *   loss[t] = weight[t] temperature^2 sum_j p_j (log p_j - log q[top_index_j])
+ *   dz[t, v] = weight[t] temperature (q[v] - sum of p_j over the entries with top_index_j = v)
+ * dz is the gradient of the losses' sum.
+ *   z          T x V logits of `type`, leading dimension ldz >= V
+ *   top_index  T x k int32, negative: no entry (rows may hold any number from 0 to k); top_logit  T x k fp32
+ *   weight     nullable (1), T fp32.  A row of weight 0 or without an entry has loss 0 and a gradient of zeros,
+ *              whatever its logits are.  An entry with a logit of -inf counts as none.
+ *   loss       T fp32 out;  dz  nullable, T x V out of `type`, leading dimension lddz; dz == z allowed (lddz == ldz)
+ * An index >= V latches OBC_ERR_BAD_ARG and counts as no entry.  0 <= k <= 1024, temperature > 0. */
+int obc_distill(obc_ctx *ctx, const void *z, int type, int T, int V, int64_t ldz, const int32_t *top_index,
+                const float *top_logit, int k, float temperature, const float *weight, float *loss, void *dz,
+                int64_t lddz);
+
 #ifdef __cplusplus
 }
 #endif

@@ -11,6 +11,8 @@ import ctypes
 import os
 from ctypes import POINTER, byref, c_char_p, c_float, c_int, c_int64, c_size_t, c_void_p
 
+from typing import NamedTuple
+
 import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -21,6 +23,8 @@ OBC_ERR_BAD_ARG, OBC_ERR_BAD_SHAPE, OBC_ERR_NOT_SPD = -1, -2, -3
 OBC_ERR_WORKSPACE, OBC_ERR_NUMERIC, OBC_ERR_HIP = -4, -5, -6
 STRATEGY_AUTO, STRATEGY_RANK1, STRATEGY_BLOCKED = 0, 1, 2
 QUANT_OUTLIERS = 1
+F32, F16, BF16, I8 = 0, 1, 2, 3
+GRID_SYMMETRIC, GRID_ZERO = 1, 2
 SELECT_STATIC_MAX_WEIGHTS, SELECT_STATIC_MAX_ROWS = 2359296, 8192   # limits of obc_global_select_static
 
 EXPORTS = [
@@ -32,7 +36,12 @@ EXPORTS = [
     "obc_rows_workspace_bytes", "obc_prune_rows", "obc_blocks_workspace_bytes", "obc_prune_blocks", "obc_quant_rows", "obc_minmax_grid",
     "obc_global_select_workspace_bytes", "obc_global_select", "obc_global_select_static", "obc_gather_trace",
     "obc_reconstruct_workspace_bytes", "obc_reconstruct_rows",
+    "obc_group_grid", "obc_pack4_bytes", "obc_pack4",
+    "obc_product4_workspace_bytes", "obc_product4", "obc_product4_grad_workspace_bytes", "obc_product4_grad",
+    "obc_rmsnorm", "obc_rmsnorm_grad_workspace_bytes", "obc_rmsnorm_grad", "obc_distill",
 ]
+
+_TYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16, torch.int8: I8}
 
 
 KERNEL_CLASSES = ("panel", "flush", "rank1")
@@ -41,6 +50,14 @@ KERNEL_CLASSES = ("panel", "flush", "rank1")
 class KernelStat(ctypes.Structure):
     _fields_ = [("launches", c_int), ("ms", ctypes.c_double), ("bytes", ctypes.c_double),
                 ("flops", ctypes.c_double)]
+
+
+class Packed4(NamedTuple):
+    """A layer's weights as obc_pack4 lays them out: opaque bytes, and the sizes they were packed for."""
+    data: torch.Tensor
+    rows: int
+    cols: int
+    group: int
 
 
 class ObcError(RuntimeError):
@@ -96,6 +113,18 @@ def load_library():
     lib.obc_gather_trace.argtypes = [vp, vp, vp, vp, c_int, c_int, c_int, vp]
     lib.obc_reconstruct_workspace_bytes.argtypes = [c_int, c_int, c_int, sp]
     lib.obc_reconstruct_rows.argtypes = [vp, vp, vp, vp, c_int, c_int, c_int, vp, vp, c_size_t]
+    i64 = c_int64
+    lib.obc_group_grid.argtypes = [vp, vp, vp, c_int, c_int, c_int, c_int, c_int, vp, vp]
+    lib.obc_pack4_bytes.argtypes = [c_int, c_int, c_int, sp]
+    lib.obc_pack4.argtypes = [vp, vp, vp, vp, c_int, c_int, c_int, vp]
+    lib.obc_product4_workspace_bytes.argtypes = [c_int, c_int, c_int, c_int, c_int, sp]
+    lib.obc_product4.argtypes = [vp, vp, c_int, c_int, c_int, vp, c_int, vp, c_int, i64, vp, c_int, i64, vp, c_size_t]
+    lib.obc_product4_grad_workspace_bytes.argtypes = [c_int, c_int, c_int, c_int, c_int, sp]
+    lib.obc_product4_grad.argtypes = [vp, vp, c_int, c_int, c_int, vp, c_int, c_int, i64, vp, i64, vp, c_size_t]
+    lib.obc_rmsnorm.argtypes = [vp, vp, vp, c_int, vp, c_float, c_int, c_int, vp, vp, c_int, vp, vp]
+    lib.obc_rmsnorm_grad_workspace_bytes.argtypes = [c_int, c_int, sp]
+    lib.obc_rmsnorm_grad.argtypes = [vp, vp, vp, vp, vp, vp, c_int, c_int, c_int, vp, vp, vp, c_size_t]
+    lib.obc_distill.argtypes = [vp, vp, c_int, c_int, c_int, i64, vp, vp, c_int, c_float, vp, vp, vp, i64]
     for name in EXPORTS:
         fn = getattr(lib, name)
         if name not in ("obc_last_error", "obc_version"):
@@ -116,6 +145,38 @@ def _ptr(t, dtype=None):
     return c_void_p(t.data_ptr())
 
 
+def _type_of(t, what, i8=False):
+    code = _TYPES.get(t.dtype)
+    if code is None or (code == I8 and not i8):
+        raise ValueError("%s: unsupported type %s" % (what, t.dtype))
+    return code
+
+
+def _rows_of(t, what, shape=None):
+    """Address and leading dimension of a device matrix whose rows are contiguous."""
+    if not t.is_cuda:
+        raise ValueError("libobc takes device tensors")
+    if t.dim() != 2:
+        raise ValueError("%s must be a matrix" % what)
+    if shape is not None and tuple(t.shape) != shape:
+        raise ValueError("%s must be %d x %d, got %s" % (what, shape[0], shape[1], tuple(t.shape)))
+    rows, cols = t.shape
+    ld = t.stride(0)
+    if rows <= 1:
+        ld = max(ld, cols)
+    if (cols > 1 and t.stride(1) != 1) or ld < cols:
+        raise ValueError("%s must have unit stride along its rows, and rows that do not overlap" % what)
+    return t.data_ptr(), ld
+
+
+def _vector(t, n, what):
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s must be %d contiguous fp32 values on the device" % (what, n))
+    return t.data_ptr()
+
+
 class Context:
     """An obc_ctx bound to a torch stream (default: the current one)."""
 
@@ -128,6 +189,7 @@ class Context:
             raise ObcError(rc, "obc_create failed")
         self.h = h
         self._ws = None
+        self._needs = {}
 
     def close(self):
         if getattr(self, "h", None):
@@ -375,3 +437,164 @@ class Context:
                                                _ptr(mask, torch.uint8), R, d, int(max_pruned), _ptr(W_out),
                                                c_void_p(ws.data_ptr()), ws.numel()))
         return W_out
+
+    # ------------------------------------------------------- running compressed layers
+    def _empty(self, shape, dtype, device):
+        """An output for kernels on the context's stream: allocated on that stream, which need not be the current
+        one, so that the allocator does not hand out memory that the current stream still uses."""
+        if torch.cuda.current_stream(device) == self.stream:
+            return torch.empty(shape, dtype=dtype, device=device)
+        with torch.cuda.stream(self.stream):
+            return torch.empty(shape, dtype=dtype, device=device)
+
+    def _need(self, query, *sizes):
+        """Workspace of one of the queries (asked once for each set of sizes): address and bytes."""
+        key = (query,) + sizes
+        n = self._needs.get(key)
+        if n is None:
+            need = c_size_t()
+            rc = getattr(self.lib, query)(*sizes, byref(need))
+            if rc != OBC_OK:
+                raise ObcError(rc, query)
+            if len(self._needs) >= 4096:
+                self._needs.clear()
+            n = self._needs[key] = need.value
+        if n == 0:
+            return None, 0
+        ws = self.workspace(n)
+        return ws.data_ptr(), ws.numel()
+
+    def obc_group_grid(self, W, bits=4, group=0, live=None, symmetric=False, zero=False):
+        """Steps and offsets (R x groups) of a grid of 2^bits values, bits <= 4; group 0: one per row, which
+        obc_quant_rows takes as [:, 0]."""
+        R, d = W.shape
+        maxq = (1 << bits) - 1
+        n = 1 if group <= 0 or group >= d else -(-d // group)
+        delta = self._empty((R, n), torch.float32, W.device)
+        offset = self._empty((R, n), torch.float32, W.device)
+        flags = (GRID_SYMMETRIC if symmetric else 0) | (GRID_ZERO if zero else 0)
+        if live is not None and live.shape != W.shape:
+            raise ValueError("live must have W's shape")
+        self._ck(self.lib.obc_group_grid(self.h, _ptr(W, torch.float32), _ptr(live, torch.uint8), R, d, int(group), maxq,
+                                         flags, _ptr(delta), _ptr(offset)))
+        return delta, offset, maxq
+
+    def obc_pack4(self, codes, delta, offset, group=0):
+        """Codes (R x d int32) and their grid (R x groups; R values do for one group) as a Packed4."""
+        R, d = codes.shape
+        need = c_size_t()
+        rc = self.lib.obc_pack4_bytes(R, d, int(group), byref(need))
+        if rc != OBC_OK:
+            raise ObcError(rc, "obc_pack4_bytes")
+        n = 1 if group <= 0 or group >= d else -(-d // group)
+        if delta.numel() != R * n or offset.numel() != R * n:
+            raise ValueError("delta and offset must hold %d x %d values" % (R, n))
+        data = self._empty((max(need.value, 16),), torch.uint8, codes.device)
+        self._ck(self.lib.obc_pack4(self.h, _ptr(codes, torch.int32), _ptr(delta, torch.float32),
+                                    _ptr(offset, torch.float32), R, d, int(group), _ptr(data)))
+        return Packed4(data, R, d, int(group))
+
+    def obc_product4(self, W, x, x_scale=None, out=None, out_dtype=None):
+        """y = x W^T (T x rows) of a Packed4.  x: T x cols, fp32, fp16, bf16, or int8 with its scales (T).  y has
+        out's type, else out_dtype, else x's (int8: bf16)."""
+        xt = _type_of(x, "x", i8=True)
+        xp, ldx = _rows_of(x, "x")
+        T, d = x.shape
+        if d != W.cols:
+            raise ValueError("x has %d columns, the weights %d" % (d, W.cols))
+        if out is None:
+            if out_dtype is None:
+                out_dtype = torch.bfloat16 if xt == I8 else x.dtype
+            out = self._empty((T, W.rows), out_dtype, x.device)
+        yp, ldy = _rows_of(out, "out", (T, W.rows))
+        ws, n = self._need("obc_product4_workspace_bytes", T, W.rows, d, W.group, xt)
+        self._ck(self.lib.obc_product4(self.h, W.data.data_ptr(), W.rows, d, W.group, xp, xt, _vector(x_scale, T, "x_scale"),
+                                       T, ldx, yp, _type_of(out, "out"), ldy, ws, n))
+        return out
+
+    def obc_product4_grad(self, W, dy, out=None):
+        """dx = dy W (T x cols), the gradient of obc_product4's inputs, in dy's type."""
+        t = _type_of(dy, "dy")
+        dp, lddy = _rows_of(dy, "dy")
+        T, R = dy.shape
+        if R != W.rows:
+            raise ValueError("dy has %d columns, the weights %d rows" % (R, W.rows))
+        if out is None:
+            out = self._empty((T, W.cols), dy.dtype, dy.device)
+        if out.dtype != dy.dtype:
+            raise ValueError("out must have dy's type")
+        xp, lddx = _rows_of(out, "out", (T, W.cols))
+        ws, n = self._need("obc_product4_grad_workspace_bytes", T, R, W.cols, W.group, t)
+        self._ck(self.lib.obc_product4_grad(self.h, W.data.data_ptr(), R, W.cols, W.group, dp, t, T, lddy, xp, lddx, ws, n))
+        return out
+
+    def obc_rmsnorm(self, x, gain, eps=1e-6, residual=None, quant8=False, want_rstd=False, out=None):
+        """h = x + residual and its root-mean-square norm y.  out may hold h, y, scale (quant8) and rstd; without a
+        residual, h is x itself."""
+        T, d = x.shape
+        t = _type_of(x, "x")
+        out = {} if out is None else out
+        h = out.get("h")
+        if h is None and residual is not None:
+            h = self._empty((T, d), x.dtype, x.device)
+        y = out.get("y")
+        if y is None:
+            y = self._empty((T, d), torch.int8 if quant8 else x.dtype, x.device)
+        scale = out.get("scale")
+        if scale is None and quant8:
+            scale = self._empty((T,), torch.float32, x.device)
+        rstd = out.get("rstd")
+        if rstd is None and want_rstd:
+            rstd = self._empty((T,), torch.float32, x.device)
+        for other in (residual, h, y):
+            if other is not None and other.shape != x.shape:
+                raise ValueError("residual, h and y must have x's shape")
+        self._ck(self.lib.obc_rmsnorm(self.h, _ptr(x), _ptr(residual, x.dtype), t, _vector(gain, d, "gain"), float(eps), T, d,
+                                      _ptr(h, x.dtype), _ptr(y, torch.int8 if quant8 else x.dtype), I8 if quant8 else t,
+                                      _vector(scale, T, "scale") if quant8 else None, _vector(rstd, T, "rstd")))
+        return dict(h=x if h is None else h, y=y, scale=scale, rstd=rstd)
+
+    def obc_rmsnorm_grad(self, h, gain, rstd, dy, dh=None, out=None):
+        """Gradients of x (and of the residual) and of the gain, from what the forward pass left; out may hold dx and
+        dgain."""
+        T, d = h.shape
+        t = _type_of(h, "h")
+        out = {} if out is None else out
+        dx = out.get("dx")
+        if dx is None:
+            dx = self._empty((T, d), h.dtype, h.device)
+        dgain = out.get("dgain")
+        if dgain is None:
+            dgain = self._empty((d,), torch.float32, h.device)
+        for other in (dy, dh, dx):
+            if other is not None and other.shape != h.shape:
+                raise ValueError("dy, dh and dx must have h's shape")
+        ws, n = self._need("obc_rmsnorm_grad_workspace_bytes", T, d)
+        self._ck(self.lib.obc_rmsnorm_grad(self.h, _ptr(h), _vector(gain, d, "gain"), _vector(rstd, T, "rstd"), _ptr(dy, h.dtype),
+                                           _ptr(dh, h.dtype), t, T, d, _ptr(dx, h.dtype), _vector(dgain, d, "dgain"), ws, n))
+        return dict(dx=dx, dgain=dgain)
+
+    def obc_distill(self, z, top_index, top_logit, temperature=1.0, weight=None, want_grad=False, out=None):
+        """Distillation loss (T) of logits z (T x V) against a teacher's top logits (T x k), and the gradient dz with
+        want_grad; out may hold loss and dz (z itself, to overwrite the logits)."""
+        t = _type_of(z, "z")
+        zp, ldz = _rows_of(z, "z")
+        T, V = z.shape
+        out = {} if out is None else out
+        loss = out.get("loss")
+        if loss is None:
+            loss = self._empty((T,), torch.float32, z.device)
+        dz = out.get("dz") if want_grad else None
+        if dz is None and want_grad:
+            dz = self._empty((T, V), z.dtype, z.device)
+        gp, ldg = (None, 0)
+        if dz is not None:
+            if dz.dtype != z.dtype:
+                raise ValueError("dz must have z's type")
+            gp, ldg = _rows_of(dz, "dz", (T, V))
+        if top_index.shape != top_logit.shape or top_index.dim() != 2 or top_index.shape[0] != T:
+            raise ValueError("top_index and top_logit must be T x k")
+        k = top_index.shape[1]
+        self._ck(self.lib.obc_distill(self.h, zp, t, T, V, ldz, _ptr(top_index, torch.int32), _ptr(top_logit, torch.float32), k,
+                                      float(temperature), _vector(weight, T, "weight"), _vector(loss, T, "loss"), gp, ldg))
+        return dict(loss=loss, dz=dz)

@@ -1,0 +1,96 @@
+// What the products with 4-bit weights share: operand types of the matrix instructions, loads of
+// activations in their order, codes as numbers.
+#pragma once
+
+#include "pack4.h"
+
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef int intx4 __attribute__((ext_vector_type(4)));
+typedef int intx2 __attribute__((ext_vector_type(2)));
+typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
+typedef unsigned uintx2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
+typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
+// the same, at any element's address
+typedef unsigned uintx4_at2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef unsigned uintx2_at1 __attribute__((ext_vector_type(2), aligned(1)));
+typedef float floatx4_at4 __attribute__((ext_vector_type(4), aligned(4)));
+
+// A code q as the 16-bit number 16 + q, exactly: the code in the top four bits of the mantissa under the
+// exponent of 16.  (A base of 16 costs the sums two or three bits by cancellation, where 128 or 1024, which the
+// code's bits at the bottom of the mantissa would give, cost five or eight.)
+constexpr float kCodeBase = 16.f;
+
+// dword i of the operand holds the columns 2 i and 2 i + 1
+__device__ inline uintx4 codes_bf16(unsigned w)
+{
+    constexpr unsigned mask = 0x00780078u, base = 0x41804180u;
+    return uintx4{((w << 3) & mask) | base, ((w >> 1) & mask) | base, ((w >> 5) & mask) | base, ((w >> 9) & mask) | base};
+}
+
+__device__ inline uintx4 codes_f16(unsigned w)
+{
+    constexpr unsigned mask = 0x03c003c0u, base = 0x4c004c00u;
+    return uintx4{((w << 6) & mask) | base, ((w << 2) & mask) | base, ((w >> 2) & mask) | base, ((w >> 6) & mask) | base};
+}
+
+// Eight codes as bytes, in the order of the columns 0 4 1 5 2 6 3 7; bytes_like_codes brings eight 8-bit
+// inputs into the same order.
+__device__ inline uintx2 codes_i8(unsigned w) { return uintx2{w & 0x0f0f0f0fu, (w >> 4) & 0x0f0f0f0fu}; }
+
+__device__ inline uintx2 bytes_like_codes(uintx2 x)
+{
+    return uintx2{__builtin_amdgcn_perm(x.y, x.x, 0x05010400u), __builtin_amdgcn_perm(x.y, x.x, 0x07030602u)};
+}
+
+__device__ inline floatx4 mfma_bf16(uintx4 a, uintx4 b, floatx4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+__device__ inline floatx4 mfma_f16(uintx4 a, uintx4 b, floatx4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(halfx8, a), __builtin_bit_cast(halfx8, b), c, 0, 0, 0);
+}
+
+// 32 columns of 8-bit inputs: half the depth of this type's instruction, so that a group of 32 ends between two
+__device__ inline intx4 mfma_i8(uintx2 a, uintx2 b, intx4 c)
+{
+    return __builtin_amdgcn_mfma_i32_16x16x32_i8(__builtin_bit_cast(long, a), __builtin_bit_cast(long, b), c, 0, 0, 0);
+}
+
+__device__ inline unsigned pair_bf16(float lo, float hi)
+{
+    return __builtin_bit_cast(unsigned, bf16x2{(__bf16)lo, (__bf16)hi});
+}
+
+__device__ inline unsigned pair_f16(float lo, float hi)
+{
+    return __builtin_bit_cast(unsigned, halfx2{(_Float16)lo, (_Float16)hi});
+}
+
+// x = h + m + l, three bf16 numbers, exact from 2^-110 on; an infinity or a NaN stays in h alone.
+__device__ inline void split3(float x, float &h, float &m, float &l)
+{
+    h = (float)(__bf16)x;
+    const float r = x - h;
+    const bool finite = fabsf(h) < __builtin_inff();
+    m = finite ? (float)(__bf16)r : 0.f;
+    l = finite ? (float)(__bf16)(r - m) : 0.f;
+}
+
+__device__ inline float half_lo(unsigned w) { return (float)__builtin_bit_cast(_Float16, (unsigned short)(w & 0xffffu)); }
+__device__ inline float half_hi(unsigned w) { return (float)__builtin_bit_cast(_Float16, (unsigned short)(w >> 16)); }
+
+template <int YT>
+__device__ inline void store_as(void *y, int64_t at, float v)
+{
+    if (YT == OBC_F32) ((float *)y)[at] = v;
+    else if (YT == OBC_F16) ((_Float16 *)y)[at] = (_Float16)v;
+    else ((__bf16 *)y)[at] = (__bf16)v;
+}
+
+static inline bool float_type(int type) { return type == OBC_F32 || type == OBC_F16 || type == OBC_BF16; }
+static inline size_t size_of_type(int type) { return type == OBC_F32 ? 4 : type == OBC_I8 ? 1 : 2; }

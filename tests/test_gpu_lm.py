@@ -1,0 +1,662 @@
+"""Operators around compressed layers (4-bit products and their input gradient, root-mean-square norm, distillation)
+against plain implementations in 64 bits.  Bounds are worst-case ones of the arithmetic that the header states: a
+sum of n fp32 terms is off by at most n 2^-24 of the sum of their magnitudes, a result is rounded once to its type."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+U32 = 2.0 ** -24
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+ROUND = {k: torch.finfo(t).eps / 2 for k, t in TYPES.items()}      # half a unit in the last place, relative
+TINY = {"f32": 0.0, "f16": 2.0 ** -24, "bf16": 0.0}      # half precision's smallest number
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    import paper_2208_11580_amd as pkg
+
+    c = pkg.Context()
+    yield c
+    c.close()
+
+
+def _gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def _layer(R, d, group, g, live=None):
+    """Random codes with the grid they belong to, and the weights in 64 bits."""
+    G = d if group <= 0 or group >= d else group
+    n = -(-d // G)
+    codes = torch.randint(0, 16, (R, d), generator=g, device="cuda", dtype=torch.int32)
+    delta = (torch.rand(R, n, generator=g, device="cuda") * 0.02 + 0.001).half().float()
+    offset = (-7.5 * delta + 0.01 * torch.randn(R, n, generator=g, device="cuda")).half().float()
+    col = torch.arange(d, device="cuda") // G
+    step, off = delta.double()[:, col], offset.double()[:, col]
+    return codes, delta, offset, off + step * codes.double(), step * (16.0 + codes.double()) + (off - 16.0 * step).abs()
+
+
+def _within(got, want, bound):
+    err = (got.double() - want).abs()
+    bad = ~(err <= bound)
+    assert not bad.any(), "%d of %d outside, worst %.3g of its bound" % (
+        int(bad.sum()), bad.numel(), float((err / bound.clamp_min(1e-300)).nan_to_num(float("inf")).max()))
+
+
+def _product_bound(x, mag, want, kind, d):
+    # a group's sum has at most 128 terms in three parts (fp32 inputs), then one multiply-add for each of two
+    # sums per 32 columns, and the waves' partial sums
+    n = 3 * 128 + 2 * (d // 32 + 1) + 32
+    return n * U32 * (x.double().abs() @ mag.T) + ROUND[kind] * 1.01 * want.abs() + TINY[kind]
+
+
+SHAPES = [  # T, R, d, group
+    (1, 1, 1, 0), (1, 16, 128, 128), (1, 768, 768, 64), (1, 17, 129, 32), (2, 33, 31, 32), (3, 100, 1000, 256),
+    (5, 48, 65, 64), (13, 500, 499, 32), (16, 64, 4096, 128), (17, 31, 640, 0), (31, 257, 255, 128), (33, 300, 384, 384),
+    (64, 128, 512, 64), (65, 80, 200, 32), (100, 513, 1283, 0), (129, 260, 300, 128), (200, 64, 2304, 64), (257, 272, 130, 32),
+    (300, 600, 1025, 128), (512, 256, 256, 256),
+]
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T,R,d,group", SHAPES)
+def test_product(ctx, T, R, d, group, kind):
+    g = _gen(T * 7 + R + d)
+    codes, delta, offset, W, mag = _layer(R, d, group, g)
+    P = ctx.obc_pack4(codes, delta, offset, group)
+    x = torch.randn(T, d, generator=g, device="cuda").to(TYPES[kind])
+    y = ctx.obc_product4(P, x)
+    ctx.obc_check()
+    want = x.double() @ W.T
+    _within(y, want, _product_bound(x, mag, want, kind, d))
+    assert torch.equal(y, ctx.obc_product4(P, x))
+
+
+@pytest.mark.parametrize("out", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T,R,d,group", SHAPES)
+def test_product_of_8_bit_inputs(ctx, T, R, d, group, out):
+    g = _gen(T + 3 * R + d)
+    codes, delta, offset, W, mag = _layer(R, d, group, g)
+    P = ctx.obc_pack4(codes, delta, offset, group)
+    x = torch.randint(-128, 128, (T, d), generator=g, device="cuda", dtype=torch.int8)
+    scale = torch.rand(T, generator=g, device="cuda") * 0.01
+    y = ctx.obc_product4(P, x, x_scale=scale, out_dtype=TYPES[out])
+    ctx.obc_check()
+    xs = x.double() * scale.double()[:, None]
+    want = xs @ W.T
+    _within(y, want, _product_bound(xs, mag, want, out, d))
+
+
+@pytest.mark.parametrize("T", [1, 7, 40, 150])
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16", "i8"])
+def test_product_of_strided_and_misaligned_rows(ctx, T, kind):
+    """Rows at odd element offsets with gaps between them; what lies in the gaps (NaN) is not read into a result, and
+    the gaps of y are not written."""
+    R, d, group = 70, 333, 64
+    g = _gen(5)
+    codes, delta, offset, W, mag = _layer(R, d, group, g)
+    P = ctx.obc_pack4(codes, delta, offset, group)
+    if kind == "i8":
+        buf = torch.randint(-128, 128, (T, d + 6), generator=g, device="cuda", dtype=torch.int8)
+        scale = torch.rand(T, generator=g, device="cuda") + 0.5
+    else:
+        buf = torch.full((T, d + 6), float("nan"), device="cuda", dtype=TYPES[kind])
+        buf[:, 3:3 + d] = torch.randn(T, d, generator=g, device="cuda").to(TYPES[kind])
+        scale = None
+    x = buf[:, 3:3 + d]
+    ybuf = torch.full((T, R + 5), 77.0, device="cuda", dtype=torch.float32 if kind == "i8" else TYPES[kind])
+    ctx.obc_product4(P, x, x_scale=scale, out=ybuf[:, 1:1 + R])
+    xs = x.double() if scale is None else x.double() * scale.double()[:, None]
+    want = xs @ W.T
+    _within(ybuf[:, 1:1 + R], want, _product_bound(xs, mag, want, "f32" if kind == "i8" else kind, d))
+    assert torch.all(ybuf[:, 0] == 77.0) and torch.all(ybuf[:, 1 + R:] == 77.0)
+
+
+def test_product_sees_cancelling_and_large_inputs(ctx):
+    """fp32 inputs over a wide range: the three terms carry all 24 bits."""
+    g = _gen(8)
+    for T in (2, 90):
+        codes, delta, offset, W, mag = _layer(50, 700, 128, g)
+        P = ctx.obc_pack4(codes, delta, offset, 128)
+        x = torch.randn(T, 700, generator=g, device="cuda") * torch.logspace(-15, 15, 700, device="cuda")
+        want = x.double() @ W.T
+        _within(ctx.obc_product4(P, x), want, _product_bound(x, mag, want, "f32", 700))
+
+
+def test_non_finite_inputs_stay_with_their_token(ctx):
+    for kind in TYPES:
+        for T in (5, 70, 200):
+            g = _gen(9)
+            codes, delta, offset, W, mag = _layer(40, 300, 64, g)
+            P = ctx.obc_pack4(codes, delta, offset, 64)
+            x = torch.randn(T, 300, generator=g, device="cuda").to(TYPES[kind])
+            x[1, 7], x[3, 299] = float("inf"), float("nan")
+            y = ctx.obc_product4(P, x)
+            rest = torch.ones(T, dtype=torch.bool, device="cuda")
+            rest[1] = rest[3] = False
+            assert not torch.isfinite(y[~rest].float()).any(), (kind, T)
+            want = x[rest].double() @ W.T
+            _within(y[rest], want, _product_bound(x[rest], mag, want, kind, 300))
+
+
+def _grad_bound(dy, W, want, kind):
+    weights = {"f32": 2.0 ** -22, "f16": ROUND["f16"], "bf16": ROUND["bf16"]}[kind]
+    n = 6 * W.shape[0] + 64
+    total = dy.double().abs() @ W.abs()
+    tiny = 2.0 ** -25 * dy.double().abs().sum(1, keepdim=True) if kind == "f16" else 0.0
+    return (weights * 1.01 + n * U32) * total + tiny + ROUND[kind] * 1.01 * want.abs() + TINY[kind]
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T,R,d,group", SHAPES)
+def test_product_grad(ctx, T, R, d, group, kind):
+    g = _gen(T * 5 + R + d)
+    codes, delta, offset, W, _ = _layer(R, d, group, g)
+    P = ctx.obc_pack4(codes, delta, offset, group)
+    dy = torch.randn(T, R, generator=g, device="cuda").to(TYPES[kind])
+    dx = ctx.obc_product4_grad(P, dy)
+    ctx.obc_check()
+    want = dy.double() @ W
+    _within(dx, want, _grad_bound(dy, W, want, kind))
+    assert torch.equal(dx, ctx.obc_product4_grad(P, dy))
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T", [1, 20, 150])
+def test_product_grad_of_strided_and_misaligned_rows(ctx, T, kind):
+    R, d, group = 75, 333, 32
+    g = _gen(6)
+    codes, delta, offset, W, _ = _layer(R, d, group, g)
+    P = ctx.obc_pack4(codes, delta, offset, group)
+    buf = torch.full((T, R + 6), float("nan"), device="cuda", dtype=TYPES[kind])
+    buf[:, 3:3 + R] = torch.randn(T, R, generator=g, device="cuda").to(TYPES[kind])
+    dy = buf[:, 3:3 + R]
+    obuf = torch.full((T, d + 5), 77.0, device="cuda", dtype=TYPES[kind])
+    ctx.obc_product4_grad(P, dy, out=obuf[:, 1:1 + d])
+    want = dy.double() @ W
+    _within(obuf[:, 1:1 + d], want, _grad_bound(dy, W, want, kind))
+    assert torch.all(obuf[:, 0] == 77.0) and torch.all(obuf[:, 1 + d:] == 77.0)
+
+
+def test_product_and_its_gradient_are_adjoint(ctx):
+    """<dy, x W^T> = <dy W, x>, and a difference of products along a direction is the gradient's inner product."""
+    g = _gen(4)
+    T, R, d = 37, 210, 500
+    codes, delta, offset, W, _ = _layer(R, d, 128, g)
+    P = ctx.obc_pack4(codes, delta, offset, 128)
+    x, v = (torch.randn(T, d, generator=g, device="cuda") for _ in range(2))
+    dy = torch.randn(T, R, generator=g, device="cuda")
+    dx = ctx.obc_product4_grad(P, dy).double()
+    terms = (dy.double().abs() * (x.double().abs() @ W.abs().T)).sum()
+    assert abs((dy.double() * ctx.obc_product4(P, x).double()).sum() - (dx * x.double()).sum()) <= 2e-5 * terms
+    diff = (ctx.obc_product4(P, x + v).double() - ctx.obc_product4(P, x - v).double()) / 2
+    terms = (dy.double().abs() * ((x.double().abs() + v.double().abs()) @ W.abs().T)).sum()
+    assert abs((dy.double() * diff).sum() - (dx * v.double()).sum()) <= 4e-5 * terms
+
+
+def test_products_of_nothing(ctx):
+    g = _gen(1)
+    codes, delta, offset, W, _ = _layer(20, 40, 32, g)
+    P = ctx.obc_pack4(codes, delta, offset, 32)
+    assert ctx.obc_product4(P, torch.empty(0, 40, device="cuda")).shape == (0, 20)
+    assert ctx.obc_product4_grad(P, torch.empty(0, 20, device="cuda")).shape == (0, 40)
+    none = ctx.obc_pack4(codes[:0], delta[:0], offset[:0], 32)
+    assert ctx.obc_product4(none, torch.ones(3, 40, device="cuda")).shape == (3, 0)
+    assert torch.equal(ctx.obc_product4_grad(none, torch.empty(3, 0, device="cuda")), torch.zeros(3, 40, device="cuda"))
+
+
+def test_product_refusals(ctx):
+    import paper_2208_11580_amd as pkg
+
+    g = _gen(1)
+    codes, delta, offset, _, _ = _layer(20, 200, 32, g)
+    P = ctx.obc_pack4(codes, delta, offset, 32)
+    x = torch.ones(3, 200, device="cuda")
+    for group in (48, 16, -1, 130):
+        with pytest.raises((pkg.ObcError, ValueError)):
+            ctx.obc_pack4(codes, delta, offset, group)
+    with pytest.raises(ValueError):
+        ctx.obc_product4(P, x[:, :199])
+    with pytest.raises(ValueError):
+        ctx.obc_product4(P, x.t().contiguous().t())
+    with pytest.raises(ValueError):
+        ctx.obc_product4(P, x.double())
+    with pytest.raises(ValueError):
+        ctx.obc_product4(P, x, out=torch.empty(3, 19, device="cuda"))
+    with pytest.raises(ValueError):
+        ctx.obc_product4(P, x.cpu())
+    with pytest.raises(pkg.ObcError):
+        ctx.obc_product4(P, x, x_scale=torch.ones(3, device="cuda"))
+    with pytest.raises(pkg.ObcError):
+        ctx.obc_product4(P, x.to(torch.int8))
+    with pytest.raises(ValueError):
+        ctx.obc_product4_grad(P, x)
+    with pytest.raises(ValueError):
+        ctx.obc_product4_grad(P, torch.ones(3, 20, device="cuda", dtype=torch.int8))
+    # codes and steps that 4 bits and half precision do not hold are reported by the check
+    for code in (16, -2, -1):
+        c = codes.clone()
+        c[3, 5] = code
+        off = offset.clone()
+        off[3, 0] = -delta[3, 0] * 2.5        # between two codes: no zero for the pruned weight
+        ctx.obc_pack4(c, delta, off, 32)
+        with pytest.raises(pkg.ObcError) as e:
+            ctx.obc_check()
+        assert e.value.code == pkg.OBC_ERR_BAD_ARG
+    for value in (1e6, float("inf"), float("nan")):
+        dl = delta.clone()
+        dl[0, 0] = value
+        ctx.obc_pack4(codes, dl, offset, 32)
+        with pytest.raises(pkg.ObcError) as e:
+            ctx.obc_check()
+        assert e.value.code == pkg.OBC_ERR_NUMERIC
+    ctx.obc_check()
+
+
+@pytest.mark.parametrize("R,d,group", [(1, 1, 0), (30, 300, 32), (17, 129, 64), (40, 1000, 128), (5, 777, 0), (9, 700, 256)])
+@pytest.mark.parametrize("symmetric,zero", [(False, False), (True, False), (False, True), (True, True)])
+def test_group_grid(ctx, R, d, group, symmetric, zero):
+    g = _gen(R + d)
+    W = torch.randn(R, d, generator=g, device="cuda") * 0.05 + 0.01 * torch.randn(R, 1, generator=g, device="cuda")
+    W[0] = 0.25
+    live = (torch.rand(R, d, generator=g, device="cuda") < 0.6).to(torch.uint8)
+    if R > 2:
+        live[2] = 0
+    G = d if group <= 0 or group >= d else group
+    for mask in (None, live):
+        delta, offset, maxq = ctx.obc_group_grid(W, 4, group, live=mask, symmetric=symmetric, zero=zero)
+        ctx.obc_check()
+        assert maxq == 15 and delta.shape == (R, -(-d // G))
+        assert torch.equal(delta, delta.half().float()) and torch.equal(offset, offset.half().float())
+        assert (delta > 0).all()
+        col = torch.arange(d, device="cuda") // G
+        lo, top = offset.double()[:, col], offset.double()[:, col] + 15 * delta.double()[:, col]
+        on = torch.ones_like(W, dtype=torch.bool) if mask is None else mask.bool()
+        assert ((W.double() >= lo) & (W.double() <= top))[on].all()
+        if zero:
+            z = torch.round(-offset / delta)
+            assert torch.all(z * delta + offset == 0) and (z >= 0).all() and (z <= 15).all()
+        # no coarser than the range asks for: half precision's rounding of both numbers, seven bits with a zero, and
+        # the zero's own rounding to a code
+        w = torch.where(on, W, float("nan"))
+        pad = torch.nn.functional.pad(w, (0, delta.shape[1] * G - d), value=float("nan")).view(R, -1, G)
+        hi = pad.nan_to_num(-1e9).amax(2).double()
+        low = pad.nan_to_num(1e9).amin(2).double()
+        some = hi >= low
+        m = torch.maximum(hi.abs(), low.abs())
+        span = 2 * m if symmetric else (torch.maximum(hi, torch.zeros_like(hi)) - torch.minimum(low, torch.zeros_like(hi)) if zero else hi - low)
+        most = span / 15 * (15 / 14 * (1 + 2 ** -6) * (15 / 13.0) if zero else 1 + 2.0 ** -9) + m * 2.0 ** -10 / 15 + 1e-9
+        need = some & (span > 0)
+        assert (delta.double()[need] <= most[need] * (1.0 if not zero else 1.1)).all()
+
+
+def test_pruned_and_quantized_layer(ctx):
+    """Codes of -1 (pruned) take the grid's zero: the product is that of the sparse weights."""
+    g = _gen(3)
+    R, d = 40, 320
+    W = torch.randn(R, d, generator=g, device="cuda") * 0.05
+    live = (torch.rand(R, d, generator=g, device="cuda") < 0.5).to(torch.uint8)
+    delta, offset, maxq = ctx.obc_group_grid(W, 4, 64, live=live, zero=True)
+    col = torch.arange(d, device="cuda") // 64
+    codes = torch.round((W - offset[:, col]) / delta[:, col]).clamp(0, 15).to(torch.int32)
+    dense = torch.where(live.bool(), offset.double()[:, col] + delta.double()[:, col] * codes, 0.0)
+    codes[live == 0] = -1
+    P = ctx.obc_pack4(codes, delta, offset, 64)
+    ctx.obc_check()
+    x = torch.randn(6, d, generator=g, device="cuda")
+    want = x.double() @ dense.T
+    mag = 40.0 * delta.double()[:, col]
+    _within(ctx.obc_product4(P, x), want, _product_bound(x, mag, want, "f32", d))
+
+
+def test_codes_of_the_layer_solver(ctx):
+    """obc_quant_rows on a row's half-precision grid, packed: the product is that of its dequantized weights."""
+    import obc_inputs
+
+    W, X, _ = obc_inputs.make_layer("lin16x32", device="cuda:0")
+    Hinv = ctx.obc_invert(ctx.obc_hessian(X, damp_rel=0.01))
+    delta, offset, maxq = ctx.obc_group_grid(W, 4)
+    q = ctx.obc_quant_rows(W, Hinv, delta[:, 0].contiguous(), offset[:, 0].contiguous(), maxq)
+    P = ctx.obc_pack4(q["codes"], delta, offset)
+    ctx.obc_check()
+    x = X.t()[:50].contiguous()
+    want = x.double() @ q["W"].double().T
+    mag = 40.0 * delta.double().expand(16, 32)
+    _within(ctx.obc_product4(P, x), want, _product_bound(x, mag, want, "f32", 32) + 2.0 ** -24 * (x.double().abs() @ q["W"].double().abs().T))
+
+
+def test_layers_beyond_32_bit_offsets(ctx):
+    """Codes past 4 GB and inputs past 2^31 elements: the last rows' products and the last token's are those of small
+    layers with the same codes."""
+    g = _gen(2)
+    R, d = 16 * 4200, 131072                   # 4.4 GB of codes
+    codes, delta, offset, W, mag = _layer(32, d, 0, g)
+    small = ctx.obc_pack4(codes, delta, offset)
+    import paper_2208_11580_amd as pkg
+    import ctypes
+
+    need = ctypes.c_size_t()
+    assert ctx.lib.obc_pack4_bytes(R, d, 0, ctypes.byref(need)) == 0 and need.value > 2 ** 32
+    data = torch.zeros(need.value, dtype=torch.uint8, device="cuda")
+    tile_bytes = 2 * (d // 128) * 1024           # two blocks of 16 rows
+    codes_bytes = (R // 16) * (d // 128) * 1024
+    data[codes_bytes - tile_bytes:codes_bytes] = small.data[:tile_bytes]
+    data[codes_bytes + (R - 32) * 4:codes_bytes + R * 4] = small.data[tile_bytes:tile_bytes + 128]
+    big = pkg.Packed4(data, R, d, 0)
+    for T in (3, 100):
+        x = torch.randn(T, d, generator=g, device="cuda").bfloat16()
+        y = ctx.obc_product4(big, x)
+        assert torch.equal(y[:, -32:], ctx.obc_product4(small, x)) and not y[:, :-32].any()
+    dy = torch.zeros(4, R, device="cuda")
+    dy[:, -32:] = torch.randn(4, 32, generator=g, device="cuda")
+    want = dy[:, -32:].double() @ W
+    _within(ctx.obc_product4_grad(big, dy), want, _grad_bound(dy[:, -32:], W, want, "f32"))
+    del big, data, dy
+    # 17 tokens, 2^27 + 3 elements apart
+    ld = 2 ** 27 + 3
+    buf = torch.zeros(16 * ld + d, dtype=torch.bfloat16, device="cuda")
+    x = buf.as_strided((17, d), (ld, 1))
+    x.copy_(torch.randn(17, d, generator=g, device="cuda"))
+    assert torch.equal(ctx.obc_product4(small, x), ctx.obc_product4(small, x.contiguous()))
+
+
+def test_work_on_a_stream_of_its_own():
+    """A context on another stream, with its input written there just before."""
+    import paper_2208_11580_amd as pkg
+
+    side = torch.cuda.Stream()
+    ctx = pkg.Context(side)
+    g = _gen(12)
+    codes, delta, offset, W, mag = _layer(256, 2048, 128, g)
+    x = torch.randn(9, 2048, generator=g, device="cuda")
+    torch.cuda.synchronize()
+    P = ctx.obc_pack4(codes, delta, offset, 128)
+    with torch.cuda.stream(side):
+        x2 = x * 2.0
+    y = ctx.obc_product4(P, x2)
+    side.synchronize()
+    want = 2.0 * x.double() @ W.T
+    _within(y, want, _product_bound(2 * x, mag, want, "f32", 2048))
+    ctx.close()
+
+
+# ------------------------------------------------------------------------------------------------- norm
+NORMS = [(1, 1), (1, 7), (3, 64), (2, 1000), (5, 2047), (4, 2048), (3, 2049), (1, 4096), (7, 5001), (2, 8192), (3, 8195),
+         (2, 16384), (2, 16391), (1, 40000), (1, 65536), (300, 512), (700, 96)]
+
+
+def _norm_inputs(T, d, kind, seed):
+    g = _gen(seed)
+    x = torch.randn(T, d, generator=g, device="cuda").to(TYPES[kind])
+    r = (3 * torch.randn(T, d, generator=g, device="cuda")).to(TYPES[kind])
+    gain = 1 + 0.3 * torch.randn(d, generator=g, device="cuda")
+    return x, r, gain, g
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T,d", NORMS)
+def test_rmsnorm(ctx, T, d, kind):
+    x, r, gain, _ = _norm_inputs(T, d, kind, T + d)
+    for res in (r, None):
+        out = ctx.obc_rmsnorm(x, gain, eps=1e-5, residual=res, want_rstd=True)
+        q = ctx.obc_rmsnorm(x, gain, eps=1e-5, residual=res, quant8=True)
+        ctx.obc_check()
+        h = x.double() + (res.double() if res is not None else 0.0)
+        rstd = 1 / torch.sqrt(h.square().mean(1) + 1e-5)
+        y = h * rstd[:, None] * gain.double()
+        # 64 terms a thread at most, then a tree of ten steps
+        rel = 100 * U32
+        _within(out["h"], h, ROUND[kind] * 1.01 * h.abs() + TINY[kind])
+        _within(out["rstd"], rstd, rel * rstd)
+        _within(out["y"], y, (rel + ROUND[kind] * 1.01) * y.abs() + TINY[kind])
+        top = y.abs().amax(1)
+        _within(q["scale"], top / 127, 2 * rel * top / 127)
+        t = y / (top[:, None] / 127)
+        code = q["y"].double()
+        assert ((code - t).abs() <= 0.5 + 127 * 2 * rel).all() and code.abs().max() <= 127
+        assert torch.equal(q["h"], out["h"])
+
+
+def test_rmsnorm_rows_that_hold_nothing_or_too_much(ctx):
+    for kind in TYPES:
+        for d in (8, 500, 5000):
+            x, r, gain, _ = _norm_inputs(6, d, kind, d)
+            x[0] = 0
+            x[1, d // 2] = float("nan")
+            x[2, d - 1] = float("inf")
+            x[3] = 1e-30 if kind != "f16" else 6e-8       # squares vanish in fp32 (half precision: its smallest number)
+            out = ctx.obc_rmsnorm(x, gain, eps=1e-6)
+            q = ctx.obc_rmsnorm(x, gain, eps=1e-6, quant8=True)
+            assert not out["y"][0].any() and not q["y"][0].any() and q["scale"][0] == 1
+            for t in (1, 2):
+                assert torch.isnan(q["scale"][t]) and not q["y"][t].any()
+                assert not torch.isfinite(out["y"][t].float()).all()
+            h = x[3].double()
+            y = h / torch.sqrt(h.square().mean() + 1e-6) * gain.double()
+            code = q["y"][3].double()
+            assert ((code - y / y.abs().max() * 127).abs() <= 0.5 + 1e-2).all() and code.abs().max() == 127
+            for t in (4, 5):
+                h = x[t].double()
+                y = h / torch.sqrt(h.square().mean() + 1e-6) * gain.double()
+                assert ((q["y"][t].double() * q["scale"][t].double() - y).abs() <= 0.51 * q["scale"][t].double()).all()
+
+
+def test_rmsnorm_in_place(ctx):
+    x, r, gain, _ = _norm_inputs(33, 777, "bf16", 1)
+    want = ctx.obc_rmsnorm(x, gain, residual=r)
+    x2, r2 = x.clone(), r.clone()
+    got = ctx.obc_rmsnorm(x2, gain, residual=r2, out={"h": r2, "y": x2})
+    assert torch.equal(got["h"], want["h"]) and torch.equal(got["y"], want["y"]) and got["h"] is r2
+
+
+def _norm_grad(h, gain, rstd, dy, dh):
+    xh = h * rstd[:, None]
+    gy = dy * gain
+    return dh + rstd[:, None] * (gy - xh * (gy * xh).mean(1, keepdim=True)), (dy * xh).sum(0)
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T,d", NORMS + [(1500, 40), (2100, 3)])
+def test_rmsnorm_grad(ctx, T, d, kind):
+    h, dh, gain, g = _norm_inputs(T, d, kind, T + 2 * d)
+    dy = torch.randn(T, d, generator=g, device="cuda").to(TYPES[kind])
+    rstd = (h.float().square().mean(1) + 1e-6).rsqrt()
+    for add in (dh, None):
+        out = ctx.obc_rmsnorm_grad(h, gain, rstd, dy, dh=add)
+        ctx.obc_check()
+        wide = [t.double() for t in (h, gain, rstd, dy)]
+        dx, dgain = _norm_grad(*wide, add.double() if add is not None else torch.zeros_like(wide[0]))
+        xh, gy = wide[0] * wide[2][:, None], wide[3] * wide[1]
+        mag = wide[2][:, None] * (gy.abs() + xh.abs() * (gy * xh).abs().mean(1, keepdim=True))
+        if add is not None:
+            mag = mag + add.double().abs()
+        _within(out["dx"], dx, 100 * U32 * mag + ROUND[kind] * 1.01 * dx.abs() + TINY[kind])
+        _within(out["dgain"], dgain, (T + 32) * U32 * (wide[3] * xh).abs().sum(0) + 1e-30)
+        again = ctx.obc_rmsnorm_grad(h, gain, rstd, dy, dh=add)
+        assert torch.equal(out["dgain"], again["dgain"]) and torch.equal(out["dx"], again["dx"])
+
+
+def test_rmsnorm_grad_against_differences(ctx):
+    h, v, gain, g = _norm_inputs(6, 300, "f32", 77)
+    dy = torch.randn(6, 300, generator=g, device="cuda")
+    vg = torch.randn(300, generator=g, device="cuda")
+    out = ctx.obc_rmsnorm(h, gain, want_rstd=True)
+    grad = ctx.obc_rmsnorm_grad(h, gain, out["rstd"], dy)
+
+    def value(a, b):
+        return (ctx.obc_rmsnorm(a, b)["y"].double() * dy.double()).sum()
+
+    e = 2.0 ** -7
+    dx = (value(h + e * v, gain) - value(h - e * v, gain)) / (2 * e)
+    dg = (value(h, gain + e * vg) - value(h, gain - e * vg)) / (2 * e)
+
+    def value64(a):
+        return (a / torch.sqrt(a.square().mean(1, keepdim=True) + 1e-6) * gain.double() * dy.double()).sum()
+
+    # the quotient's own distance from the derivative, in 64 bits; rounding is 2^-23 of 1800 terms of size about 1 over e
+    quotient = (value64(h.double() + e * v.double()) - value64(h.double() - e * v.double())) / (2 * e)
+    want, _ = _norm_grad(h.double(), gain.double(), 1 / torch.sqrt(h.double().square().mean(1) + 1e-6), dy.double(), 0.0)
+    curved = abs(quotient - (want * v.double()).sum())
+    assert abs(dx - (grad["dx"].double() * v.double()).sum()) <= 0.05 + curved
+    assert abs(dg - (grad["dgain"].double() * vg.double()).sum()) <= 0.05
+
+
+def test_norm_of_nothing_and_refusals(ctx):
+    import paper_2208_11580_amd as pkg
+
+    gain = torch.ones(16, device="cuda")
+    none = torch.empty(0, 16, device="cuda")
+    assert ctx.obc_rmsnorm(none, gain)["y"].shape == (0, 16)
+    out = ctx.obc_rmsnorm_grad(none, gain, torch.empty(0, device="cuda"), none)
+    assert out["dx"].shape == (0, 16) and not out["dgain"].any()
+    x = torch.ones(4, 16, device="cuda")
+    for bad in (dict(gain=gain[:15]), dict(gain=gain.half()), dict(residual=x.half()), dict(residual=x[:3]),
+                dict(x=x.t()), dict(x=x.cpu()), dict(x=x.double()), dict(out={"y": x.half()})):
+        with pytest.raises((ValueError, pkg.ObcError)):
+            ctx.obc_rmsnorm(bad.pop("x", x), bad.pop("gain", gain), **bad)
+    with pytest.raises(pkg.ObcError):
+        ctx.obc_rmsnorm(x, gain, eps=-1.0)
+    with pytest.raises(pkg.ObcError):
+        ctx.obc_rmsnorm(torch.ones(1, 65537, device="cuda"), torch.ones(65537, device="cuda"))
+    with pytest.raises(ValueError):
+        ctx.obc_rmsnorm_grad(x, gain, torch.ones(3, device="cuda"), x)
+
+
+# --------------------------------------------------------------------------------------------- distillation
+def _distill(z, index, logit, tau, weight):
+    """Loss and gradient in 64 bits, a row at a time; a bound on the fp32 arithmetic's error with each."""
+    T, V = z.shape
+    loss = torch.zeros(T, dtype=torch.float64)
+    dz = torch.zeros(T, V, dtype=torch.float64)
+    lb, db = torch.zeros_like(loss), torch.zeros_like(dz)
+    z, index, logit, weight = z.double().cpu(), index.cpu(), logit.double().cpu(), weight.double().cpu()
+    for t in range(T):
+        on = [j for j in range(index.shape[1]) if 0 <= int(index[t, j]) < V and logit[t, j] > float("-inf")]
+        w = float(weight[t])
+        if not on or w == 0.0:
+            continue
+        lq = torch.log_softmax(z[t] / tau, 0)
+        lp = torch.log_softmax(logit[t, on] / tau, 0)
+        at = index[t, on].long()
+        loss[t] = w * tau * tau * (lp.exp() * (lp - lq[at])).sum()
+        q, p = lq.exp(), torch.zeros(V, dtype=torch.float64).index_add_(0, at, lp.exp())
+        dz[t] = w * tau * (q - p)
+        # exponents carry 2^-22 of their argument, sums 150 roundings
+        lb[t] = w * tau * tau * (200 * U32 + 20 * U32 * (lp.exp() * (lp.abs() + lq[at].abs())).sum())
+        db[t] = w * tau * ((200 + 16 * (z[t] / tau - (z[t] / tau).max()).abs()) * U32 * q
+                           + (200 + 16 * float((logit[t, on].max() - logit[t, on].min()) / tau)) * U32 * p)
+    return loss, dz, lb, db
+
+
+def _logits(T, V, k, kind, seed):
+    g = _gen(seed)
+    z = (3 * torch.randn(T, V, generator=g, device="cuda")).to(TYPES[kind])
+    t = z.float() * 0.7 + 2 * torch.randn(T, V, generator=g, device="cuda")
+    top = t.topk(k, dim=1)
+    return z, top.indices.to(torch.int32), top.values.contiguous(), torch.rand(T, generator=g, device="cuda") + 0.1, g
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T,V,k,tau", [(1, 1, 1, 1.0), (2, 5, 5, 0.5), (3, 100, 7, 2.0), (1, 1023, 64, 1.0), (5, 4097, 20, 3.0),
+                                       (2, 32000, 256, 1.0), (2, 50001, 64, 0.7), (1, 131072, 1000, 1.5), (1, 200003, 33, 1.0),
+                                       (40, 777, 3, 1.0)])
+def test_distill(ctx, T, V, k, tau, kind):
+    k = min(k, V)
+    z, index, logit, weight, g = _logits(T, V, k, kind, T + V)
+    count = torch.randint(1, k + 1, (T, 1), generator=g, device="cuda")
+    index = torch.where(torch.arange(k, device="cuda") < count, index, -1).to(torch.int32)
+    out = ctx.obc_distill(z, index, logit, temperature=tau, weight=weight, want_grad=True)
+    ctx.obc_check()
+    loss, dz, lb, db = _distill(z, index, logit, tau, weight)
+    _within(out["loss"].cpu(), loss, lb + 2 * U32 * loss.abs())
+    _within(out["dz"].cpu(), dz, db + ROUND[kind] * 1.01 * dz.abs() + max(TINY[kind], 1e-38))
+    alone = ctx.obc_distill(z, index, logit, temperature=tau, weight=weight)
+    assert torch.equal(alone["loss"], out["loss"]) and alone["dz"] is None
+    again = z.clone()
+    over = ctx.obc_distill(again, index, logit, temperature=tau, weight=weight, want_grad=True, out={"dz": again})
+    assert torch.equal(over["dz"], out["dz"]) and over["dz"] is again
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("V", [50, 3001, 70001])
+def test_distill_rows_and_entries_that_do_not_count(ctx, V, kind):
+    inf = float("inf")
+    z, index, logit, weight, g = _logits(9, V, 6, kind, V)
+    z[0], z[1] = float("nan"), inf
+    weight[0] = 0.0                                # masked: its NaN stays inside
+    index[1] = -1                                  # no entry at all
+    logit[2, 3:] = -inf                            # entries without mass
+    logit[3] = -inf                                # only such
+    index[4, 1] = index[4, 0]                      # a token named twice
+    index[5, 2:] = -7
+    z[6, 40] = -inf                                # a token the student excludes, which the teacher does not name
+    index[6] = torch.where(index[6] == 40, -1, index[6])
+    z[7, :] = z[7, 0]                              # all alike
+    z[8, 3] = torch.finfo(TYPES[kind]).min         # a mask of the type's lowest value
+    index[8] = torch.where(index[8] == 3, -1, index[8])
+    out = ctx.obc_distill(z, index, logit, weight=weight, want_grad=True)
+    ctx.obc_check()
+    assert out["loss"][0] == 0 and out["loss"][1] == 0 and out["loss"][3] == 0
+    assert not out["dz"][0].any() and not out["dz"][1].any() and not out["dz"][3].any()
+    assert out["dz"][6, 40] == 0 and out["dz"][8, 3] == 0
+    rows = [2, 4, 5, 6, 7, 8]
+    loss, dz, lb, db = _distill(z[rows], index[rows], logit[rows], 1.0, weight[rows])
+    _within(out["loss"][rows].cpu(), loss, lb + 2 * U32 * loss.abs())
+    _within(out["dz"][rows].cpu(), dz, (db + ROUND[kind] * 1.01 * dz.abs() + max(TINY[kind], 1e-38)).nan_to_num(1e-38))
+
+
+def test_distill_of_strided_rows_and_no_weight(ctx):
+    for kind in TYPES:
+        for V in (333, 40001):
+            z, index, logit, _, _ = _logits(5, V, 9, kind, 3)
+            buf = torch.full((5, V + 4), float("nan"), device="cuda", dtype=TYPES[kind])
+            buf[:, 1:1 + V] = z
+            dbuf = torch.full((5, V + 3), 7.0, device="cuda", dtype=TYPES[kind])
+            out = ctx.obc_distill(buf[:, 1:1 + V], index, logit, want_grad=True, out={"dz": dbuf[:, 2:2 + V]})
+            want = ctx.obc_distill(z, index, logit, weight=torch.ones(5, device="cuda"), want_grad=True)
+            assert torch.equal(out["loss"], want["loss"]) and torch.equal(dbuf[:, 2:2 + V], want["dz"])
+            assert torch.all(dbuf[:, :2] == 7.0) and torch.all(dbuf[:, 2 + V:] == 7.0)
+
+
+def test_distill_against_differences(ctx):
+    z, index, logit, weight, g = _logits(4, 600, 12, "f32", 8)
+    v = torch.randn(4, 600, generator=g, device="cuda")
+    e = 2.0 ** -6
+
+    def value(a):
+        return ctx.obc_distill(a, index, logit, temperature=1.7, weight=weight)["loss"].double().sum()
+
+    dz = ctx.obc_distill(z, index, logit, temperature=1.7, weight=weight, want_grad=True)["dz"]
+    # rounding: losses of about 10 to 2^-21, over e; curvature: third derivatives below e^2 |v|^3
+    assert abs((value(z + e * v) - value(z - e * v)) / (2 * e) - (dz.double() * v.double()).sum()) <= 2e-2
+
+
+def test_distill_refusals(ctx):
+    import paper_2208_11580_amd as pkg
+
+    z, index, logit, weight, _ = _logits(3, 50, 4, "f32", 1)
+    assert ctx.obc_distill(z[:0], index[:0], logit[:0], want_grad=True)["loss"].shape == (0,)
+    none = ctx.obc_distill(z, index[:, :0], logit[:, :0], want_grad=True)
+    assert not none["loss"].any() and not none["dz"].any()
+    bad = index.clone()
+    bad[1, 2] = 50
+    ctx.obc_distill(z, bad, logit)
+    with pytest.raises(pkg.ObcError) as e:
+        ctx.obc_check()
+    assert e.value.code == pkg.OBC_ERR_BAD_ARG
+    for tau in (0.0, -1.0, float("nan"), float("inf")):
+        with pytest.raises(pkg.ObcError):
+            ctx.obc_distill(z, index, logit, temperature=tau)
+    with pytest.raises(pkg.ObcError):
+        ctx.obc_distill(torch.zeros(1, 2000, device="cuda"), torch.zeros(1, 1025, dtype=torch.int32, device="cuda"),
+                        torch.zeros(1, 1025, device="cuda"))
+    with pytest.raises(ValueError):
+        ctx.obc_distill(z, index[:2], logit[:2])
+    with pytest.raises(ValueError):
+        ctx.obc_distill(z, index.long(), logit)
+    with pytest.raises(ValueError):
+        ctx.obc_distill(z, index, logit, weight=weight.double())
+    ctx.obc_check()
