@@ -23,16 +23,19 @@ typedef float floatx4_at4 __attribute__((ext_vector_type(4), aligned(4)));
 // code's bits at the bottom of the mantissa would give, cost five or eight.)
 constexpr float kCodeBase = 16.f;
 
-// dword i of the operand holds the columns 2 i and 2 i + 1
+// dword i of the operand holds the columns 2 i and 2 i + 1.  (Mask and base in registers of either kind: an instruction
+// has room for one constant, and with two the and and the or become two instructions.)
 __device__ inline uintx4 codes_bf16(unsigned w)
 {
-    constexpr unsigned mask = 0x00780078u, base = 0x41804180u;
+    unsigned mask = 0x00780078u, base = 0x41804180u;
+    asm("" : "+s"(mask), "+v"(base));
     return uintx4{((w << 3) & mask) | base, ((w >> 1) & mask) | base, ((w >> 5) & mask) | base, ((w >> 9) & mask) | base};
 }
 
 __device__ inline uintx4 codes_f16(unsigned w)
 {
-    constexpr unsigned mask = 0x03c003c0u, base = 0x4c004c00u;
+    unsigned mask = 0x03c003c0u, base = 0x4c004c00u;
+    asm("" : "+s"(mask), "+v"(base));
     return uintx4{((w << 6) & mask) | base, ((w << 2) & mask) | base, ((w >> 2) & mask) | base, ((w >> 6) & mask) | base};
 }
 

@@ -210,11 +210,309 @@ __global__ __launch_bounds__(WAVES * 64) void product4_rows_kernel(Args a, int y
     }
 }
 
+
+// ---- many tokens ------------------------------------------------------------------------------
+// The tokens as product4_tiles_kernel takes them: rows at multiples of 16 bytes, columns up to a multiple of 128, zeros
+// from d on; fp32 as three planes of bf16 terms.  Only where x is not like that already.
+template <int XT>
+__global__ __launch_bounds__(256) void product4_lay_kernel(const void *x, int64_t ldx, int d, int pieces, int64_t jobs, int64_t plane,
+                                                           uintx4 *out)
+{
+    constexpr int E = XT == OBC_I8 ? 16 : 8;
+    const int64_t job = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (job >= jobs) return;
+    const int64_t t = job / pieces;
+    const int c = (int)(job - t * pieces) * E;
+    const int64_t at = t * ldx + c;
+    if constexpr (XT == OBC_I8) {
+        uintx4 v = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            if (c + j < d) v[j >> 2] |= (unsigned)((const uint8_t *)x)[at + j] << (8 * (j & 3));
+        out[job] = v;
+    } else {
+        Operand<XT> o;
+        o.load(x, at, d - c);
+        if constexpr (XT == OBC_F32) {
+            out[job] = o.v[0];
+            out[job + plane] = o.v[1];
+            out[job + 2 * plane] = o.v[2];
+        } else {
+            out[job] = o.v;
+        }
+    }
+}
+
+template <int V>
+struct Type {
+    static constexpr int value = V;
+};
+
+struct Tokens {
+    const char *x;           // first plane
+    int64_t ld, plane;       // bytes between rows, between planes
+};
+
+typedef __attribute__((address_space(1))) const void *global_ptr;
+typedef __attribute__((address_space(3))) void *lds_ptr;
+
+// BM tokens x 128 rows of W to a workgroup of 2 x 2 waves, BM / 2 x 64 each.  The tokens go through LDS, two tiles
+// in turn; a wave's codes come straight from memory in operand order and are unpacked once for its BM / 2 tokens.
+// The inputs' sums of every group are kept in LDS and meet the offsets in one fp32 product of matrices at the end.
+constexpr int kWaitVm0 = 0x0f70;    // s_waitcnt vmcnt(0), the other counters not waited for
+constexpr int kSumGroups = 32;      // groups whose sums LDS holds; more are worked off in between
+
+template <int XT, int SUB, int BM>
+__global__ __launch_bounds__(256, 2) void product4_tiles_kernel(Args a, Tokens tok, int y_type, int mtiles)
+{
+    constexpr int P = XT == OBC_F32 ? 3 : 1, MF = BM / 32;
+    constexpr int ROW = XT == OBC_I8 ? 8 : 16;      // 16-byte pieces of a token's 128 columns
+    // two arrays, not one of two: the compiler then knows that reading one does not wait for loads to the other
+    __shared__ uintx4 even[P * BM * ROW], odd[P * BM * ROW];
+    __shared__ float sums[kSumGroups][BM];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int n = lane & 15, quad = lane >> 4;
+    const int wm = wave & 1, wn = wave >> 1;
+    // consecutive workgroups go to different dies: give each die a run of tiles
+    const int tiles = gridDim.x, per = tiles >> 3, left = tiles & 7, die = blockIdx.x & 7;
+    const int tile = die * per + (die < left ? die : left) + (blockIdx.x >> 3);
+    const int t0 = (tile % mtiles) * BM, rb0 = (tile / mtiles) * 8 + wn * 4;
+    constexpr float base = XT == OBC_I8 ? 0.f : kCodeBase;
+    floatx4 acc[MF][4];
+#pragma unroll
+    for (int m = 0; m < MF; ++m)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[m][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    int64_t rb[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) rb[j] = rb0 + j < a.RB ? rb0 + j : a.RB - 1;      // beyond the last: not stored
+    // Piece o of token t lies at place o ^ (t mod ROW) of its row, so that the 16 tokens of an operand lie in different
+    // banks.  The lanes of a load to LDS write 64 places in a row: each fetches the piece that belongs to its place.
+    auto fetch = [&](int kt, uintx4 *lds) {
+        constexpr int TOK = 64 / ROW;      // tokens of one load
+#pragma unroll
+        for (int i = 0; i < P * BM / TOK / 4; ++i) {
+            const int first = (i * 4 + wave) * TOK;                  // row of the planes, one below the other
+            const int p = P > 1 ? first / BM : 0, t = first - p * BM + lane / ROW;
+            const int row = t0 + t < a.T ? t0 + t : a.T - 1;
+            const char *src = tok.x + p * tok.plane + row * tok.ld + (int64_t)kt * (ROW * 16) + ((lane % ROW) ^ (t % ROW)) * 16;
+            __builtin_amdgcn_global_load_lds((global_ptr)src, (lds_ptr)(lds + first * ROW), 16, 0, 0);
+        }
+    };
+    auto operand = [&](const uintx4 *lds, int p, int m, int o) {
+        return lds[(p * BM + 16 * m + n) * ROW + (o ^ (n & (ROW - 1)))];
+    };
+    // 8-bit inputs: the eight columns of step k, in the codes' order
+    auto operand8 = [&](const uintx4 *lds, int m, int k) {
+        const int e = 4 * k + quad;
+        return bytes_like_codes(((const uintx2 *)lds)[((16 * m + n) * ROW + ((e >> 1) ^ (n & (ROW - 1)))) * 2 + (e & 1)]);
+    };
+    // sums x offsets of the groups [g0, g0 + count): four groups to an instruction
+    auto offsets = [&](int g0, int count) {
+        for (int g = 0; g < count; g += 4) {
+            const bool in = g + quad < count;
+            float b[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                unsigned sc = 0;
+                if (in) {
+                    const int at = g0 + g + quad;
+                    sc = SUB > 1 ? a.scales[((rb[j] * a.KT + at / SUB) * 16 + n) * SUB + at % SUB]
+                                 : a.scales[(rb[j] * a.NG + at / a.tpg) * 16 + n];
+                }
+                b[j] = half_hi(sc) - base * half_lo(sc);
+            }
+#pragma unroll
+            for (int m = 0; m < MF; ++m) {
+                const float s = in ? sums[g + quad][wm * (BM / 2) + 16 * m + n] : 0.f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[m][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(s, b[j], acc[m][j], 0, 0, 0);
+            }
+        }
+    };
+    uintx4 codes[4];
+    unsigned scale[4][SUB];
+    auto fetch_codes = [&](int kt) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            codes[j] = a.codes[(rb[j] * a.KT + kt) * 64 + lane];
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
+                scale[j][u] = SUB > 1 ? a.scales[((rb[j] * a.KT + kt) * 16 + n) * SUB + u] : a.scales[(rb[j] * a.NG + kt / a.tpg) * 16 + n];
+        }
+    };
+    fetch(0, even);
+    fetch_codes(0);
+    __builtin_amdgcn_s_waitcnt(kWaitVm0);
+    __syncthreads();
+    int done = 0;      // tiles whose offsets are in
+    auto turn = [&](const int kt, const uintx4 *lds, uintx4 *lds_next) __attribute__((always_inline)) {
+        uintx4 w[4];
+        float step[4][SUB];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            w[j] = codes[j];
+#pragma unroll
+            for (int u = 0; u < SUB; ++u) step[j][u] = half_lo(scale[j][u]);
+        }
+        // (the last tile again after the last: a branch here would make the compiler wait for all of it at once)
+        const int ahead = kt + 1 < a.KT ? kt + 1 : kt;
+        fetch(ahead, lds_next);
+        fetch_codes(ahead);
+        // the tile's sums, a quarter of the tokens to each wave
+        for (int m = wave; m < BM / 16; m += 4) {
+#pragma unroll
+            for (int u = 0; u < SUB; ++u) {
+                Sum<XT> s;
+#pragma unroll
+                for (int k = u * 4 / SUB; k < (u + 1) * 4 / SUB; ++k) {
+                    Operand<XT> x;
+                    if constexpr (XT == OBC_F32) {
+#pragma unroll
+                        for (int p = 0; p < 3; ++p) x.v[p] = operand(lds, p, m, 4 * k + quad);
+                    } else if constexpr (XT == OBC_I8) {
+                        x.v = operand8(lds, m, k);
+                    } else {
+                        x.v = operand(lds, 0, m, 4 * k + quad);
+                    }
+                    s.add(x, Codes<XT>::ones());
+                }
+                if (n == 0)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sums[(kt - done) * SUB + u][16 * m + 4 * quad + i] = s[i];
+            }
+        }
+        uintx4 B[4][XT == OBC_I8 ? 2 : 4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if constexpr (XT == OBC_I8) {
+                    const uintx2 c = codes_i8(w[j][k]);
+                    B[j][k >> 1][2 * (k & 1)] = c.x;
+                    B[j][k >> 1][2 * (k & 1) + 1] = c.y;
+                } else {
+                    B[j][k] = XT == OBC_F16 ? codes_f16(w[j][k]) : codes_bf16(w[j][k]);
+                }
+            }
+#pragma unroll
+        for (int m = 0; m < MF; ++m) {
+            const int mm = wm * MF + m;
+            if constexpr (XT == OBC_I8) {
+                uintx4 A[2];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uintx2 x = operand8(lds, mm, k);
+                    A[k >> 1][2 * (k & 1)] = x.x;
+                    A[k >> 1][2 * (k & 1) + 1] = x.y;
+                }
+#pragma unroll
+                for (int u = 0; u < SUB; ++u) {
+                    intx4 S[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        S[j] = intx4{0, 0, 0, 0};
+                        if constexpr (SUB == 4) {
+                            const uintx4 x = A[u >> 1], b = B[j][u >> 1];
+                            S[j] = u & 1 ? mfma_i8(uintx2{x.z, x.w}, uintx2{b.z, b.w}, S[j]) : mfma_i8(uintx2{x.x, x.y}, uintx2{b.x, b.y}, S[j]);
+                        } else {
+#pragma unroll
+                            for (int k = u * 2 / SUB; k < (u + 1) * 2 / SUB; ++k)
+                                S[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(intx4, A[k]), __builtin_bit_cast(intx4, B[j][k]), S[j], 0, 0, 0);
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[m][j][i] = fmaf(step[j][u], (float)S[j][i], acc[m][j][i]);
+                }
+            } else {
+#pragma unroll
+                for (int u = 0; u < SUB; ++u) {
+                    floatx4 S[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) S[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int k = u * 4 / SUB; k < (u + 1) * 4 / SUB; ++k) {
+#pragma unroll
+                        for (int p = P - 1; p >= 0; --p) {
+                            const uintx4 A = operand(lds, p, mm, 4 * k + quad);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) S[j] = XT == OBC_F16 ? mfma_f16(A, B[j][k], S[j]) : mfma_bf16(A, B[j][k], S[j]);
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[m][j][i] = fmaf(step[j][u], S[j][i], acc[m][j][i]);
+                }
+            }
+        }
+        __builtin_amdgcn_s_waitcnt(kWaitVm0);      // the next tile is in LDS
+        __syncthreads();
+        if ((kt + 1 - done + 1) * SUB > kSumGroups || kt + 1 == a.KT) {
+            offsets(done * SUB, (kt + 1 - done) * SUB);
+            done = kt + 1;
+            __syncthreads();
+        }
+    };
+    for (int kt = 0;; kt += 2) {
+        turn(kt, even, odd);
+        if (kt + 1 >= a.KT) break;
+        turn(kt + 1, odd, even);
+        if (kt + 2 >= a.KT) break;
+    }
+    auto put = [&](auto type) {
+        constexpr int YT = decltype(type)::value;
+#pragma unroll
+        for (int m = 0; m < MF; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int t = t0 + wm * (BM / 2) + 16 * m + 4 * quad + i;
+                if (t >= a.T) continue;
+                const float xs = XT == OBC_I8 ? a.xs[t] : 1.f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int r = (rb0 + j) * 16 + n;
+                    if (r < a.R) store_as<YT>(a.y, (int64_t)t * a.ldy + r, XT == OBC_I8 ? acc[m][j][i] * xs : acc[m][j][i]);
+                }
+            }
+    };
+    if (y_type == OBC_F32) put(Type<OBC_F32>());
+    else if (y_type == OBC_F16) put(Type<OBC_F16>());
+    else put(Type<OBC_BF16>());
+}
+
+// True where the tiles' kernel can read x as it lies.
+inline bool laid_out(const void *x, int x_type, int64_t ldx, int d)
+{
+    return x_type != OBC_F32 && d % 128 == 0 && ((uintptr_t)x & 15) == 0 && (ldx * (int64_t)size_of_type(x_type)) % 16 == 0;
+}
+
+inline size_t laid_bytes(int T, int KT, int x_type)
+{
+    return (size_t)T * KT * 128 * (x_type == OBC_F32 ? 6 : x_type == OBC_I8 ? 1 : 2);
+}
+
 template <int XT, int SUB>
-int launch(obc_ctx *ctx, const Args &a, int y_type)
+int launch(obc_ctx *ctx, const Args &a, int y_type, void *ws)
 {
     if (a.T <= 16) {
         product4_rows_kernel<XT, SUB, 1, 8><<<dim3(a.RB, 1), 512, 0, ctx->stream>>>(a, y_type);
+    } else if (a.T > 64) {
+        constexpr int BM = XT == OBC_F32 ? 64 : 128;
+        const int mtiles = a.T / BM + (a.T % BM != 0), ntiles = (a.RB + 7) / 8;
+        if ((int64_t)mtiles * ntiles > 0x7fffffff) return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_product4: too many tiles");
+        Tokens tok = {(const char *)a.x, a.ldx * (int64_t)size_of_type(XT), 0};
+        if (!laid_out(a.x, XT, a.ldx, a.d)) {
+            const int pieces = a.KT * (XT == OBC_I8 ? 8 : 16);
+            const int64_t jobs = (int64_t)a.T * pieces;
+            if ((jobs + 255) / 256 > 0x7fffffff) return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_product4: too many inputs");
+            product4_lay_kernel<XT><<<(unsigned)((jobs + 255) / 256), 256, 0, ctx->stream>>>(a.x, a.ldx, a.d, pieces, jobs, jobs, (uintx4 *)ws);
+            OBC_LAUNCH_CHECK(ctx, "product4_lay_kernel");
+            tok = Tokens{(const char *)ws, (int64_t)pieces * 16, jobs * 16};
+        }
+        product4_tiles_kernel<XT, SUB, BM><<<mtiles * ntiles, 256, 0, ctx->stream>>>(a, tok, y_type, mtiles);
     } else {
         const int per = 64, blocks = (a.T + per - 1) / per;
         for (int b0 = 0; b0 < blocks; b0 += 65535) {
@@ -233,9 +531,9 @@ int launch(obc_ctx *ctx, const Args &a, int y_type)
 }
 
 template <int XT>
-int launch_sub(obc_ctx *ctx, const Args &a, int sub, int y_type)
+int launch_sub(obc_ctx *ctx, const Args &a, int sub, int y_type, void *ws)
 {
-    return sub == 1 ? launch<XT, 1>(ctx, a, y_type) : sub == 2 ? launch<XT, 2>(ctx, a, y_type) : launch<XT, 4>(ctx, a, y_type);
+    return sub == 1 ? launch<XT, 1>(ctx, a, y_type, ws) : sub == 2 ? launch<XT, 2>(ctx, a, y_type, ws) : launch<XT, 4>(ctx, a, y_type, ws);
 }
 
 }  // namespace
@@ -247,7 +545,8 @@ int obc_product4_workspace_bytes(int T, int R, int d, int group, int x_type, siz
     pack4_layout L;
     if (!bytes || T < 0 || R < 0 || d <= 0 || !(float_type(x_type) || x_type == OBC_I8) || !pack4_layout_of(R, d, group, &L))
         return OBC_ERR_BAD_ARG;
-    *bytes = 0;
+    // rows that are not laid out for the tiles' kernel; a workspace for T tokens serves fewer
+    *bytes = T > 64 ? laid_bytes(T, L.KT, x_type) : 0;
     return OBC_OK;
 }
 
@@ -269,8 +568,8 @@ int obc_product4(obc_ctx *ctx, const void *packed, int R, int d, int group, cons
     if (((uintptr_t)packed & 15) != 0) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_product4: packed is not aligned to 16 bytes");
     if (((uintptr_t)x & (size_of_type(x_type) - 1)) != 0 || ((uintptr_t)y & (size_of_type(y_type) - 1)) != 0)
         return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_product4: x or y is not aligned to its elements");
-    (void)ws;
-    (void)ws_bytes;
+    if (T > 64 && !laid_out(x, x_type, ldx, d) && (!ws || ((uintptr_t)ws & 15) != 0 || ws_bytes < laid_bytes(T, L.KT, x_type)))
+        return obc_fail(ctx, OBC_ERR_WORKSPACE, "obc_product4: workspace of %zu bytes needed", laid_bytes(T, L.KT, x_type));
     Args a;
     a.codes = (const uintx4 *)packed;
     a.scales = (const unsigned *)((const char *)packed + L.scales);
@@ -278,10 +577,10 @@ int obc_product4(obc_ctx *ctx, const void *packed, int R, int d, int group, cons
     a.T = T; a.R = R; a.d = d; a.RB = L.RB; a.KT = L.KT; a.NG = L.NG; a.tpg = L.tpg;
     a.ldx = ldx; a.ldy = ldy;
     switch (x_type) {
-    case OBC_F32: return launch_sub<OBC_F32>(ctx, a, L.SUB, y_type);
-    case OBC_F16: return launch_sub<OBC_F16>(ctx, a, L.SUB, y_type);
-    case OBC_BF16: return launch_sub<OBC_BF16>(ctx, a, L.SUB, y_type);
-    default: return launch_sub<OBC_I8>(ctx, a, L.SUB, y_type);
+    case OBC_F32: return launch_sub<OBC_F32>(ctx, a, L.SUB, y_type, ws);
+    case OBC_F16: return launch_sub<OBC_F16>(ctx, a, L.SUB, y_type, ws);
+    case OBC_BF16: return launch_sub<OBC_BF16>(ctx, a, L.SUB, y_type, ws);
+    default: return launch_sub<OBC_I8>(ctx, a, L.SUB, y_type, ws);
     }
 }
 
