@@ -84,6 +84,9 @@ __device__ inline void split3(float x, float &h, float &m, float &l)
     l = finite ? (float)(__bf16)(r - m) : 0.f;
 }
 
+// (By value: a bit cast of a vector's element in place takes the vector's first.)
+__device__ inline halfx2 half_pair(unsigned w) { return __builtin_bit_cast(halfx2, w); }
+__device__ inline unsigned bits_of(halfx2 v) { return __builtin_bit_cast(unsigned, v); }
 __device__ inline float half_lo(unsigned w) { return (float)__builtin_bit_cast(_Float16, (unsigned short)(w & 0xffffu)); }
 __device__ inline float half_hi(unsigned w) { return (float)__builtin_bit_cast(_Float16, (unsigned short)(w >> 16)); }
 
