@@ -17,7 +17,16 @@ struct Args {
     const float *xs;
     void *y;
     int T, R, d, RB, KT, NG, tpg;
+    unsigned tpg_inv;            // floor(2^32 / tpg) + 1, 0 for tpg = 1
     int64_t ldx, ldy;
+
+    // kt / tpg: exact while kt tpg < 2^32 (a row of 8 million columns)
+    __device__ int group_of(int kt) const { return tpg_inv ? (int)__umulhi((unsigned)kt, tpg_inv) : kt; }
+};
+
+template <int V>
+struct Type {
+    static constexpr int value = V;
 };
 
 // One 16x16x32 operand of token rows: the lane's eight columns from `c` on of row `row`, zeros from d on.
@@ -142,74 +151,175 @@ struct Sum<OBC_I8> {
     __device__ float operator[](int i) const { return (float)s[i]; }
 };
 
-// 16 rows of W and 16 MF tokens to a workgroup whose WAVES waves take turns along the columns' tiles and sum in LDS.
-template <int XT, int SUB, int MF, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void product4_rows_kernel(Args a, int y_type)
+// ---- few tokens ------------------------------------------------------------------------------
+constexpr int kRowsTokens = 16;
+constexpr int kRowsLds = 147456;     // of a compute unit, for its workgroups' tokens
+// waves of a workgroup at most, as registers allow: an fp32 operand is three
+constexpr int rows_waves(int XT) { return XT == OBC_F32 ? 8 : 16; }
+
+// Bytes of a token's tile of 128 columns in LDS
+constexpr int tile_bytes(int XT) { return XT == OBC_F32 ? 768 : XT == OBC_I8 ? 128 : 256; }
+
+// 16 NF rows of W and up to 16 tokens to a workgroup, whose waves take turns along the columns' tiles and sum in LDS.  The
+// weights' bytes bound it: a wave has its next tile's codes on their way (more than one only costs registers and instructions: 16 waves
+// to a compute unit cover the rest).  Loads come back in order, so the tokens must not be among them: they go through LDS, `chunk`
+// tiles at a time.
+template <int XT, int SUB, int NF>
+__global__ __launch_bounds__(rows_waves(XT) * 64) void product4_rows_kernel(Args a, int y_type, int chunk)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int P = XT == OBC_F32 ? 3 : 1, OPS = XT == OBC_I8 ? 8 : 16;      // planes; 16-byte places of a token's tile
+    extern __shared__ uintx4 lds[];
+    // (the wave's number is the same in all its lanes, which the compiler does not see by itself)
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int n = lane & 15, quad = lane >> 4;
-    const int rb = blockIdx.x;
-    const int t0 = blockIdx.y * 16 * MF;
-    int64_t row_at[MF];
+    const int rb0 = blockIdx.x * NF;
+    int64_t rb[NF];
 #pragma unroll
-    for (int m = 0; m < MF; ++m) {
-        const int t = t0 + 16 * m + n;
-        row_at[m] = (int64_t)(t < a.T ? t : a.T - 1) * a.ldx;      // rows beyond the last: their sums are not stored
-    }
-    float acc[MF][4];
+    for (int j = 0; j < NF; ++j) rb[j] = rb0 + j < a.RB ? rb0 + j : a.RB - 1;
+    float acc[NF][4];
 #pragma unroll
-    for (int m = 0; m < MF; ++m)
+    for (int j = 0; j < NF; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[m][i] = 0.f;
+        for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
     constexpr float base = XT == OBC_I8 ? 0.f : kCodeBase;
     const Codes<XT> ones = Codes<XT>::ones();
-    for (int kt = wave; kt < a.KT; kt += WAVES) {
-        const uintx4 w = a.codes[((int64_t)rb * a.KT + kt) * 64 + lane];
-        unsigned sc[SUB];
+    struct Weights {
+        uintx4 w[NF];
+        unsigned sc[NF][SUB];
+    };
+    auto fetch = [&](Weights &g, int kt) {
+        if (kt >= a.KT) kt = a.KT - 1;
 #pragma unroll
-        for (int u = 0; u < SUB; ++u)
-            sc[u] = SUB > 1 ? a.scales[(((int64_t)rb * a.KT + kt) * 16 + n) * SUB + u]
-                            : a.scales[((int64_t)rb * a.NG + kt / a.tpg) * 16 + n];
+        for (int j = 0; j < NF; ++j) {
+            g.w[j] = a.codes[(rb[j] * a.KT + kt) * 64 + lane];
+            if constexpr (SUB == 4) {
+                const uintx4 v = *((const uintx4 *)a.scales + (rb[j] * a.KT + kt) * 16 + n);
 #pragma unroll
-        for (int m = 0; m < MF; ++m) {
-#pragma unroll
-            for (int u = 0; u < SUB; ++u) {
-                Sum<XT> S, s;
-#pragma unroll
-                for (int k = u * 4 / SUB; k < (u + 1) * 4 / SUB; ++k) {
-                    Operand<XT> x;
-                    const int c = kt * 128 + 32 * k + 8 * quad;
-                    x.load(a.x, row_at[m] + c, a.d - c);
-                    S.add(x, Codes<XT>(w[k]));
-                    s.add(x, ones);
-                }
-                const float step = half_lo(sc[u]), off = half_hi(sc[u]) - base * step;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[m][i] = fmaf(step, S[i], fmaf(off, s[i], acc[m][i]));
+                for (int u = 0; u < 4; ++u) g.sc[j][u] = v[u];
+            } else if constexpr (SUB == 2) {
+                const uintx2 v = *((const uintx2 *)a.scales + (rb[j] * a.KT + kt) * 16 + n);
+                g.sc[j][0] = v.x;
+                g.sc[j][1] = v.y;
+            } else {
+                g.sc[j][0] = a.scales[(rb[j] * a.NG + a.group_of(kt)) * 16 + n];
             }
         }
+    };
+    // Operand o (step k, quad) of token t and tile i of the chunk, at place o ^ (t mod 16) of its row; 8-bit inputs: 8 bytes
+    auto place = [&](int i, int p, int t, int o) { return ((i * P + p) * a.T + t) * OPS + (XT == OBC_I8 ? o >> 1 : o ^ (t & 15)); };
+    auto put = [&](const Operand<XT> &x, int i, int t, int o) {
+        if constexpr (XT == OBC_F32) {
+#pragma unroll
+            for (int p = 0; p < 3; ++p) lds[place(i, p, t, o)] = x.v[p];
+        } else if constexpr (XT == OBC_I8) {
+            ((uintx2 *)&lds[place(i, 0, t, o)])[o & 1] = x.v;
+        } else {
+            lds[place(i, 0, t, o)] = x.v;
+        }
+    };
+    auto stage = [&](int kt0, int tiles) {
+        // tiles that are whole: 64 operands of a token to a wave, several loads on their way at a time; the tile that d ends
+        // in: element by element
+        const int full = (a.d >> 7) - kt0 < tiles ? (a.d >> 7) - kt0 : tiles;
+        const int ops = full * 16, blocks = (ops + 63) >> 6;
+        constexpr int N = XT == OBC_F32 ? 2 : 8;
+        int t = 0, b = wave;
+        while (t < a.T && blocks > 0) {
+            Operand<XT> x[N];
+            int ts[N], bs[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                while (b >= blocks && t < a.T) {
+                    b -= blocks;
+                    ++t;
+                }
+                ts[i] = t;
+                bs[i] = b;
+                if (t < a.T) {
+                    int e = b * 64 + lane;
+                    e = e < ops ? e : ops - 1;
+                    x[i].load(a.x, t * a.ldx + kt0 * 128 + 8 * e, 8);
+                }
+                b += waves;
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int e = bs[i] * 64 + lane;
+                if (ts[i] < a.T && e < ops) put(x[i], e >> 4, ts[i], e & 15);
+            }
+        }
+        if (full < tiles)
+            for (int e = threadIdx.x; e < a.T * 16; e += blockDim.x) {
+                const int o = e & 15, c = (kt0 + full) * 128 + 8 * o;
+                Operand<XT> x;
+                x.load(a.x, (e >> 4) * a.ldx + c, a.d - c);
+                put(x, full, e >> 4, o);
+            }
+    };
+    const int t = n < a.T ? n : a.T - 1;      // rows beyond the last token: not stored
+    auto compute = [&](const Weights &g, int i) {
+        Operand<XT> x[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if constexpr (XT == OBC_F32) {
+#pragma unroll
+                for (int p = 0; p < 3; ++p) x[k].v[p] = lds[place(i, p, t, 4 * k + quad)];
+            } else if constexpr (XT == OBC_I8) {
+                x[k].v = ((const uintx2 *)&lds[place(i, 0, t, 4 * k + quad)])[quad & 1];
+            } else {
+                x[k].v = lds[place(i, 0, t, 4 * k + quad)];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+            Sum<XT> s, S[NF];
+#pragma unroll
+            for (int k = u * 4 / SUB; k < (u + 1) * 4 / SUB; ++k) {
+                s.add(x[k], ones);
+#pragma unroll
+                for (int j = 0; j < NF; ++j) S[j].add(x[k], Codes<XT>(g.w[j][k]));
+            }
+#pragma unroll
+            for (int j = 0; j < NF; ++j) {
+                const float step = half_lo(g.sc[j][u]), off = half_hi(g.sc[j][u]) - base * step;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[j][v] = fmaf(step, S[j][v], fmaf(off, s[v], acc[j][v]));
+            }
+        }
+    };
+    Weights next;
+    fetch(next, wave);
+    for (int kt0 = 0; kt0 < a.KT; kt0 += chunk) {      // chunks are multiples of the waves, but for the last
+        const int tiles = kt0 + chunk < a.KT ? chunk : a.KT - kt0;
+        if (kt0) __syncthreads();
+        stage(kt0, tiles);
+        __syncthreads();
+        for (int i = wave; i < tiles; i += waves) {
+            const Weights now = next;
+            fetch(next, kt0 + i + waves);
+            compute(now, i);
+        }
     }
-    __shared__ float part[WAVES][MF][64][4];
-#pragma unroll
-    for (int m = 0; m < MF; ++m)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) part[wave][m][lane][i] = acc[m][i];
     __syncthreads();
-    for (int e = threadIdx.x; e < MF * 256; e += WAVES * 64) {
-        const int m = e >> 8, i = (e >> 6) & 3, l = e & 63;
-        float v = 0.f;
+    float *const part = (float *)lds;      // waves x NF x 4 x 64
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) v += part[w][m][l][i];
-        const int t = t0 + 16 * m + 4 * (l >> 4) + i, r = rb * 16 + (l & 15);
-        if (t >= a.T || r >= a.R) continue;
-        if (XT == OBC_I8) v *= a.xs[t];
-        const int64_t at = (int64_t)t * a.ldy + r;
+    for (int j = 0; j < NF; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) part[((wave * NF + j) * 4 + i) * 64 + lane] = acc[j][i];
+    __syncthreads();
+    for (int e = threadIdx.x; e < NF * 256; e += blockDim.x) {
+        const int l = e & 63, i = (e >> 6) & 3, j = e >> 8;
+        const int to = 4 * (l >> 4) + i, r = (rb0 + j) * 16 + (l & 15);
+        if (to >= a.T || r >= a.R) continue;
+        float v = 0.f;
+        for (int w = 0; w < waves; ++w) v += part[w * (NF * 256) + e];
+        if (XT == OBC_I8) v *= a.xs[to];
+        const int64_t at = (int64_t)to * a.ldy + r;
         if (y_type == OBC_F32) store_as<OBC_F32>(a.y, at, v);
         else if (y_type == OBC_F16) store_as<OBC_F16>(a.y, at, v);
         else store_as<OBC_BF16>(a.y, at, v);
     }
 }
-
 
 // ---- many tokens ------------------------------------------------------------------------------
 // The tokens as product4_tiles_kernel takes them: rows at multiples of 16 bytes, columns up to a multiple of 128, zeros
@@ -243,49 +353,49 @@ __global__ __launch_bounds__(256) void product4_lay_kernel(const void *x, int64_
     }
 }
 
-template <int V>
-struct Type {
-    static constexpr int value = V;
-};
-
 struct Tokens {
     const char *x;           // first plane
     int64_t ld, plane;       // bytes between rows, between planes
+    int mtiles, tiles;       // blocks of BM tokens, of those x 128 rows
+    int per;                 // column tiles of a slice
+    float *part;             // slices x T x R sums, where there are several
 };
 
 typedef __attribute__((address_space(1))) const void *global_ptr;
 typedef __attribute__((address_space(3))) void *lds_ptr;
 
-// BM tokens x 128 rows of W to a workgroup of 2 x 2 waves, BM / 2 x 64 each.  The tokens go through LDS, two tiles
-// in turn; a wave's codes come straight from memory in operand order and are unpacked once for its BM / 2 tokens.
+// BM tokens x 128 rows of W to a workgroup of WM x (4 / WM) waves.  The tokens go through LDS, two tiles in turn; a wave's
+// codes come straight from memory in operand order and are unpacked once for its BM / WM tokens.
 // The inputs' sums of every group are kept in LDS and meet the offsets in one fp32 product of matrices at the end.
 constexpr int kWaitVm0 = 0x0f70;    // s_waitcnt vmcnt(0), the other counters not waited for
 constexpr int kSumGroups = 32;      // groups whose sums LDS holds; more are worked off in between
 
-template <int XT, int SUB, int BM>
-__global__ __launch_bounds__(256, 2) void product4_tiles_kernel(Args a, Tokens tok, int y_type, int mtiles)
+template <int XT, int SUB, int BM, int WM>
+__global__ __launch_bounds__(256, 2) void product4_tiles_kernel(Args a, Tokens tok, int y_type)
 {
-    constexpr int P = XT == OBC_F32 ? 3 : 1, MF = BM / 32;
+    constexpr int P = XT == OBC_F32 ? 3 : 1, WN = 4 / WM, MF = BM / WM / 16, NF = 8 / WN;
     constexpr int ROW = XT == OBC_I8 ? 8 : 16;      // 16-byte pieces of a token's 128 columns
     // two arrays, not one of two: the compiler then knows that reading one does not wait for loads to the other
     __shared__ uintx4 even[P * BM * ROW], odd[P * BM * ROW];
     __shared__ float sums[kSumGroups][BM];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 15, quad = lane >> 4;
-    const int wm = wave & 1, wn = wave >> 1;
+    const int wm = wave % WM, wn = wave / WM;
     // consecutive workgroups go to different dies: give each die a run of tiles
-    const int tiles = gridDim.x, per = tiles >> 3, left = tiles & 7, die = blockIdx.x & 7;
-    const int tile = die * per + (die < left ? die : left) + (blockIdx.x >> 3);
-    const int t0 = (tile % mtiles) * BM, rb0 = (tile / mtiles) * 8 + wn * 4;
+    const int slice = blockIdx.x / tok.tiles, id = blockIdx.x % tok.tiles;
+    const int each = tok.tiles >> 3, left = tok.tiles & 7, die = id & 7;
+    const int tile = die * each + (die < left ? die : left) + (id >> 3);
+    const int t0 = (tile % tok.mtiles) * BM, rb0 = (tile / tok.mtiles) * 8 + wn * NF;
+    const int kt0 = slice * tok.per, kt1 = kt0 + tok.per < a.KT ? kt0 + tok.per : a.KT;
     constexpr float base = XT == OBC_I8 ? 0.f : kCodeBase;
-    floatx4 acc[MF][4];
+    floatx4 acc[MF][NF];
 #pragma unroll
     for (int m = 0; m < MF; ++m)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[m][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    int64_t rb[4];
+        for (int j = 0; j < NF; ++j) acc[m][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    int64_t rb[NF];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) rb[j] = rb0 + j < a.RB ? rb0 + j : a.RB - 1;      // beyond the last: not stored
+    for (int j = 0; j < NF; ++j) rb[j] = rb0 + j < a.RB ? rb0 + j : a.RB - 1;      // beyond the last: not stored
     // Piece o of token t lies at place o ^ (t mod ROW) of its row, so that the 16 tokens of an operand lie in different
     // banks.  The lanes of a load to LDS write 64 places in a row: each fetches the piece that belongs to its place.
     auto fetch = [&](int kt, uintx4 *lds) {
@@ -311,52 +421,52 @@ __global__ __launch_bounds__(256, 2) void product4_tiles_kernel(Args a, Tokens t
     auto offsets = [&](int g0, int count) {
         for (int g = 0; g < count; g += 4) {
             const bool in = g + quad < count;
-            float b[4];
+            float b[NF];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < NF; ++j) {
                 unsigned sc = 0;
                 if (in) {
                     const int at = g0 + g + quad;
                     sc = SUB > 1 ? a.scales[((rb[j] * a.KT + at / SUB) * 16 + n) * SUB + at % SUB]
-                                 : a.scales[(rb[j] * a.NG + at / a.tpg) * 16 + n];
+                                 : a.scales[(rb[j] * a.NG + a.group_of(at)) * 16 + n];
                 }
                 b[j] = half_hi(sc) - base * half_lo(sc);
             }
 #pragma unroll
             for (int m = 0; m < MF; ++m) {
-                const float s = in ? sums[g + quad][wm * (BM / 2) + 16 * m + n] : 0.f;
+                const float s = in ? sums[g + quad][wm * (BM / WM) + 16 * m + n] : 0.f;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[m][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(s, b[j], acc[m][j], 0, 0, 0);
+                for (int j = 0; j < NF; ++j) acc[m][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(s, b[j], acc[m][j], 0, 0, 0);
             }
         }
     };
-    uintx4 codes[4];
-    unsigned scale[4][SUB];
+    uintx4 codes[NF];
+    unsigned scale[NF][SUB];
     auto fetch_codes = [&](int kt) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < NF; ++j) {
             codes[j] = a.codes[(rb[j] * a.KT + kt) * 64 + lane];
 #pragma unroll
             for (int u = 0; u < SUB; ++u)
-                scale[j][u] = SUB > 1 ? a.scales[((rb[j] * a.KT + kt) * 16 + n) * SUB + u] : a.scales[(rb[j] * a.NG + kt / a.tpg) * 16 + n];
+                scale[j][u] = SUB > 1 ? a.scales[((rb[j] * a.KT + kt) * 16 + n) * SUB + u] : a.scales[(rb[j] * a.NG + a.group_of(kt)) * 16 + n];
         }
     };
-    fetch(0, even);
-    fetch_codes(0);
+    fetch(kt0, even);
+    fetch_codes(kt0);
     __builtin_amdgcn_s_waitcnt(kWaitVm0);
     __syncthreads();
-    int done = 0;      // tiles whose offsets are in
+    int done = kt0;      // tiles whose offsets are in
     auto turn = [&](const int kt, const uintx4 *lds, uintx4 *lds_next) __attribute__((always_inline)) {
-        uintx4 w[4];
-        float step[4][SUB];
+        uintx4 w[NF];
+        float step[NF][SUB];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < NF; ++j) {
             w[j] = codes[j];
 #pragma unroll
             for (int u = 0; u < SUB; ++u) step[j][u] = half_lo(scale[j][u]);
         }
         // (the last tile again after the last: a branch here would make the compiler wait for all of it at once)
-        const int ahead = kt + 1 < a.KT ? kt + 1 : kt;
+        const int ahead = kt + 1 < kt1 ? kt + 1 : kt;
         fetch(ahead, lds_next);
         fetch_codes(ahead);
         // the tile's sums, a quarter of the tokens to each wave
@@ -382,9 +492,9 @@ __global__ __launch_bounds__(256, 2) void product4_tiles_kernel(Args a, Tokens t
                     for (int i = 0; i < 4; ++i) sums[(kt - done) * SUB + u][16 * m + 4 * quad + i] = s[i];
             }
         }
-        uintx4 B[4][XT == OBC_I8 ? 2 : 4];
+        uintx4 B[NF][XT == OBC_I8 ? 2 : 4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < NF; ++j)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 if constexpr (XT == OBC_I8) {
@@ -408,9 +518,9 @@ __global__ __launch_bounds__(256, 2) void product4_tiles_kernel(Args a, Tokens t
                 }
 #pragma unroll
                 for (int u = 0; u < SUB; ++u) {
-                    intx4 S[4];
+                    intx4 S[NF];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
+                    for (int j = 0; j < NF; ++j) {
                         S[j] = intx4{0, 0, 0, 0};
                         if constexpr (SUB == 4) {
                             const uintx4 x = A[u >> 1], b = B[j][u >> 1];
@@ -422,27 +532,27 @@ __global__ __launch_bounds__(256, 2) void product4_tiles_kernel(Args a, Tokens t
                         }
                     }
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
+                    for (int j = 0; j < NF; ++j)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) acc[m][j][i] = fmaf(step[j][u], (float)S[j][i], acc[m][j][i]);
                 }
             } else {
 #pragma unroll
                 for (int u = 0; u < SUB; ++u) {
-                    floatx4 S[4];
+                    floatx4 S[NF];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) S[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+                    for (int j = 0; j < NF; ++j) S[j] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int k = u * 4 / SUB; k < (u + 1) * 4 / SUB; ++k) {
 #pragma unroll
                         for (int p = P - 1; p >= 0; --p) {
                             const uintx4 A = operand(lds, p, mm, 4 * k + quad);
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) S[j] = XT == OBC_F16 ? mfma_f16(A, B[j][k], S[j]) : mfma_bf16(A, B[j][k], S[j]);
+                            for (int j = 0; j < NF; ++j) S[j] = XT == OBC_F16 ? mfma_f16(A, B[j][k], S[j]) : mfma_bf16(A, B[j][k], S[j]);
                         }
                     }
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
+                    for (int j = 0; j < NF; ++j)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) acc[m][j][i] = fmaf(step[j][u], S[j][i], acc[m][j][i]);
                 }
@@ -450,17 +560,17 @@ __global__ __launch_bounds__(256, 2) void product4_tiles_kernel(Args a, Tokens t
         }
         __builtin_amdgcn_s_waitcnt(kWaitVm0);      // the next tile is in LDS
         __syncthreads();
-        if ((kt + 1 - done + 1) * SUB > kSumGroups || kt + 1 == a.KT) {
+        if ((kt + 1 - done + 1) * SUB > kSumGroups || kt + 1 == kt1) {
             offsets(done * SUB, (kt + 1 - done) * SUB);
             done = kt + 1;
             __syncthreads();
         }
     };
-    for (int kt = 0;; kt += 2) {
+    for (int kt = kt0;; kt += 2) {
         turn(kt, even, odd);
-        if (kt + 1 >= a.KT) break;
+        if (kt + 1 >= kt1) break;
         turn(kt + 1, odd, even);
-        if (kt + 2 >= a.KT) break;
+        if (kt + 2 >= kt1) break;
     }
     auto put = [&](auto type) {
         constexpr int YT = decltype(type)::value;
@@ -468,13 +578,17 @@ __global__ __launch_bounds__(256, 2) void product4_tiles_kernel(Args a, Tokens t
         for (int m = 0; m < MF; ++m)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int t = t0 + wm * (BM / 2) + 16 * m + 4 * quad + i;
+                const int t = t0 + wm * (BM / WM) + 16 * m + 4 * quad + i;
                 if (t >= a.T) continue;
-                const float xs = XT == OBC_I8 ? a.xs[t] : 1.f;
+                const bool sliced = tok.part != nullptr;
+                const float xs = XT == OBC_I8 && !sliced ? a.xs[t] : 1.f;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
+                for (int j = 0; j < NF; ++j) {
                     const int r = (rb0 + j) * 16 + n;
-                    if (r < a.R) store_as<YT>(a.y, (int64_t)t * a.ldy + r, XT == OBC_I8 ? acc[m][j][i] * xs : acc[m][j][i]);
+                    const float v = XT == OBC_I8 ? acc[m][j][i] * xs : acc[m][j][i];
+                    if (r >= a.R) continue;
+                    if (sliced) tok.part[((int64_t)slice * a.T + t) * a.R + r] = v;
+                    else store_as<YT>(a.y, (int64_t)t * a.ldy + r, v);
                 }
             }
     };
@@ -483,57 +597,104 @@ __global__ __launch_bounds__(256, 2) void product4_tiles_kernel(Args a, Tokens t
     else put(Type<OBC_BF16>());
 }
 
+// The slices' sums, in their order.
+__global__ __launch_bounds__(256) void product4_add_kernel(Args a, const float *__restrict__ part, int slices, int y_type)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, n = (int64_t)a.T * a.R;
+    if (i >= n) return;
+    float v = part[i];
+    for (int s = 1; s < slices; ++s) v += part[s * n + i];
+    const int64_t t = i / a.R;
+    if (a.xs) v *= a.xs[t];
+    const int64_t at = t * a.ldy + (i - t * a.R);
+    if (y_type == OBC_F32) store_as<OBC_F32>(a.y, at, v);
+    else if (y_type == OBC_F16) store_as<OBC_F16>(a.y, at, v);
+    else store_as<OBC_BF16>(a.y, at, v);
+}
+
 // True where the tiles' kernel can read x as it lies.
 inline bool laid_out(const void *x, int x_type, int64_t ldx, int d)
 {
     return x_type != OBC_F32 && d % 128 == 0 && ((uintptr_t)x & 15) == 0 && (ldx * (int64_t)size_of_type(x_type)) % 16 == 0;
 }
 
-inline size_t laid_bytes(int T, int KT, int x_type)
+// What a product with more tokens than the rows' kernel takes is cut into, and its workspace.
+struct Plan {
+    int BM, mtiles, ntiles, slices, per;
+    size_t laid, part, bytes;      // tokens laid out (where x is not like that already), the slices' sums
+};
+
+Plan plan_of(const pack4_layout &L, int T, int x_type)
 {
-    return (size_t)T * KT * 128 * (x_type == OBC_F32 ? 6 : x_type == OBC_I8 ? 1 : 2);
+    Plan p;
+    p.BM = T <= 32 ? 32 : T <= 64 || x_type == OBC_F32 ? 64 : 128;
+    p.mtiles = T / p.BM + (T % p.BM != 0);
+    p.ntiles = (L.RB + 7) / 8;
+    // two workgroups to a compute unit, two tiles at least to a slice
+    const int64_t tiles = (int64_t)p.mtiles * p.ntiles;
+    int64_t s = tiles > 0 ? 512 / tiles : 1;
+    if (s > 16) s = 16;
+    if (s > L.KT / 2) s = L.KT / 2;
+    if (s < 1) s = 1;
+    p.per = (int)((L.KT + s - 1) / s);
+    p.slices = (L.KT + p.per - 1) / p.per;
+    p.laid = obc_align_up((size_t)T * L.KT * 128 * (x_type == OBC_F32 ? 6 : x_type == OBC_I8 ? 1 : 2), 256);
+    p.part = p.slices > 1 ? (size_t)p.slices * T * L.R * 4 : 0;
+    p.bytes = p.laid + p.part;
+    return p;
+}
+
+template <int XT, int SUB, int NF>
+void launch_rows(obc_ctx *ctx, const Args &a, int y_type, int waves, int chunk)
+{
+    const size_t tokens = (size_t)chunk * a.T * tile_bytes(XT), sums = (size_t)waves * NF * 1024;
+    product4_rows_kernel<XT, SUB, NF><<<(a.RB + NF - 1) / NF, waves * 64, tokens > sums ? tokens : sums, ctx->stream>>>(a, y_type, chunk);
 }
 
 template <int XT, int SUB>
-int launch(obc_ctx *ctx, const Args &a, int y_type, void *ws)
+int launch(obc_ctx *ctx, const Args &a, int y_type, const Plan &p, void *ws)
 {
-    if (a.T <= 16) {
-        product4_rows_kernel<XT, SUB, 1, 8><<<dim3(a.RB, 1), 512, 0, ctx->stream>>>(a, y_type);
-    } else if (a.T > 64) {
-        constexpr int BM = XT == OBC_F32 ? 64 : 128;
-        const int mtiles = a.T / BM + (a.T % BM != 0), ntiles = (a.RB + 7) / 8;
-        if ((int64_t)mtiles * ntiles > 0x7fffffff) return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_product4: too many tiles");
-        Tokens tok = {(const char *)a.x, a.ldx * (int64_t)size_of_type(XT), 0};
-        if (!laid_out(a.x, XT, a.ldx, a.d)) {
-            const int pieces = a.KT * (XT == OBC_I8 ? 8 : 16);
-            const int64_t jobs = (int64_t)a.T * pieces;
-            if ((jobs + 255) / 256 > 0x7fffffff) return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_product4: too many inputs");
-            product4_lay_kernel<XT><<<(unsigned)((jobs + 255) / 256), 256, 0, ctx->stream>>>(a.x, a.ldx, a.d, pieces, jobs, jobs, (uintx4 *)ws);
-            OBC_LAUNCH_CHECK(ctx, "product4_lay_kernel");
-            tok = Tokens{(const char *)ws, (int64_t)pieces * 16, jobs * 16};
-        }
-        product4_tiles_kernel<XT, SUB, BM><<<mtiles * ntiles, 256, 0, ctx->stream>>>(a, tok, y_type, mtiles);
-    } else {
-        const int per = 64, blocks = (a.T + per - 1) / per;
-        for (int b0 = 0; b0 < blocks; b0 += 65535) {
-            Args c = a;
-            const int64_t t0 = (int64_t)b0 * per;
-            c.x = (const char *)a.x + t0 * a.ldx * (int64_t)size_of_type(XT);
-            c.y = (char *)a.y + t0 * a.ldy * (int64_t)size_of_type(y_type);
-            if (a.xs) c.xs = a.xs + t0;
-            c.T = a.T - (int)t0;
-            const int nb = blocks - b0 < 65535 ? blocks - b0 : 65535;
-            product4_rows_kernel<XT, SUB, 4, 4><<<dim3(a.RB, nb), 256, 0, ctx->stream>>>(c, y_type);
-        }
+    if (a.T <= kRowsTokens) {
+        // sixteen waves to a compute unit, in one workgroup or two; no more than there are tiles
+        const int NF = a.RB > 256 ? 2 : 1, blocks = (a.RB + NF - 1) / NF;
+        int waves = blocks > 256 || XT == OBC_F32 ? 8 : 16;
+        const int room = kRowsLds / (blocks > 256 ? 2 : 1) / (a.T * tile_bytes(XT));
+        while (waves > 1 && (waves / 2 >= a.KT || (room < a.KT && room < waves))) waves /= 2;
+        const int chunk = room >= a.KT ? a.KT : room / waves * waves;
+        if (NF == 2) launch_rows<XT, SUB, 2>(ctx, a, y_type, waves, chunk);
+        else launch_rows<XT, SUB, 1>(ctx, a, y_type, waves, chunk);
+        OBC_LAUNCH_CHECK(ctx, "product4_rows_kernel");
+        return OBC_OK;
     }
-    OBC_LAUNCH_CHECK(ctx, "product4_rows_kernel");
+    const int64_t blocks = (int64_t)p.mtiles * p.ntiles * p.slices, adds = ((int64_t)a.T * a.R + 255) / 256;
+    if (blocks > 0x7fffffff || (p.slices > 1 && adds > 0x7fffffff)) return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_product4: too many tiles");
+    Tokens tok = {(const char *)a.x, a.ldx * (int64_t)size_of_type(XT), 0, p.mtiles, p.mtiles * p.ntiles, p.per,
+                  p.slices > 1 ? (float *)((char *)ws + p.laid) : nullptr};
+    if (!laid_out(a.x, XT, a.ldx, a.d)) {
+        const int pieces = a.KT * (XT == OBC_I8 ? 8 : 16);
+        const int64_t jobs = (int64_t)a.T * pieces;
+        if ((jobs + 255) / 256 > 0x7fffffff) return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_product4: too many inputs");
+        product4_lay_kernel<XT><<<(unsigned)((jobs + 255) / 256), 256, 0, ctx->stream>>>(a.x, a.ldx, a.d, pieces, jobs, jobs, (uintx4 *)ws);
+        OBC_LAUNCH_CHECK(ctx, "product4_lay_kernel");
+        tok.x = (const char *)ws;
+        tok.ld = (int64_t)pieces * 16;
+        tok.plane = jobs * 16;
+    }
+    if (p.BM == 32) product4_tiles_kernel<XT, SUB, 32, 1><<<(unsigned)blocks, 256, 0, ctx->stream>>>(a, tok, y_type);
+    else if (p.BM == 64 && XT != OBC_F32) product4_tiles_kernel<XT, SUB, 64, 1><<<(unsigned)blocks, 256, 0, ctx->stream>>>(a, tok, y_type);
+    else product4_tiles_kernel<XT, SUB, XT == OBC_F32 ? 64 : 128, 2><<<(unsigned)blocks, 256, 0, ctx->stream>>>(a, tok, y_type);
+    OBC_LAUNCH_CHECK(ctx, "product4_tiles_kernel");
+    if (p.slices > 1) {
+        product4_add_kernel<<<(unsigned)adds, 256, 0, ctx->stream>>>(a, tok.part, p.slices, y_type);
+        OBC_LAUNCH_CHECK(ctx, "product4_add_kernel");
+    }
     return OBC_OK;
 }
 
 template <int XT>
-int launch_sub(obc_ctx *ctx, const Args &a, int sub, int y_type, void *ws)
+int launch_sub(obc_ctx *ctx, const Args &a, int sub, int y_type, const Plan &p, void *ws)
 {
-    return sub == 1 ? launch<XT, 1>(ctx, a, y_type, ws) : sub == 2 ? launch<XT, 2>(ctx, a, y_type, ws) : launch<XT, 4>(ctx, a, y_type, ws);
+    return sub == 1 ? launch<XT, 1>(ctx, a, y_type, p, ws) : sub == 2 ? launch<XT, 2>(ctx, a, y_type, p, ws) : launch<XT, 4>(ctx, a, y_type, p, ws);
 }
 
 }  // namespace
@@ -545,8 +706,7 @@ int obc_product4_workspace_bytes(int T, int R, int d, int group, int x_type, siz
     pack4_layout L;
     if (!bytes || T < 0 || R < 0 || d <= 0 || !(float_type(x_type) || x_type == OBC_I8) || !pack4_layout_of(R, d, group, &L))
         return OBC_ERR_BAD_ARG;
-    // rows that are not laid out for the tiles' kernel; a workspace for T tokens serves fewer
-    *bytes = T > 64 ? laid_bytes(T, L.KT, x_type) : 0;
+    *bytes = T > kRowsTokens && R > 0 ? plan_of(L, T, x_type).bytes : 0;
     return OBC_OK;
 }
 
@@ -568,19 +728,24 @@ int obc_product4(obc_ctx *ctx, const void *packed, int R, int d, int group, cons
     if (((uintptr_t)packed & 15) != 0) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_product4: packed is not aligned to 16 bytes");
     if (((uintptr_t)x & (size_of_type(x_type) - 1)) != 0 || ((uintptr_t)y & (size_of_type(y_type) - 1)) != 0)
         return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_product4: x or y is not aligned to its elements");
-    if (T > 64 && !laid_out(x, x_type, ldx, d) && (!ws || ((uintptr_t)ws & 15) != 0 || ws_bytes < laid_bytes(T, L.KT, x_type)))
-        return obc_fail(ctx, OBC_ERR_WORKSPACE, "obc_product4: workspace of %zu bytes needed", laid_bytes(T, L.KT, x_type));
+    const Plan p = plan_of(L, T, x_type);
+    if (T > kRowsTokens) {
+        const size_t need = p.slices > 1 || !laid_out(x, x_type, ldx, d) ? p.bytes : 0;
+        if (need > 0 && (!ws || ((uintptr_t)ws & 15) != 0 || ws_bytes < need))
+            return obc_fail(ctx, OBC_ERR_WORKSPACE, "obc_product4: workspace of %zu bytes needed", need);
+    }
     Args a;
     a.codes = (const uintx4 *)packed;
     a.scales = (const unsigned *)((const char *)packed + L.scales);
     a.x = x; a.xs = x_scale; a.y = y;
     a.T = T; a.R = R; a.d = d; a.RB = L.RB; a.KT = L.KT; a.NG = L.NG; a.tpg = L.tpg;
+    a.tpg_inv = L.tpg > 1 ? (unsigned)(0x100000000ull / (unsigned)L.tpg) + 1u : 0u;
     a.ldx = ldx; a.ldy = ldy;
     switch (x_type) {
-    case OBC_F32: return launch_sub<OBC_F32>(ctx, a, L.SUB, y_type, ws);
-    case OBC_F16: return launch_sub<OBC_F16>(ctx, a, L.SUB, y_type, ws);
-    case OBC_BF16: return launch_sub<OBC_BF16>(ctx, a, L.SUB, y_type, ws);
-    default: return launch_sub<OBC_I8>(ctx, a, L.SUB, y_type, ws);
+    case OBC_F32: return launch_sub<OBC_F32>(ctx, a, L.SUB, y_type, p, ws);
+    case OBC_F16: return launch_sub<OBC_F16>(ctx, a, L.SUB, y_type, p, ws);
+    case OBC_BF16: return launch_sub<OBC_BF16>(ctx, a, L.SUB, y_type, p, ws);
+    default: return launch_sub<OBC_I8>(ctx, a, L.SUB, y_type, p, ws);
     }
 }
 
