@@ -322,41 +322,75 @@ __global__ __launch_bounds__(rows_waves(XT) * 64) void product4_rows_kernel(Args
 }
 
 // ---- many tokens ------------------------------------------------------------------------------
-// The tokens as product4_tiles_kernel takes them: rows at multiples of 16 bytes, columns up to a multiple of 128, zeros
-// from d on; fp32 as three planes of bf16 terms.  Only where x is not like that already.
-template <int XT>
-__global__ __launch_bounds__(256) void product4_lay_kernel(const void *x, int64_t ldx, int d, int pieces, int64_t jobs, int64_t plane,
-                                                           uintx4 *out)
+// What the tiles' kernel needs beside x: the sums of every token's groups, as three planes of bf16 terms (T x NGP each, zeros
+// from NG on); and, where x is not laid out like that already, the tokens' rows at multiples of 16 bytes with zeros up to a multiple
+// of 128 columns -- fp32 as three planes of bf16 terms.  A team of TEAM lanes to a token and group.
+struct Lay {
+    unsigned short *sums;
+    uintx4 *rows;      // null: x as it lies
+    int NGP, G;        // groups of a row, padded to 32; columns of a group
+    int64_t jobs;      // T x NG
+};
+
+template <int XT, int TEAM>
+__global__ __launch_bounds__(256) void product4_lay_kernel(Args a, Lay lay)
 {
-    constexpr int E = XT == OBC_I8 ? 16 : 8;
-    const int64_t job = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (job >= jobs) return;
-    const int64_t t = job / pieces;
-    const int c = (int)(job - t * pieces) * E;
-    const int64_t at = t * ldx + c;
-    if constexpr (XT == OBC_I8) {
-        uintx4 v = {0u, 0u, 0u, 0u};
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-            if (c + j < d) v[j >> 2] |= (unsigned)((const uint8_t *)x)[at + j] << (8 * (j & 3));
-        out[job] = v;
-    } else {
+    const int64_t job = ((int64_t)blockIdx.x * 256 + threadIdx.x) / TEAM;
+    const int lane = threadIdx.x % TEAM;
+    if (job >= lay.jobs) return;
+    const int64_t t = job / a.NG;
+    const int g = (int)(job - t * a.NG);
+    const int pieces = a.KT * 16, first = g * (lay.G / 8), end = g == a.NG - 1 ? pieces : first + lay.G / 8;
+    const int64_t plane = (int64_t)a.T * pieces;
+    float sum = 0.f;
+    for (int p = first + lane; p < end; p += TEAM) {
+        const int c = p * 8;
         Operand<XT> o;
-        o.load(x, at, d - c);
+        o.load(a.x, t * a.ldx + c, a.d - c);
         if constexpr (XT == OBC_F32) {
-            out[job] = o.v[0];
-            out[job + plane] = o.v[1];
-            out[job + 2 * plane] = o.v[2];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                sum += (bf16_lo(o.v[0][j]) + bf16_lo(o.v[1][j]) + bf16_lo(o.v[2][j])) + (bf16_hi(o.v[0][j]) + bf16_hi(o.v[1][j]) + bf16_hi(o.v[2][j]));
+            }
+            if (lay.rows)
+#pragma unroll
+                for (int q = 0; q < 3; ++q) lay.rows[q * plane + t * pieces + p] = o.v[q];
+        } else if constexpr (XT == OBC_I8) {
+            const uintx2 x = natural_bytes(o.v);
+            int s = __builtin_amdgcn_sdot4((int)x.x, 0x01010101, 0, false);
+            s = __builtin_amdgcn_sdot4((int)x.y, 0x01010101, s, false);
+            sum += (float)s;
+            if (lay.rows) ((uintx2 *)lay.rows)[t * pieces + p] = x;
         } else {
-            out[job] = o.v;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const unsigned w = o.v[j];
+                sum += XT == OBC_F16 ? half_lo(w) + half_hi(w) : bf16_lo(w) + bf16_hi(w);
+            }
+            if (lay.rows) lay.rows[t * pieces + p] = o.v;
         }
     }
+#pragma unroll
+    for (int off = TEAM / 2; off > 0; off >>= 1) sum += __shfl_xor(sum, off, TEAM);
+    float term[3];
+    split3(sum, term[0], term[1], term[2]);
+    unsigned short *const at = lay.sums + t * lay.NGP;
+    const int64_t splane = (int64_t)a.T * lay.NGP;
+    if (lane == 0)
+#pragma unroll
+        for (int q = 0; q < 3; ++q) at[q * splane + g] = (unsigned short)pair_bf16(term[q], 0.f);
+    if (g == a.NG - 1)
+        for (int z = a.NG + lane; z < lay.NGP; z += TEAM)
+#pragma unroll
+            for (int q = 0; q < 3; ++q) at[q * splane + z] = 0;
 }
 
 struct Tokens {
     const char *x;           // first plane
     int64_t ld, plane;       // bytes between rows, between planes
-    int mtiles, tiles;       // blocks of BM tokens, of those x 128 rows
+    const unsigned short *sums;
+    int NGP;
+    int mtiles, tiles;       // blocks of BM tokens, of those x BN rows
     int per;                 // column tiles of a slice
     float *part;             // slices x T x R sums, where there are several
 };
@@ -364,20 +398,45 @@ struct Tokens {
 typedef __attribute__((address_space(1))) const void *global_ptr;
 typedef __attribute__((address_space(3))) void *lds_ptr;
 
-// BM tokens x 128 rows of W to a workgroup of WM x (4 / WM) waves.  The tokens go through LDS, two tiles in turn; a wave's
-// codes come straight from memory in operand order and are unpacked once for its BM / WM tokens.
-// The inputs' sums of every group are kept in LDS and meet the offsets in one fp32 product of matrices at the end.
-constexpr int kWaitVm0 = 0x0f70;    // s_waitcnt vmcnt(0), the other counters not waited for
-constexpr int kSumGroups = 32;      // groups whose sums LDS holds; more are worked off in between
+// s_waitcnt vmcnt(n) lgkmcnt(0): all loads but the n newest, and every access to LDS
+constexpr int wait_loads(int n) { return 0x0070 | (n & 15) | (n >> 4) << 14; }
 
-template <int XT, int SUB, int BM, int WM>
-__global__ __launch_bounds__(256, 2) void product4_tiles_kernel(Args a, Tokens tok, int y_type)
+// A barrier that waits for nothing itself: __syncthreads (and a fence) would wait for every load on its way, the newest stages'
+// among them.  wait_loads goes before it: what a wave has read from LDS has then arrived, and its share of the next stage is there.
+__device__ inline void stage_barrier()
 {
-    constexpr int P = XT == OBC_F32 ? 3 : 1, WN = 4 / WM, MF = BM / WM / 16, NF = 8 / WN;
-    constexpr int ROW = XT == OBC_I8 ? 8 : 16;      // 16-byte pieces of a token's 128 columns
-    // two arrays, not one of two: the compiler then knows that reading one does not wait for loads to the other
-    __shared__ uintx4 even[P * BM * ROW], odd[P * BM * ROW];
-    __shared__ float sums[kSumGroups][BM];
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// BM tokens x BN rows of W to a workgroup of WM x WN waves.  Tokens, codes and steps of STAGES column tiles go through LDS in
+// turn, so that loads have STAGES - 1 tiles' time to arrive; a wave waits for all but its newest ones and then for the others.
+// Within a tile the codes are unpacked step by step between the matrix instructions of the step before.
+constexpr int tile_waves(int BN) { return BN / 32; }
+
+template <int XT, int SUB, int BM, int BN, int WM, int STAGES>
+struct Tile {
+    static constexpr int WAVES = tile_waves(BN);
+    static constexpr int WN = WAVES / WM;
+    static constexpr int P = XT == OBC_F32 ? 3 : 1, MF = BM / WM / 16, NF = BN / WN / 16;
+    static constexpr int ROW = XT == OBC_I8 ? 8 : 16;      // 16-byte pieces of a token's 128 columns
+    static constexpr int XN = P * BM * ROW, WN16 = BN * 4, SN = BN * SUB / 4;      // 16-byte places of a stage: tokens, codes, steps
+    static constexpr int PLACES = XN + WN16 + SN;
+    // loads of a wave for a stage: 64 places each, the steps 4 bytes a lane
+    static constexpr int XL = XN / 64 / WAVES, WL = WN16 / 64 / WAVES, SL = BN * SUB / 64 / WAVES > 0 ? BN * SUB / 64 / WAVES : 1;
+    static constexpr int SLANES = BN * SUB / WAVES < 64 ? BN * SUB / WAVES : 64;
+    static constexpr int LOADS = XL + WL + SL;
+    static_assert(XN % (64 * WAVES) == 0 && WN16 % (64 * WAVES) == 0, "whole loads");
+};
+
+template <int XT, int SUB, int BM, int BN, int WM, int STAGES>
+__global__ __launch_bounds__(tile_waves(BN) * 64, 2) void product4_tiles_kernel(Args a, Tokens tok, int y_type)
+{
+    using C = Tile<XT, SUB, BM, BN, WM, STAGES>;
+    constexpr int P = C::P, MF = C::MF, NF = C::NF, ROW = C::ROW, WN = C::WN;
+    // separate arrays: the compiler then knows that reading one does not wait for loads to another
+    __shared__ uintx4 lds0[C::PLACES], lds1[C::PLACES], lds2[STAGES > 2 ? C::PLACES : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 15, quad = lane >> 4;
     const int wm = wave % WM, wn = wave / WM;
@@ -385,206 +444,216 @@ __global__ __launch_bounds__(256, 2) void product4_tiles_kernel(Args a, Tokens t
     const int slice = blockIdx.x / tok.tiles, id = blockIdx.x % tok.tiles;
     const int each = tok.tiles >> 3, left = tok.tiles & 7, die = id & 7;
     const int tile = die * each + (die < left ? die : left) + (id >> 3);
-    const int t0 = (tile % tok.mtiles) * BM, rb0 = (tile / tok.mtiles) * 8 + wn * NF;
+    const int t0 = (tile % tok.mtiles) * BM, rb0 = (tile / tok.mtiles) * (BN / 16);
     const int kt0 = slice * tok.per, kt1 = kt0 + tok.per < a.KT ? kt0 + tok.per : a.KT;
     constexpr float base = XT == OBC_I8 ? 0.f : kCodeBase;
+    auto row_block = [&](int j) { return (int64_t)(rb0 + j < a.RB ? rb0 + j : a.RB - 1); };      // beyond the last: not stored
+
+    // where this lane's loads come from, at the slice's first tile
+    const char *xsrc[C::XL], *wsrc[C::WL], *ssrc[C::SL];
+    // Piece o of token t lies at place o ^ (t mod ROW) of its row, so that the 16 tokens of an operand lie in different
+    // banks.  The lanes of a load to LDS write 64 places in a row: each fetches the piece that belongs to its place.
+#pragma unroll
+    for (int i = 0; i < C::XL; ++i) {
+        const int first = (i * C::WAVES + wave) * (64 / ROW);      // row of the planes, one below the other
+        const int p = P > 1 ? first / BM : 0, t = first - p * BM + lane / ROW;
+        const int row = t0 + t < a.T ? t0 + t : a.T - 1;
+        xsrc[i] = tok.x + p * tok.plane + row * tok.ld + (int64_t)kt0 * (ROW * 16) + ((lane % ROW) ^ (t % ROW)) * 16;
+    }
+#pragma unroll
+    for (int i = 0; i < C::WL; ++i) wsrc[i] = (const char *)a.codes + (row_block(i * C::WAVES + wave) * a.KT + kt0) * 1024 + lane * 16;
+    // steps: row r of the tile, group u of its SUB at (r SUB + u) * 4
+    int64_t srow[C::SL];
+#pragma unroll
+    for (int i = 0; i < C::SL; ++i) {
+        const int e = (i * C::WAVES + wave) * C::SLANES + lane, r = (e / SUB) % BN;
+        srow[i] = SUB > 1 ? ((row_block(r >> 4) * a.KT) * 16 + (r & 15)) * SUB + e % SUB : row_block(r >> 4) * a.NG * 16 + (r & 15);
+        ssrc[i] = (const char *)a.scales + srow[i] * 4;
+    }
+    auto fetch = [&](int kt, uintx4 *lds) __attribute__((always_inline)) {
+        const int k = (kt < kt1 ? kt : kt1 - 1) - kt0;      // (behind the last: its tile again, for the count of loads)
+#pragma unroll
+        for (int i = 0; i < C::XL; ++i)
+            __builtin_amdgcn_global_load_lds((global_ptr)(xsrc[i] + (int64_t)k * (ROW * 16)), (lds_ptr)(lds + (i * C::WAVES + wave) * 64), 16, 0, 0);
+#pragma unroll
+        for (int i = 0; i < C::WL; ++i)
+            __builtin_amdgcn_global_load_lds((global_ptr)(wsrc[i] + (int64_t)k * 1024), (lds_ptr)(lds + C::XN + (i * C::WAVES + wave) * 64), 16, 0, 0);
+        const int64_t s = SUB > 1 ? (int64_t)(k + kt0) * 64 * SUB : (int64_t)a.group_of(k + kt0) * 64;
+        if (C::SLANES == 64 || lane < C::SLANES)
+#pragma unroll
+            for (int i = 0; i < C::SL; ++i)
+                __builtin_amdgcn_global_load_lds((global_ptr)(ssrc[i] + s), (lds_ptr)((unsigned *)(lds + C::XN + C::WN16) + (i * C::WAVES + wave) * C::SLANES), 4, 0, 0);
+    };
+    fetch(kt0, lds0);
+    if (STAGES > 2) fetch(kt0 + 1, lds1);
+
     floatx4 acc[MF][NF];
 #pragma unroll
     for (int m = 0; m < MF; ++m)
 #pragma unroll
         for (int j = 0; j < NF; ++j) acc[m][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    int64_t rb[NF];
-#pragma unroll
-    for (int j = 0; j < NF; ++j) rb[j] = rb0 + j < a.RB ? rb0 + j : a.RB - 1;      // beyond the last: not stored
-    // Piece o of token t lies at place o ^ (t mod ROW) of its row, so that the 16 tokens of an operand lie in different
-    // banks.  The lanes of a load to LDS write 64 places in a row: each fetches the piece that belongs to its place.
-    auto fetch = [&](int kt, uintx4 *lds) {
-        constexpr int TOK = 64 / ROW;      // tokens of one load
-#pragma unroll
-        for (int i = 0; i < P * BM / TOK / 4; ++i) {
-            const int first = (i * 4 + wave) * TOK;                  // row of the planes, one below the other
-            const int p = P > 1 ? first / BM : 0, t = first - p * BM + lane / ROW;
-            const int row = t0 + t < a.T ? t0 + t : a.T - 1;
-            const char *src = tok.x + p * tok.plane + row * tok.ld + (int64_t)kt * (ROW * 16) + ((lane % ROW) ^ (t % ROW)) * 16;
-            __builtin_amdgcn_global_load_lds((global_ptr)src, (lds_ptr)(lds + first * ROW), 16, 0, 0);
-        }
-    };
-    auto operand = [&](const uintx4 *lds, int p, int m, int o) {
-        return lds[(p * BM + 16 * m + n) * ROW + (o ^ (n & (ROW - 1)))];
-    };
-    // 8-bit inputs: the eight columns of step k, in the codes' order
-    auto operand8 = [&](const uintx4 *lds, int m, int k) {
-        const int e = 4 * k + quad;
-        return bytes_like_codes(((const uintx2 *)lds)[((16 * m + n) * ROW + ((e >> 1) ^ (n & (ROW - 1)))) * 2 + (e & 1)]);
-    };
-    // sums x offsets of the groups [g0, g0 + count): four groups to an instruction
-    auto offsets = [&](int g0, int count) {
-        for (int g = 0; g < count; g += 4) {
-            const bool in = g + quad < count;
-            float b[NF];
+    // the groups' sums times what codes leave out of the weights, offset - 16 step: six of the nine products of terms (the
+    // first slice's work)
+    if (slice == 0) {
+        for (int g0 = 0; g0 < a.NG; g0 += 32) {
+            uintx4 B[3][NF];
 #pragma unroll
             for (int j = 0; j < NF; ++j) {
-                unsigned sc = 0;
-                if (in) {
-                    const int at = g0 + g + quad;
-                    sc = SUB > 1 ? a.scales[((rb[j] * a.KT + at / SUB) * 16 + n) * SUB + at % SUB]
-                                 : a.scales[(rb[j] * a.NG + a.group_of(at)) * 16 + n];
+                const int64_t rb = row_block(wn * NF + j);
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int g = g0 + 8 * quad + e;
+                    unsigned sc = 0;
+                    if (g < a.NG) sc = SUB > 1 ? a.scales[((rb * a.KT + g / SUB) * 16 + n) * SUB + g % SUB] : a.scales[(rb * a.NG + g) * 16 + n];
+                    v[e] = half_hi(sc) - base * half_lo(sc);
                 }
-                b[j] = half_hi(sc) - base * half_lo(sc);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float h0, m0, l0, h1, m1, l1;
+                    split3(v[2 * e], h0, m0, l0);
+                    split3(v[2 * e + 1], h1, m1, l1);
+                    B[0][j][e] = pair_bf16(h0, h1);
+                    B[1][j][e] = pair_bf16(m0, m1);
+                    B[2][j][e] = pair_bf16(l0, l1);
+                }
             }
 #pragma unroll
             for (int m = 0; m < MF; ++m) {
-                const float s = in ? sums[g + quad][wm * (BM / WM) + 16 * m + n] : 0.f;
+                const int t = t0 + (wm * MF + m) * 16 + n;
+                const unsigned short *src = tok.sums + (int64_t)(t < a.T ? t : a.T - 1) * tok.NGP + g0 + 8 * quad;
+                uintx4 A[3];
 #pragma unroll
-                for (int j = 0; j < NF; ++j) acc[m][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(s, b[j], acc[m][j], 0, 0, 0);
+                for (int p = 0; p < 3; ++p) A[p] = *(const uintx4 *)(src + p * (int64_t)a.T * tok.NGP);
+#pragma unroll
+                for (int o = 2; o >= 0; --o)
+#pragma unroll
+                    for (int p = 0; p <= o; ++p)
+#pragma unroll
+                        for (int j = 0; j < NF; ++j) acc[m][j] = mfma_bf16(A[p], B[o - p][j], acc[m][j]);
             }
         }
-    };
-    uintx4 codes[NF];
-    unsigned scale[NF][SUB];
-    auto fetch_codes = [&](int kt) {
-#pragma unroll
-        for (int j = 0; j < NF; ++j) {
-            codes[j] = a.codes[(rb[j] * a.KT + kt) * 64 + lane];
-#pragma unroll
-            for (int u = 0; u < SUB; ++u)
-                scale[j][u] = SUB > 1 ? a.scales[((rb[j] * a.KT + kt) * 16 + n) * SUB + u] : a.scales[(rb[j] * a.NG + a.group_of(kt)) * 16 + n];
-        }
-    };
-    fetch(kt0, even);
-    fetch_codes(kt0);
-    __builtin_amdgcn_s_waitcnt(kWaitVm0);
-    __syncthreads();
-    int done = kt0;      // tiles whose offsets are in
+    }
+    __builtin_amdgcn_s_waitcnt(wait_loads(0));
+    stage_barrier();
+
     auto turn = [&](const int kt, const uintx4 *lds, uintx4 *lds_next) __attribute__((always_inline)) {
+        fetch(kt + STAGES - 1, lds_next);
         uintx4 w[NF];
         float step[NF][SUB];
 #pragma unroll
         for (int j = 0; j < NF; ++j) {
-            w[j] = codes[j];
+            w[j] = lds[C::XN + (wn * NF + j) * 64 + lane];
 #pragma unroll
-            for (int u = 0; u < SUB; ++u) step[j][u] = half_lo(scale[j][u]);
+            for (int u = 0; u < SUB; ++u)
+                step[j][u] = half_lo(((const unsigned *)(lds + C::XN + C::WN16))[((wn * NF + j) * 16 + n) * SUB + u]);
         }
-        // (the last tile again after the last: a branch here would make the compiler wait for all of it at once)
-        const int ahead = kt + 1 < kt1 ? kt + 1 : kt;
-        fetch(ahead, lds_next);
-        fetch_codes(ahead);
-        // the tile's sums, a quarter of the tokens to each wave
-        for (int m = wave; m < BM / 16; m += 4) {
+        if constexpr (XT == OBC_I8) {
 #pragma unroll
             for (int u = 0; u < SUB; ++u) {
-                Sum<XT> s;
+                intx4 S[MF][NF];
+#pragma unroll
+                for (int m = 0; m < MF; ++m)
+#pragma unroll
+                    for (int j = 0; j < NF; ++j) S[m][j] = intx4{0, 0, 0, 0};
+                // eight columns of step k in the codes' order
+                auto operand = [&](int m, int k) {
+                    const int e = 4 * k + quad;
+                    return bytes_like_codes(((const uintx2 *)lds)[((16 * (wm * MF + m) + n) * ROW + ((e >> 1) ^ (n & (ROW - 1)))) * 2 + (e & 1)]);
+                };
+                if constexpr (SUB == 4) {
+                    uintx2 B[NF];
+#pragma unroll
+                    for (int j = 0; j < NF; ++j) B[j] = codes_i8(w[j][u]);
+#pragma unroll
+                    for (int m = 0; m < MF; ++m) {
+                        const uintx2 A = operand(m, u);
+#pragma unroll
+                        for (int j = 0; j < NF; ++j) S[m][j] = mfma_i8(A, B[j], S[m][j]);
+                    }
+                } else {
+#pragma unroll
+                    for (int k = u * 2 / SUB; k < (u + 1) * 2 / SUB; ++k) {
+                        intx4 B[NF];
+#pragma unroll
+                        for (int j = 0; j < NF; ++j) {
+                            const uintx2 lo = codes_i8(w[j][2 * k]), hi = codes_i8(w[j][2 * k + 1]);
+                            B[j] = intx4{(int)lo.x, (int)lo.y, (int)hi.x, (int)hi.y};
+                        }
+#pragma unroll
+                        for (int m = 0; m < MF; ++m) {
+                            const uintx2 lo = operand(m, 2 * k), hi = operand(m, 2 * k + 1);
+                            const intx4 A = {(int)lo.x, (int)lo.y, (int)hi.x, (int)hi.y};
+#pragma unroll
+                            for (int j = 0; j < NF; ++j) S[m][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(A, B[j], S[m][j], 0, 0, 0);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int m = 0; m < MF; ++m)
+#pragma unroll
+                    for (int j = 0; j < NF; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[m][j][i] = fmaf(step[j][u], (float)S[m][j][i], acc[m][j][i]);
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < SUB; ++u) {
+                floatx4 S[MF][NF];
+#pragma unroll
+                for (int m = 0; m < MF; ++m)
+#pragma unroll
+                    for (int j = 0; j < NF; ++j) S[m][j] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int k = u * 4 / SUB; k < (u + 1) * 4 / SUB; ++k) {
-                    Operand<XT> x;
-                    if constexpr (XT == OBC_F32) {
+                    uintx4 B[NF];
 #pragma unroll
-                        for (int p = 0; p < 3; ++p) x.v[p] = operand(lds, p, m, 4 * k + quad);
-                    } else if constexpr (XT == OBC_I8) {
-                        x.v = operand8(lds, m, k);
-                    } else {
-                        x.v = operand(lds, 0, m, 4 * k + quad);
-                    }
-                    s.add(x, Codes<XT>::ones());
-                }
-                if (n == 0)
+                    for (int j = 0; j < NF; ++j) B[j] = XT == OBC_F16 ? codes_f16(w[j][k]) : codes_bf16(w[j][k]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) sums[(kt - done) * SUB + u][16 * m + 4 * quad + i] = s[i];
-            }
-        }
-        uintx4 B[NF][XT == OBC_I8 ? 2 : 4];
-#pragma unroll
-        for (int j = 0; j < NF; ++j)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if constexpr (XT == OBC_I8) {
-                    const uintx2 c = codes_i8(w[j][k]);
-                    B[j][k >> 1][2 * (k & 1)] = c.x;
-                    B[j][k >> 1][2 * (k & 1) + 1] = c.y;
-                } else {
-                    B[j][k] = XT == OBC_F16 ? codes_f16(w[j][k]) : codes_bf16(w[j][k]);
-                }
-            }
-#pragma unroll
-        for (int m = 0; m < MF; ++m) {
-            const int mm = wm * MF + m;
-            if constexpr (XT == OBC_I8) {
-                uintx4 A[2];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uintx2 x = operand8(lds, mm, k);
-                    A[k >> 1][2 * (k & 1)] = x.x;
-                    A[k >> 1][2 * (k & 1) + 1] = x.y;
-                }
-#pragma unroll
-                for (int u = 0; u < SUB; ++u) {
-                    intx4 S[NF];
-#pragma unroll
-                    for (int j = 0; j < NF; ++j) {
-                        S[j] = intx4{0, 0, 0, 0};
-                        if constexpr (SUB == 4) {
-                            const uintx4 x = A[u >> 1], b = B[j][u >> 1];
-                            S[j] = u & 1 ? mfma_i8(uintx2{x.z, x.w}, uintx2{b.z, b.w}, S[j]) : mfma_i8(uintx2{x.x, x.y}, uintx2{b.x, b.y}, S[j]);
-                        } else {
-#pragma unroll
-                            for (int k = u * 2 / SUB; k < (u + 1) * 2 / SUB; ++k)
-                                S[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(intx4, A[k]), __builtin_bit_cast(intx4, B[j][k]), S[j], 0, 0, 0);
-                        }
-                    }
-#pragma unroll
-                    for (int j = 0; j < NF; ++j)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[m][j][i] = fmaf(step[j][u], (float)S[j][i], acc[m][j][i]);
-                }
-            } else {
-#pragma unroll
-                for (int u = 0; u < SUB; ++u) {
-                    floatx4 S[NF];
-#pragma unroll
-                    for (int j = 0; j < NF; ++j) S[j] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int k = u * 4 / SUB; k < (u + 1) * 4 / SUB; ++k) {
+                    for (int m = 0; m < MF; ++m)
 #pragma unroll
                         for (int p = P - 1; p >= 0; --p) {
-                            const uintx4 A = operand(lds, p, mm, 4 * k + quad);
+                            const uintx4 A = lds[(p * BM + 16 * (wm * MF + m) + n) * ROW + ((4 * k + quad) ^ n)];
 #pragma unroll
-                            for (int j = 0; j < NF; ++j) S[j] = XT == OBC_F16 ? mfma_f16(A, B[j][k], S[j]) : mfma_bf16(A, B[j][k], S[j]);
+                            for (int j = 0; j < NF; ++j) S[m][j] = XT == OBC_F16 ? mfma_f16(A, B[j], S[m][j]) : mfma_bf16(A, B[j], S[m][j]);
                         }
-                    }
+                }
+#pragma unroll
+                for (int m = 0; m < MF; ++m)
 #pragma unroll
                     for (int j = 0; j < NF; ++j)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[m][j][i] = fmaf(step[j][u], S[j][i], acc[m][j][i]);
-                }
+                        for (int i = 0; i < 4; ++i) acc[m][j][i] = fmaf(step[j][u], S[m][j][i], acc[m][j][i]);
             }
         }
-        __builtin_amdgcn_s_waitcnt(kWaitVm0);      // the next tile is in LDS
-        __syncthreads();
-        if ((kt + 1 - done + 1) * SUB > kSumGroups || kt + 1 == kt1) {
-            offsets(done * SUB, (kt + 1 - done) * SUB);
-            done = kt + 1;
-            __syncthreads();
-        }
+        __builtin_amdgcn_s_waitcnt(wait_loads(STAGES > 2 ? C::LOADS : 0));      // the next tile is in LDS
+        stage_barrier();
     };
-    for (int kt = kt0;; kt += 2) {
-        turn(kt, even, odd);
-        if (kt + 1 >= kt1) break;
-        turn(kt + 1, odd, even);
-        if (kt + 2 >= kt1) break;
+    for (int kt = kt0;;) {
+        turn(kt, lds0, STAGES > 2 ? lds2 : lds1);
+        if (++kt >= kt1) break;
+        turn(kt, lds1, lds0);
+        if (++kt >= kt1) break;
+        if (STAGES > 2) {
+            turn(kt, lds2, lds1);
+            if (++kt >= kt1) break;
+        }
     }
+    // (loads behind the last tile still write to LDS: they are waited for before it can be another workgroup's)
+    __builtin_amdgcn_s_waitcnt(wait_loads(0));
+    const bool sliced = tok.part != nullptr;
     auto put = [&](auto type) {
         constexpr int YT = decltype(type)::value;
 #pragma unroll
         for (int m = 0; m < MF; ++m)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int t = t0 + wm * (BM / WM) + 16 * m + 4 * quad + i;
+                const int t = t0 + (wm * MF + m) * 16 + 4 * quad + i;
                 if (t >= a.T) continue;
-                const bool sliced = tok.part != nullptr;
                 const float xs = XT == OBC_I8 && !sliced ? a.xs[t] : 1.f;
 #pragma unroll
                 for (int j = 0; j < NF; ++j) {
-                    const int r = (rb0 + j) * 16 + n;
+                    const int r = (rb0 + wn * NF + j) * 16 + n;
                     const float v = XT == OBC_I8 ? acc[m][j][i] * xs : acc[m][j][i];
                     if (r >= a.R) continue;
                     if (sliced) tok.part[((int64_t)slice * a.T + t) * a.R + r] = v;
@@ -620,28 +689,56 @@ inline bool laid_out(const void *x, int x_type, int64_t ldx, int d)
 
 // What a product with more tokens than the rows' kernel takes is cut into, and its workspace.
 struct Plan {
-    int BM, mtiles, ntiles, slices, per;
-    size_t laid, part, bytes;      // tokens laid out (where x is not like that already), the slices' sums
+    int BM, BN, mtiles, ntiles, slices, per, NGP;
+    size_t sums, laid, part, bytes;      // the groups' sums, tokens laid out (where x is not like that already), the slices' sums
 };
 
 Plan plan_of(const pack4_layout &L, int T, int x_type)
 {
     Plan p;
-    p.BM = T <= 32 ? 32 : T <= 64 || x_type == OBC_F32 ? 64 : 128;
-    p.mtiles = T / p.BM + (T % p.BM != 0);
-    p.ntiles = (L.RB + 7) / 8;
+    auto cut = [&](int BM, int BN) {
+        p.BM = BM;
+        p.BN = BN;
+        p.mtiles = T / BM + (T % BM != 0);
+        p.ntiles = (L.RB * 16 + BN - 1) / BN;
+        return (int64_t)p.mtiles * p.ntiles;
+    };
+    int64_t tiles = 0;
+    if (x_type == OBC_F32) tiles = T > 32 ? cut(64, 128) : cut(32, 128);
+    else if (T <= 32) tiles = cut(32, 128);
+    else if (T <= 64 || (tiles = cut(128, 256)) < 192) tiles = cut(64, 128);
     // two workgroups to a compute unit, two tiles at least to a slice
-    const int64_t tiles = (int64_t)p.mtiles * p.ntiles;
-    int64_t s = tiles > 0 ? 512 / tiles : 1;
+    int64_t s = p.BM < 128 && tiles > 0 ? 512 / tiles : 1;
     if (s > 16) s = 16;
     if (s > L.KT / 2) s = L.KT / 2;
     if (s < 1) s = 1;
     p.per = (int)((L.KT + s - 1) / s);
     p.slices = (L.KT + p.per - 1) / p.per;
-    p.laid = obc_align_up((size_t)T * L.KT * 128 * (x_type == OBC_F32 ? 6 : x_type == OBC_I8 ? 1 : 2), 256);
-    p.part = p.slices > 1 ? (size_t)p.slices * T * L.R * 4 : 0;
-    p.bytes = p.laid + p.part;
+    p.NGP = (L.NG + 31) / 32 * 32;
+    size_t at = 0;
+    auto take = [&](size_t n) { const size_t b = at; at += obc_align_up(n, 256); return b; };
+    p.sums = take((size_t)T * p.NGP * 6);
+    p.part = take(p.slices > 1 ? (size_t)p.slices * T * L.R * 4 : 0);
+    p.laid = take((size_t)T * L.KT * 128 * (x_type == OBC_F32 ? 6 : x_type == OBC_I8 ? 1 : 2));
+    p.bytes = at;
     return p;
+}
+
+template <int XT>
+void launch_lay(obc_ctx *ctx, const Args &a, const Lay &lay)
+{
+    auto blocks = [&](int team) { return (unsigned)((lay.jobs * team + 255) / 256); };
+    if (lay.G <= 32) product4_lay_kernel<XT, 4><<<blocks(4), 256, 0, ctx->stream>>>(a, lay);
+    else if (lay.G <= 64) product4_lay_kernel<XT, 8><<<blocks(8), 256, 0, ctx->stream>>>(a, lay);
+    else if (lay.G <= 128) product4_lay_kernel<XT, 16><<<blocks(16), 256, 0, ctx->stream>>>(a, lay);
+    else product4_lay_kernel<XT, 64><<<blocks(64), 256, 0, ctx->stream>>>(a, lay);
+}
+
+template <int XT, int SUB, int BM, int BN, int WM, int STAGES>
+void launch_tiles(obc_ctx *ctx, const Args &a, const Tokens &tok, int y_type, int slices)
+{
+    product4_tiles_kernel<XT, SUB, BM, BN, WM, STAGES>
+        <<<(unsigned)(tok.tiles * slices), tile_waves(BN) * 64, 0, ctx->stream>>>(a, tok, y_type);
 }
 
 template <int XT, int SUB, int NF>
@@ -667,22 +764,35 @@ int launch(obc_ctx *ctx, const Args &a, int y_type, const Plan &p, void *ws)
         return OBC_OK;
     }
     const int64_t blocks = (int64_t)p.mtiles * p.ntiles * p.slices, adds = ((int64_t)a.T * a.R + 255) / 256;
-    if (blocks > 0x7fffffff || (p.slices > 1 && adds > 0x7fffffff)) return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_product4: too many tiles");
-    Tokens tok = {(const char *)a.x, a.ldx * (int64_t)size_of_type(XT), 0, p.mtiles, p.mtiles * p.ntiles, p.per,
-                  p.slices > 1 ? (float *)((char *)ws + p.laid) : nullptr};
-    if (!laid_out(a.x, XT, a.ldx, a.d)) {
-        const int pieces = a.KT * (XT == OBC_I8 ? 8 : 16);
-        const int64_t jobs = (int64_t)a.T * pieces;
-        if ((jobs + 255) / 256 > 0x7fffffff) return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_product4: too many inputs");
-        product4_lay_kernel<XT><<<(unsigned)((jobs + 255) / 256), 256, 0, ctx->stream>>>(a.x, a.ldx, a.d, pieces, jobs, jobs, (uintx4 *)ws);
-        OBC_LAUNCH_CHECK(ctx, "product4_lay_kernel");
-        tok.x = (const char *)ws;
-        tok.ld = (int64_t)pieces * 16;
-        tok.plane = jobs * 16;
+    const bool as_it_lies = laid_out(a.x, XT, a.ldx, a.d);
+    Lay lay;
+    lay.sums = (unsigned short *)((char *)ws + p.sums);
+    lay.rows = as_it_lies ? nullptr : (uintx4 *)((char *)ws + p.laid);
+    lay.NGP = p.NGP;
+    lay.G = SUB > 1 ? 128 / SUB : a.tpg * 128;
+    lay.jobs = (int64_t)a.T * a.NG;
+    if (blocks > 0x7fffffff || (p.slices > 1 && adds > 0x7fffffff) || lay.jobs > 0x7fffffff)
+        return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_product4: too many tiles");
+    launch_lay<XT>(ctx, a, lay);
+    OBC_LAUNCH_CHECK(ctx, "product4_lay_kernel");
+    Tokens tok;
+    tok.x = as_it_lies ? (const char *)a.x : (const char *)lay.rows;
+    tok.ld = as_it_lies ? a.ldx * (int64_t)size_of_type(XT) : (int64_t)a.KT * (XT == OBC_I8 ? 128 : 256);
+    tok.plane = a.T * tok.ld;
+    tok.sums = lay.sums;
+    tok.NGP = p.NGP;
+    tok.mtiles = p.mtiles;
+    tok.tiles = p.mtiles * p.ntiles;
+    tok.per = p.per;
+    tok.part = p.slices > 1 ? (float *)((char *)ws + p.part) : nullptr;
+    if constexpr (XT == OBC_F32) {
+        if (p.BM == 32) launch_tiles<XT, SUB, 32, 128, 1, 2>(ctx, a, tok, y_type, p.slices);
+        else launch_tiles<XT, SUB, 64, 128, 1, 2>(ctx, a, tok, y_type, p.slices);
+    } else {
+        if (p.BM == 32) launch_tiles<XT, SUB, 32, 128, 1, 3>(ctx, a, tok, y_type, p.slices);
+        else if (p.BM == 64) launch_tiles<XT, SUB, 64, 128, 1, 3>(ctx, a, tok, y_type, p.slices);
+        else launch_tiles<XT, SUB, 128, 256, 2, 3>(ctx, a, tok, y_type, p.slices);
     }
-    if (p.BM == 32) product4_tiles_kernel<XT, SUB, 32, 1><<<(unsigned)blocks, 256, 0, ctx->stream>>>(a, tok, y_type);
-    else if (p.BM == 64 && XT != OBC_F32) product4_tiles_kernel<XT, SUB, 64, 1><<<(unsigned)blocks, 256, 0, ctx->stream>>>(a, tok, y_type);
-    else product4_tiles_kernel<XT, SUB, XT == OBC_F32 ? 64 : 128, 2><<<(unsigned)blocks, 256, 0, ctx->stream>>>(a, tok, y_type);
     OBC_LAUNCH_CHECK(ctx, "product4_tiles_kernel");
     if (p.slices > 1) {
         product4_add_kernel<<<(unsigned)adds, 256, 0, ctx->stream>>>(a, tok.part, p.slices, y_type);
@@ -730,7 +840,8 @@ int obc_product4(obc_ctx *ctx, const void *packed, int R, int d, int group, cons
         return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_product4: x or y is not aligned to its elements");
     const Plan p = plan_of(L, T, x_type);
     if (T > kRowsTokens) {
-        const size_t need = p.slices > 1 || !laid_out(x, x_type, ldx, d) ? p.bytes : 0;
+        // (tokens that lie as the kernel wants them need no room)
+        const size_t need = laid_out(x, x_type, ldx, d) ? p.laid : p.bytes;
         if (need > 0 && (!ws || ((uintptr_t)ws & 15) != 0 || ws_bytes < need))
             return obc_fail(ctx, OBC_ERR_WORKSPACE, "obc_product4: workspace of %zu bytes needed", need);
     }
