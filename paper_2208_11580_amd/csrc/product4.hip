@@ -17,11 +17,11 @@ struct Args {
     const float *xs;
     void *y;
     int T, R, d, RB, KT, NG, tpg;
-    unsigned tpg_inv;            // floor(2^32 / tpg) + 1, 0 for tpg = 1
+    unsigned tpg_inv, tpg_one;      // floor(2^32 / tpg) + 1 and 0; for tpg = 1, 0 and all ones
     int64_t ldx, ldy;
 
     // kt / tpg: exact while kt tpg < 2^32 (a row of 8 million columns)
-    __device__ int group_of(int kt) const { return tpg_inv ? (int)__umulhi((unsigned)kt, tpg_inv) : kt; }
+    __device__ int group_of(int kt) const { return (int)(__umulhi((unsigned)kt, tpg_inv) + ((unsigned)kt & tpg_one)); }
 };
 
 template <int V>
@@ -421,12 +421,14 @@ struct Tile {
     static constexpr int WN = WAVES / WM;
     static constexpr int P = XT == OBC_F32 ? 3 : 1, MF = BM / WM / 16, NF = BN / WN / 16;
     static constexpr int ROW = XT == OBC_I8 ? 8 : 16;      // 16-byte pieces of a token's 128 columns
-    static constexpr int XN = P * BM * ROW, WN16 = BN * 4, SN = BN * SUB / 4;      // 16-byte places of a stage: tokens, codes, steps
-    static constexpr int PLACES = XN + WN16 + SN;
-    // loads of a wave for a stage: 64 places each, the steps 4 bytes a lane
+    static constexpr int XN = P * BM * ROW, WN16 = BN * 4;      // 16-byte places of a stage: tokens, codes
+    // loads of a wave for a stage: 64 places each, and 64 steps -- 32 of them twice where a wave has only 32 to load: what the
+    // compiler makes of waits depends on every path having the same loads
     static constexpr int XL = XN / 64 / WAVES, WL = WN16 / 64 / WAVES, SL = BN * SUB / 64 / WAVES > 0 ? BN * SUB / 64 / WAVES : 1;
     static constexpr int SLANES = BN * SUB / WAVES < 64 ? BN * SUB / WAVES : 64;
     static constexpr int LOADS = XL + WL + SL;
+    static constexpr int PLACES = XN + WN16 + SL * WAVES * 16;
+    static __device__ int step_at(int e) { return e / SLANES * 64 + e % SLANES; }
     static_assert(XN % (64 * WAVES) == 0 && WN16 % (64 * WAVES) == 0, "whole loads");
 };
 
@@ -462,11 +464,11 @@ __global__ __launch_bounds__(tile_waves(BN) * 64, 2) void product4_tiles_kernel(
     }
 #pragma unroll
     for (int i = 0; i < C::WL; ++i) wsrc[i] = (const char *)a.codes + (row_block(i * C::WAVES + wave) * a.KT + kt0) * 1024 + lane * 16;
-    // steps: row r of the tile, group u of its SUB at (r SUB + u) * 4
+    // steps: row r of the tile, group u of its SUB is the step r SUB + u
     int64_t srow[C::SL];
 #pragma unroll
     for (int i = 0; i < C::SL; ++i) {
-        const int e = (i * C::WAVES + wave) * C::SLANES + lane, r = (e / SUB) % BN;
+        const int e = (i * C::WAVES + wave) * C::SLANES + lane % C::SLANES, r = e / SUB;
         srow[i] = SUB > 1 ? ((row_block(r >> 4) * a.KT) * 16 + (r & 15)) * SUB + e % SUB : row_block(r >> 4) * a.NG * 16 + (r & 15);
         ssrc[i] = (const char *)a.scales + srow[i] * 4;
     }
@@ -479,10 +481,9 @@ __global__ __launch_bounds__(tile_waves(BN) * 64, 2) void product4_tiles_kernel(
         for (int i = 0; i < C::WL; ++i)
             __builtin_amdgcn_global_load_lds((global_ptr)(wsrc[i] + (int64_t)k * 1024), (lds_ptr)(lds + C::XN + (i * C::WAVES + wave) * 64), 16, 0, 0);
         const int64_t s = SUB > 1 ? (int64_t)(k + kt0) * 64 * SUB : (int64_t)a.group_of(k + kt0) * 64;
-        if (C::SLANES == 64 || lane < C::SLANES)
 #pragma unroll
-            for (int i = 0; i < C::SL; ++i)
-                __builtin_amdgcn_global_load_lds((global_ptr)(ssrc[i] + s), (lds_ptr)((unsigned *)(lds + C::XN + C::WN16) + (i * C::WAVES + wave) * C::SLANES), 4, 0, 0);
+        for (int i = 0; i < C::SL; ++i)
+            __builtin_amdgcn_global_load_lds((global_ptr)(ssrc[i] + s), (lds_ptr)((unsigned *)(lds + C::XN + C::WN16) + (i * C::WAVES + wave) * 64), 4, 0, 0);
     };
     fetch(kt0, lds0);
     if (STAGES > 2) fetch(kt0 + 1, lds1);
@@ -546,7 +547,7 @@ __global__ __launch_bounds__(tile_waves(BN) * 64, 2) void product4_tiles_kernel(
             w[j] = lds[C::XN + (wn * NF + j) * 64 + lane];
 #pragma unroll
             for (int u = 0; u < SUB; ++u)
-                step[j][u] = half_lo(((const unsigned *)(lds + C::XN + C::WN16))[((wn * NF + j) * 16 + n) * SUB + u]);
+                step[j][u] = half_lo(((const unsigned *)(lds + C::XN + C::WN16))[C::step_at(((wn * NF + j) * 16 + n) * SUB + u)]);
         }
         if constexpr (XT == OBC_I8) {
 #pragma unroll
@@ -851,6 +852,7 @@ int obc_product4(obc_ctx *ctx, const void *packed, int R, int d, int group, cons
     a.x = x; a.xs = x_scale; a.y = y;
     a.T = T; a.R = R; a.d = d; a.RB = L.RB; a.KT = L.KT; a.NG = L.NG; a.tpg = L.tpg;
     a.tpg_inv = L.tpg > 1 ? (unsigned)(0x100000000ull / (unsigned)L.tpg) + 1u : 0u;
+    a.tpg_one = L.tpg > 1 ? 0u : ~0u;
     a.ldx = ldx; a.ldy = ldy;
     switch (x_type) {
     case OBC_F32: return launch_sub<OBC_F32>(ctx, a, L.SUB, y_type, p, ws);
