@@ -107,5 +107,27 @@ __device__ inline void store_as(void *y, int64_t at, float v)
     else ((__bf16 *)y)[at] = (__bf16)v;
 }
 
+typedef __attribute__((address_space(1))) const void *global_ptr;
+typedef __attribute__((address_space(3))) void *lds_ptr;
+
+// s_waitcnt vmcnt(n) lgkmcnt(0): all loads but the n newest, and every access to LDS
+constexpr int wait_loads(int n) { return 0x0070 | (n & 15) | (n >> 4) << 14; }
+
+// A barrier that waits for nothing itself: __syncthreads (and a fence) would wait for every load on its way, the newest stages'
+// among them.  wait_loads goes before it: what a wave has read from LDS has then arrived, and its share of the next stage is there.
+__device__ inline void stage_barrier()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Consecutive workgroups go to different dies, each with a cache of its own: a die takes a run of tiles.
+__device__ inline int tile_of(int id, int tiles)
+{
+    const int each = tiles >> 3, left = tiles & 7, die = id & 7;
+    return die * each + (die < left ? die : left) + (id >> 3);
+}
+
 static inline bool float_type(int type) { return type == OBC_F32 || type == OBC_F16 || type == OBC_BF16; }
 static inline size_t size_of_type(int type) { return type == OBC_F32 ? 4 : type == OBC_I8 ? 1 : 2; }

@@ -395,21 +395,6 @@ struct Tokens {
     float *part;             // slices x T x R sums, where there are several
 };
 
-typedef __attribute__((address_space(1))) const void *global_ptr;
-typedef __attribute__((address_space(3))) void *lds_ptr;
-
-// s_waitcnt vmcnt(n) lgkmcnt(0): all loads but the n newest, and every access to LDS
-constexpr int wait_loads(int n) { return 0x0070 | (n & 15) | (n >> 4) << 14; }
-
-// A barrier that waits for nothing itself: __syncthreads (and a fence) would wait for every load on its way, the newest stages'
-// among them.  wait_loads goes before it: what a wave has read from LDS has then arrived, and its share of the next stage is there.
-__device__ inline void stage_barrier()
-{
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
-
 // BM tokens x BN rows of W to a workgroup of WM x WN waves.  Tokens, codes and steps of STAGES column tiles go through LDS in
 // turn, so that loads have STAGES - 1 tiles' time to arrive; a wave waits for all but its newest ones and then for the others.
 // Within a tile the codes are unpacked step by step between the matrix instructions of the step before.
@@ -442,10 +427,7 @@ __global__ __launch_bounds__(tile_waves(BN) * 64, 2) void product4_tiles_kernel(
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 15, quad = lane >> 4;
     const int wm = wave % WM, wn = wave / WM;
-    // consecutive workgroups go to different dies: give each die a run of tiles
-    const int slice = blockIdx.x / tok.tiles, id = blockIdx.x % tok.tiles;
-    const int each = tok.tiles >> 3, left = tok.tiles & 7, die = id & 7;
-    const int tile = die * each + (die < left ? die : left) + (id >> 3);
+    const int slice = blockIdx.x / tok.tiles, tile = tile_of(blockIdx.x % tok.tiles, tok.tiles);
     const int t0 = (tile % tok.mtiles) * BM, rb0 = (tile / tok.mtiles) * (BN / 16);
     const int kt0 = slice * tok.per, kt1 = kt0 + tok.per < a.KT ? kt0 + tok.per : a.KT;
     constexpr float base = XT == OBC_I8 ? 0.f : kCodeBase;
@@ -708,8 +690,8 @@ Plan plan_of(const pack4_layout &L, int T, int x_type)
     if (x_type == OBC_F32) tiles = T > 32 ? cut(64, 128) : cut(32, 128);
     else if (T <= 32) tiles = cut(32, 128);
     else if (T <= 64 || (tiles = cut(128, 256)) < 192) tiles = cut(64, 128);
-    // two workgroups to a compute unit, two tiles at least to a slice
-    int64_t s = p.BM < 128 && tiles > 0 ? 512 / tiles : 1;
+    // two workgroups to a compute unit (fp32 in tiles of 64: one), two tiles at least to a slice
+    int64_t s = p.BM < 128 && tiles > 0 ? (x_type == OBC_F32 && p.BM == 64 ? 256 : 512) / tiles : 1;
     if (s > 16) s = 16;
     if (s > L.KT / 2) s = L.KT / 2;
     if (s < 1) s = 1;
@@ -723,6 +705,28 @@ Plan plan_of(const pack4_layout &L, int T, int x_type)
     p.laid = take((size_t)T * L.KT * 128 * (x_type == OBC_F32 ? 6 : x_type == OBC_I8 ? 1 : 2));
     p.bytes = at;
     return p;
+}
+
+// The rows' kernel: up to 16 tokens, if they fit in LDS at once or there are rows for every compute unit.  (16 tokens through
+// 768 x 16384: 62 us in fp32 and 24 in half precision with 16 and 3 fillings of LDS in 48 workgroups, in tiles 27 and 21;
+// through 4096 x 4096 in half precision 9 us, in tiles 16.)
+struct Rows {
+    int NF, blocks, waves, chunk;
+};
+
+bool takes_rows(const pack4_layout &L, int T, int x_type, Rows *r)
+{
+    if (T > kRowsTokens) return false;
+    const bool wide = x_type == OBC_F32;
+    r->NF = L.RB > 256 ? 2 : 1;
+    r->blocks = (L.RB + r->NF - 1) / r->NF;
+    // sixteen waves to a compute unit, in one workgroup or two; no more than there are tiles
+    int waves = r->blocks > 256 || wide ? 8 : 16;
+    const int room = kRowsLds / (r->blocks > 256 ? 2 : 1) / (T * (wide ? 768 : x_type == OBC_I8 ? 128 : 256));
+    while (waves > 1 && (waves / 2 >= L.KT || (room < L.KT && room < waves))) waves /= 2;
+    r->waves = waves;
+    r->chunk = room >= L.KT ? L.KT : room / waves * waves;
+    return room >= L.KT || r->blocks >= 200;
 }
 
 template <int XT>
@@ -750,17 +754,11 @@ void launch_rows(obc_ctx *ctx, const Args &a, int y_type, int waves, int chunk)
 }
 
 template <int XT, int SUB>
-int launch(obc_ctx *ctx, const Args &a, int y_type, const Plan &p, void *ws)
+int launch(obc_ctx *ctx, const Args &a, int y_type, const Rows *rows, const Plan &p, void *ws)
 {
-    if (a.T <= kRowsTokens) {
-        // sixteen waves to a compute unit, in one workgroup or two; no more than there are tiles
-        const int NF = a.RB > 256 ? 2 : 1, blocks = (a.RB + NF - 1) / NF;
-        int waves = blocks > 256 || XT == OBC_F32 ? 8 : 16;
-        const int room = kRowsLds / (blocks > 256 ? 2 : 1) / (a.T * tile_bytes(XT));
-        while (waves > 1 && (waves / 2 >= a.KT || (room < a.KT && room < waves))) waves /= 2;
-        const int chunk = room >= a.KT ? a.KT : room / waves * waves;
-        if (NF == 2) launch_rows<XT, SUB, 2>(ctx, a, y_type, waves, chunk);
-        else launch_rows<XT, SUB, 1>(ctx, a, y_type, waves, chunk);
+    if (rows) {
+        if (rows->NF == 2) launch_rows<XT, SUB, 2>(ctx, a, y_type, rows->waves, rows->chunk);
+        else launch_rows<XT, SUB, 1>(ctx, a, y_type, rows->waves, rows->chunk);
         OBC_LAUNCH_CHECK(ctx, "product4_rows_kernel");
         return OBC_OK;
     }
@@ -803,9 +801,9 @@ int launch(obc_ctx *ctx, const Args &a, int y_type, const Plan &p, void *ws)
 }
 
 template <int XT>
-int launch_sub(obc_ctx *ctx, const Args &a, int sub, int y_type, const Plan &p, void *ws)
+int launch_sub(obc_ctx *ctx, const Args &a, int sub, int y_type, const Rows *rows, const Plan &p, void *ws)
 {
-    return sub == 1 ? launch<XT, 1>(ctx, a, y_type, p, ws) : sub == 2 ? launch<XT, 2>(ctx, a, y_type, p, ws) : launch<XT, 4>(ctx, a, y_type, p, ws);
+    return sub == 1 ? launch<XT, 1>(ctx, a, y_type, rows, p, ws) : sub == 2 ? launch<XT, 2>(ctx, a, y_type, rows, p, ws) : launch<XT, 4>(ctx, a, y_type, rows, p, ws);
 }
 
 }  // namespace
@@ -817,7 +815,8 @@ int obc_product4_workspace_bytes(int T, int R, int d, int group, int x_type, siz
     pack4_layout L;
     if (!bytes || T < 0 || R < 0 || d <= 0 || !(float_type(x_type) || x_type == OBC_I8) || !pack4_layout_of(R, d, group, &L))
         return OBC_ERR_BAD_ARG;
-    *bytes = T > kRowsTokens && R > 0 ? plan_of(L, T, x_type).bytes : 0;
+    Rows r;
+    *bytes = T > 0 && R > 0 && !takes_rows(L, T, x_type, &r) ? plan_of(L, T, x_type).bytes : 0;
     return OBC_OK;
 }
 
@@ -839,8 +838,10 @@ int obc_product4(obc_ctx *ctx, const void *packed, int R, int d, int group, cons
     if (((uintptr_t)packed & 15) != 0) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_product4: packed is not aligned to 16 bytes");
     if (((uintptr_t)x & (size_of_type(x_type) - 1)) != 0 || ((uintptr_t)y & (size_of_type(y_type) - 1)) != 0)
         return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_product4: x or y is not aligned to its elements");
-    const Plan p = plan_of(L, T, x_type);
-    if (T > kRowsTokens) {
+    Rows r;
+    const Rows *const rows = takes_rows(L, T, x_type, &r) ? &r : nullptr;
+    const Plan p = rows ? Plan() : plan_of(L, T, x_type);
+    if (!rows) {
         // (tokens that lie as the kernel wants them need no room)
         const size_t need = laid_out(x, x_type, ldx, d) ? p.laid : p.bytes;
         if (need > 0 && (!ws || ((uintptr_t)ws & 15) != 0 || ws_bytes < need))
@@ -855,10 +856,10 @@ int obc_product4(obc_ctx *ctx, const void *packed, int R, int d, int group, cons
     a.tpg_one = L.tpg > 1 ? 0u : ~0u;
     a.ldx = ldx; a.ldy = ldy;
     switch (x_type) {
-    case OBC_F32: return launch_sub<OBC_F32>(ctx, a, L.SUB, y_type, p, ws);
-    case OBC_F16: return launch_sub<OBC_F16>(ctx, a, L.SUB, y_type, p, ws);
-    case OBC_BF16: return launch_sub<OBC_BF16>(ctx, a, L.SUB, y_type, p, ws);
-    default: return launch_sub<OBC_I8>(ctx, a, L.SUB, y_type, p, ws);
+    case OBC_F32: return launch_sub<OBC_F32>(ctx, a, L.SUB, y_type, rows, p, ws);
+    case OBC_F16: return launch_sub<OBC_F16>(ctx, a, L.SUB, y_type, rows, p, ws);
+    case OBC_BF16: return launch_sub<OBC_BF16>(ctx, a, L.SUB, y_type, rows, p, ws);
+    default: return launch_sub<OBC_I8>(ctx, a, L.SUB, y_type, rows, p, ws);
     }
 }
 

@@ -33,23 +33,31 @@ struct Args {
 };
 
 // ---- layout -------------------------------------------------------------------------------------------------------
+constexpr int kKeep = 4;      // pieces of a token's gradients that a thread keeps between the largest and the rounding
 
-// Workgroups below `turns`: 64 rows x 128 columns of codes, a thread an octet of rows x an octet of columns (and a group's
-// steps along the way); the others: a token's gradients each.
+// Workgroups below `turns`: 128 rows x 128 columns of codes, through LDS; then the groups' steps; the others: a token's gradients.
 template <int TYPE>
 __global__ __launch_bounds__(256) void grad_lay_kernel(Args a, int64_t turns, int64_t scale_blocks)
 {
     const int tid = threadIdx.x;
     if ((int64_t)blockIdx.x < turns) {
-        // octets: 16 of columns (a tile's 4 dwords x 4 quads) x 16 of rows of one row tile
+        __shared__ unsigned codes[2048 + 256];      // a dword of padding behind every eight
+        auto at = [](int i) { return i + (i >> 3); };
         const int kt = (int)((int64_t)blockIdx.x / a.RT), rt = (int)((int64_t)blockIdx.x % a.RT);
-        const int co = tid & 15, ro = tid >> 4;      // column octet 4 s + quad, row octet 4 s + quad
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int e = h * 256 + tid, rb = rt * 8 + (e >> 6);      // 16-byte place of the eight tiles
+            uintx4 v = {0u, 0u, 0u, 0u};
+            if (rb < a.RB) v = *((const uintx4 *)a.codes + ((int64_t)rb * a.KT + kt) * 64 + (e & 63));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) codes[at(e * 4 + j)] = v[j];
+        }
+        __syncthreads();
+        // a thread turns an octet of rows x an octet of columns; octets count 4 s + quad
+        const int co = tid & 15, ro = tid >> 4;
         unsigned in[8], out[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int row = rt * 128 + ro * 8 + i;
-            in[i] = row < a.RB * 16 ? a.codes[((int64_t)(row >> 4) * a.KT + kt) * 256 + ((co & 3) * 16 + (row & 15)) * 4 + (co >> 2)] : 0u;
-        }
+        for (int i = 0; i < 8; ++i) in[i] = codes[at((ro >> 1) * 256 + ((co & 3) * 16 + (ro & 1) * 8 + i) * 4 + (co >> 2))];
         // nibble of element e: (e >> 1) + 4 (e & 1)
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
@@ -58,10 +66,17 @@ __global__ __launch_bounds__(256) void grad_lay_kernel(Args a, int64_t turns, in
             for (int i = 0; i < 8; ++i) w |= ((in[i] >> (4 * ((c >> 1) + 4 * (c & 1)))) & 15u) << (4 * ((i >> 1) + 4 * (i & 1)));
             out[c] = w;
         }
+        __syncthreads();
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            const int col = co * 8 + c;
-            a.turned[((int64_t)(kt * 8 + (col >> 4)) * a.RT + rt) * 256 + ((ro & 3) * 16 + (col & 15)) * 4 + (ro >> 2)] = out[c];
+        for (int c = 0; c < 8; ++c) codes[at((co >> 1) * 256 + ((ro & 3) * 16 + (co & 1) * 8 + c) * 4 + (ro >> 2))] = out[c];
+        __syncthreads();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int e = h * 256 + tid;
+            uintx4 v;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = codes[at(e * 4 + j)];
+            *((uintx4 *)a.turned + ((int64_t)(kt * 8 + (e >> 6)) * a.RT + rt) * 64 + (e & 63)) = v;
         }
         return;
     }
@@ -78,68 +93,99 @@ __global__ __launch_bounds__(256) void grad_lay_kernel(Args a, int64_t turns, in
         return;
     }
     const int64_t t = (int64_t)blockIdx.x - turns - scale_blocks;
-    const int pieces = a.RT * 16;
+    const int pieces = a.RT * 16, whole = a.R >> 3;      // pieces of eight elements, of which `whole` lie inside the row
     const int64_t at = t * a.lddy, plane = (int64_t)a.T * pieces;
-    auto load = [&](int r, float (&v)[8]) {
+    auto load = [&](int p, float (&v)[8]) {
+        const int r = p * 8;
+        if (p < whole) {
+            if (TYPE == OBC_F32) {
+                const floatx4 lo = *(const floatx4_at4 *)((const float *)a.dy + at + r), hi = *(const floatx4_at4 *)((const float *)a.dy + at + r + 4);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if (TYPE == OBC_F32) v[j] = r + j < a.R ? ((const float *)a.dy)[at + r + j] : 0.f;
-            else if (TYPE == OBC_F16) v[j] = r + j < a.R ? (float)((const _Float16 *)a.dy)[at + r + j] : 0.f;
-            else v[j] = r + j < a.R ? (float)((const __bf16 *)a.dy)[at + r + j] : 0.f;
+                for (int j = 0; j < 4; ++j) { v[j] = lo[j]; v[4 + j] = hi[j]; }
+            } else {
+                const uintx4 w = *(const uintx4_at2 *)((const unsigned short *)a.dy + at + r);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const unsigned x = w[j];
+                    v[2 * j] = TYPE == OBC_F16 ? half_lo(x) : bf16_lo(x);
+                    v[2 * j + 1] = TYPE == OBC_F16 ? half_hi(x) : bf16_hi(x);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (TYPE == OBC_F32) v[j] = r + j < a.R ? ((const float *)a.dy)[at + r + j] : 0.f;
+                else if (TYPE == OBC_F16) v[j] = r + j < a.R ? (float)((const _Float16 *)a.dy)[at + r + j] : 0.f;
+                else v[j] = r + j < a.R ? (float)((const __bf16 *)a.dy)[at + r + j] : 0.f;
+            }
         }
     };
-    float up = 1.f;
-    if (TYPE == OBC_BF16) {
-        __shared__ float tops[4];
-        float top = 0.f;
-        for (int p = tid; p < pieces; p += 256) {
-            float v[8];
-            load(p * 8, v);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(v[j]));
-        }
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-        if ((tid & 63) == 0) tops[tid >> 6] = top;
-        __syncthreads();
-        top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-        // 2^14 / the power of two below the largest; both it and its inverse are normal numbers
-        int e;
-        (void)frexpf(top, &e);
-        up = top > 0.f && top < __builtin_inff() ? ldexpf(1.f, e > -111 ? 15 - e : 126) : 1.f;
-        if (tid == 0) a.back[t] = 1.f / up;
-    }
-    for (int p = tid; p < pieces; p += 256) {
-        float v[8];
-        load(p * 8, v);
-        uint4 w[3];
-        unsigned *u = (unsigned *)w;
+    auto put = [&](int p, const float (&v)[8], float up) {
+        uintx4 w[3];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             if (TYPE == OBC_F32) {
                 float h0, m0, l0, h1, m1, l1;
                 split3(v[2 * j], h0, m0, l0);
                 split3(v[2 * j + 1], h1, m1, l1);
-                u[j] = pair_bf16(h0, h1);
-                u[4 + j] = pair_bf16(m0, m1);
-                u[8 + j] = pair_bf16(l0, l1);
+                w[0][j] = pair_bf16(h0, h1);
+                w[1][j] = pair_bf16(m0, m1);
+                w[2][j] = pair_bf16(l0, l1);
             } else {
-                u[j] = pair_f16(v[2 * j] * up, v[2 * j + 1] * up);
+                w[0][j] = pair_f16(v[2 * j] * up, v[2 * j + 1] * up);
             }
         }
-        a.rows[t * pieces + p] = w[0];
+        uintx4 *const to = (uintx4 *)a.rows + t * pieces + p;
+        to[0] = w[0];
         if (TYPE == OBC_F32) {
-            a.rows[plane + t * pieces + p] = w[1];
-            a.rows[2 * plane + t * pieces + p] = w[2];
+            to[plane] = w[1];
+            to[2 * plane] = w[2];
         }
+    };
+    if (TYPE != OBC_BF16) {
+        for (int p = tid; p < pieces; p += 256) {
+            float v[8];
+            load(p, v);
+            put(p, v, 1.f);
+        }
+        return;
+    }
+    __shared__ float tops[4];
+    float kept[kKeep][8], top = 0.f;
+#pragma unroll
+    for (int i = 0; i < kKeep; ++i)
+        if (i * 256 + tid < pieces) {
+            load(i * 256 + tid, kept[i]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(kept[i][j]));
+        }
+    for (int p = kKeep * 256 + tid; p < pieces; p += 256) {
+        float v[8];
+        load(p, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(v[j]));
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+    if ((tid & 63) == 0) tops[tid >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+    // 2^14 / the power of two below the largest; both it and its inverse are normal numbers
+    int e;
+    (void)frexpf(top, &e);
+    const float up = top > 0.f && top < __builtin_inff() ? ldexpf(1.f, e > -111 ? 15 - e : 126) : 1.f;
+    if (tid == 0) a.back[t] = 1.f / up;
+#pragma unroll
+    for (int i = 0; i < kKeep; ++i)
+        if (i * 256 + tid < pieces) put(i * 256 + tid, kept[i], up);
+    for (int p = kKeep * 256 + tid; p < pieces; p += 256) {
+        float v[8];
+        load(p, v);
+        put(p, v, up);
     }
 }
 
 // ---- product ------------------------------------------------------------------------------------------------------
-typedef __attribute__((address_space(1))) const void *global_ptr;
-typedef __attribute__((address_space(3))) void *lds_ptr;
-constexpr int kWaitVm0 = 0x0f70;      // s_waitcnt vmcnt(0)
-
 // Eight weights of a lane's column, of the eight rows that `steps` and `offsets` (half precision) belong to.
 __device__ inline uintx4 weights_f16(unsigned w, uintx4 steps, uintx4 offsets)
 {
@@ -168,68 +214,86 @@ __device__ inline void weights_split(unsigned w, uintx4 steps, uintx4 offsets, u
     }
 }
 
-// BM tokens x 128 columns to a workgroup of WM x (4 / WM) waves.
-template <int TYPE, int BM, int WM>
-__global__ __launch_bounds__(256, 2) void grad_tiles_kernel(Args a, int mtiles, int ntiles)
+template <int TYPE, int BM, int BN, int WM>
+struct Tile {
+    static constexpr int P = TYPE == OBC_F32 ? 3 : 1, WAVES = BN / 32, WN = WAVES / WM, MF = BM / WM / 16, NF = BN / WN / 16;
+    static constexpr int XN = P * BM * 16, CN = BN * 4;      // 16-byte places of a stage: gradients, codes; then steps
+    static constexpr int PLACES = XN + CN + WAVES * 32;
+    // loads of a wave for a stage: 64 places each, and twice 64 times 4 bytes of steps and offsets, a quarter of a tile's columns
+    static constexpr int XL = XN / 64 / WAVES, CL = CN / 64 / WAVES, LOADS = XL + CL + 2;
+    static_assert(XN % (64 * WAVES) == 0 && CN % (64 * WAVES) == 0, "whole loads");
+};
+
+// BM tokens x BN columns to a workgroup of WM x WN waves: gradients, codes and steps of 128 rows go through three stages of LDS in
+// turn, as in the forward product.
+template <int TYPE, int BM, int BN, int WM>
+__global__ __launch_bounds__(BN * 2, 2) void grad_tiles_kernel(Args a, int mtiles, int ntiles)
 {
-    constexpr int P = TYPE == OBC_F32 ? 3 : 1, WN = 4 / WM, MF = BM / WM / 16, NF = 8 / WN;
-    __shared__ uintx4 even[P * BM * 16], odd[P * BM * 16];
-    __shared__ uintx4 even_steps[128], odd_steps[128];       // four groups of 128 rows: steps and offsets
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    using C = Tile<TYPE, BM, BN, WM>;
+    constexpr int P = C::P, MF = C::MF, NF = C::NF;
+    __shared__ uintx4 lds0[C::PLACES], lds1[C::PLACES], lds2[C::PLACES];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 15, quad = lane >> 4;
     const int wm = wave % WM, wn = wave / WM;
-    const int tiles = mtiles * ntiles, slice = blockIdx.x / tiles, id = blockIdx.x % tiles;
-    const int per = tiles >> 3, left = tiles & 7, die = id & 7;
-    const int tile = die * per + (die < left ? die : left) + (id >> 3);
-    const int t0 = (tile % mtiles) * BM, kt = tile / mtiles;
+    const int tiles = mtiles * ntiles, slice = blockIdx.x / tiles, tile = tile_of(blockIdx.x % tiles, tiles);
+    const int t0 = (tile % mtiles) * BM, kt = tile / mtiles * (BN / 128);      // first token, first tile of 128 columns
     const int rt0 = slice * a.per, rt1 = rt0 + a.per < a.RT ? rt0 + a.per : a.RT;
     const int64_t plane = (int64_t)a.T * a.RT * 256;       // bytes
     const int64_t len = (int64_t)a.RT * 128;
+    // where this lane's loads come from, at the slice's first tile; piece o of token t at place o ^ (t mod 16) of its row
+    const char *xsrc[C::XL], *csrc[C::CL], *ssrc;
+#pragma unroll
+    for (int i = 0; i < C::XL; ++i) {
+        const int first = (i * C::WAVES + wave) * 4;
+        const int p = P > 1 ? first / BM : 0, t = first - p * BM + (lane >> 4);
+        const int row = t0 + t < a.T ? t0 + t : a.T - 1;
+        xsrc[i] = (const char *)a.rows + p * plane + ((int64_t)row * a.RT + rt0) * 256 + ((lane & 15) ^ (t & 15)) * 16;
+    }
+#pragma unroll
+    for (int i = 0; i < C::CL; ++i) {
+        int cb = kt * 8 + i * C::WAVES + wave;
+        if (cb >= a.KT * 8) cb = a.KT * 8 - 1;      // beyond the last column: not stored
+        csrc[i] = (const char *)a.turned + ((int64_t)cb * a.RT + rt0) * 1024 + lane * 16;
+    }
+    {
+        const int own = kt + (wave >> 2);      // the tile of this wave's 32 columns
+        int g = a.SUB > 1 ? own * a.SUB + (wave & 3) * a.SUB / 4 : own / a.tpg;
+        if (g >= a.NG) g = a.NG - 1;
+        ssrc = (const char *)(a.steps + 2 * g * len + rt0 * 128) + lane * 4;
+    }
+    auto fetch = [&](int rt, uintx4 *lds) __attribute__((always_inline)) {
+        const int64_t k = (rt < rt1 ? rt : rt1 - 1) - rt0;      // (behind the last: its tile again, for the count of loads)
+#pragma unroll
+        for (int i = 0; i < C::XL; ++i)
+            __builtin_amdgcn_global_load_lds((global_ptr)(xsrc[i] + k * 256), (lds_ptr)(lds + (i * C::WAVES + wave) * 64), 16, 0, 0);
+#pragma unroll
+        for (int i = 0; i < C::CL; ++i)
+            __builtin_amdgcn_global_load_lds((global_ptr)(csrc[i] + k * 1024), (lds_ptr)(lds + C::XN + (i * C::WAVES + wave) * 64), 16, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            __builtin_amdgcn_global_load_lds((global_ptr)(ssrc + i * len * 2 + k * 256), (lds_ptr)(lds + C::XN + C::CN + wave * 32 + i * 16), 4, 0, 0);
+    };
     floatx4 acc[MF][NF];
 #pragma unroll
     for (int m = 0; m < MF; ++m)
 #pragma unroll
         for (int j = 0; j < NF; ++j) acc[m][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    // piece o of token t at place o ^ (t mod 16) of its row, as in the forward product
-    auto fetch = [&](int rt, uintx4 *lds, uintx4 *steps) {
-#pragma unroll
-        for (int i = 0; i < P * BM / 16; ++i) {
-            const int first = (i * 4 + wave) * 4;
-            const int p = P > 1 ? first / BM : 0, t = first - p * BM + (lane >> 4);
-            const int row = t0 + t < a.T ? t0 + t : a.T - 1;
-            const char *src = (const char *)a.rows + p * plane + ((int64_t)row * a.RT + rt) * 256 + ((lane & 15) ^ (t & 15)) * 16;
-            __builtin_amdgcn_global_load_lds((global_ptr)src, (lds_ptr)(lds + first * 16), 16, 0, 0);
-        }
-        if (wave < 2) {
-            int g = a.SUB > 1 ? kt * a.SUB + (2 * wave + (lane >> 5)) * a.SUB / 4 : kt / a.tpg;
-            if (g >= a.NG) g = a.NG - 1;
-            const char *src = (const char *)(a.steps + (2 * g + ((lane >> 4) & 1)) * len + rt * 128) + (lane & 15) * 16;
-            __builtin_amdgcn_global_load_lds((global_ptr)src, (lds_ptr)(steps + wave * 64), 16, 0, 0);
-        }
-    };
-    uintx4 codes[NF];
-    auto fetch_codes = [&](int rt) {
-#pragma unroll
-        for (int j = 0; j < NF; ++j) codes[j] = *((const uintx4 *)a.turned + ((int64_t)(kt * 8 + wn * NF + j) * a.RT + rt) * 64 + lane);
-    };
-    fetch(rt0, even, even_steps);
-    fetch_codes(rt0);
-    __builtin_amdgcn_s_waitcnt(kWaitVm0);
-    __syncthreads();
-    auto turn = [&](const int rt, const uintx4 *lds, const uintx4 *steps, uintx4 *lds_next, uintx4 *steps_next) __attribute__((always_inline)) {
+    fetch(rt0, lds0);
+    fetch(rt0 + 1, lds1);
+    __builtin_amdgcn_s_waitcnt(wait_loads(0));
+    stage_barrier();
+    auto turn = [&](const int rt, const uintx4 *lds, uintx4 *lds_next) __attribute__((always_inline)) {
+        fetch(rt + 2, lds_next);
         uintx4 w[NF];
 #pragma unroll
-        for (int j = 0; j < NF; ++j) w[j] = codes[j];
-        const int ahead = rt + 1 < rt1 ? rt + 1 : rt;
-        fetch(ahead, lds_next, steps_next);
-        fetch_codes(ahead);
+        for (int j = 0; j < NF; ++j) w[j] = lds[C::XN + (wn * NF + j) * 64 + lane];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             uintx4 B[P][NF];
 #pragma unroll
             for (int j = 0; j < NF; ++j) {
-                const int u = (wn * NF + j) >> 1;      // which of the tile's quarters of 32 columns
-                const uintx4 step = steps[u * 32 + 4 * k + quad], off = steps[u * 32 + 16 + 4 * k + quad];
+                const uintx4 *const steps = lds + C::XN + C::CN + ((wn * NF + j) >> 1) * 32;
+                const uintx4 step = steps[4 * k + quad], off = steps[16 + 4 * k + quad];
                 if constexpr (P == 3) {
                     uintx4 r[3];
                     weights_split(w[j][k], step, off, r);
@@ -259,15 +323,19 @@ __global__ __launch_bounds__(256, 2) void grad_tiles_kernel(Args a, int mtiles, 
                 }
             }
         }
-        __builtin_amdgcn_s_waitcnt(kWaitVm0);
-        __syncthreads();
+        __builtin_amdgcn_s_waitcnt(wait_loads(C::LOADS));      // the next tile is in LDS
+        stage_barrier();
     };
-    for (int rt = rt0;; rt += 2) {
-        turn(rt, even, even_steps, odd, odd_steps);
-        if (rt + 1 >= rt1) break;
-        turn(rt + 1, odd, odd_steps, even, even_steps);
-        if (rt + 2 >= rt1) break;
+    for (int rt = rt0;;) {
+        turn(rt, lds0, lds2);
+        if (++rt >= rt1) break;
+        turn(rt, lds1, lds0);
+        if (++rt >= rt1) break;
+        turn(rt, lds2, lds1);
+        if (++rt >= rt1) break;
     }
+    // (loads behind the last tile still write to LDS: they are waited for before it can be another workgroup's)
+    __builtin_amdgcn_s_waitcnt(wait_loads(0));
 #pragma unroll
     for (int m = 0; m < MF; ++m)
 #pragma unroll
@@ -279,7 +347,7 @@ __global__ __launch_bounds__(256, 2) void grad_tiles_kernel(Args a, int mtiles, 
             for (int j = 0; j < NF; ++j) {
                 const int c = kt * 128 + (wn * NF + j) * 16 + n;
                 if (c >= a.d) continue;
-                const float v = TYPE == OBC_BF16 ? acc[m][j][i] * back : acc[m][j][i];
+                const float v = acc[m][j][i] * back;
                 if (a.slices > 1) a.part[((int64_t)slice * a.T + t) * a.d + c] = v;
                 else store_as<TYPE>(a.dx, (int64_t)t * a.lddx + c, v);
             }
@@ -299,7 +367,7 @@ __global__ __launch_bounds__(256) void grad_add_kernel(Args a)
 
 // ---- host ---------------------------------------------------------------------------------------------------------
 struct Plan {
-    int BM, mtiles, slices, per, RT;
+    int BM, BN, mtiles, ntiles, slices, per, RT;
     size_t rows, back, turned, steps, part, bytes;
 };
 
@@ -307,11 +375,18 @@ Plan plan_of(const pack4_layout &L, int T, int type)
 {
     Plan p;
     p.RT = L.R / 128 + (L.R % 128 != 0);
-    p.BM = T <= 32 ? 32 : type == OBC_F32 ? 64 : 128;
-    p.mtiles = T / p.BM + (T % p.BM != 0);
-    // two workgroups to a compute unit, two row tiles at least to a slice
-    const int64_t tiles = (int64_t)p.mtiles * L.KT;
-    int64_t s = tiles > 0 ? 512 / tiles : 1;
+    auto cut = [&](int BM, int BN) {
+        p.BM = BM;
+        p.BN = BN;
+        p.mtiles = T / BM + (T % BM != 0);
+        p.ntiles = BN == 256 ? (L.KT + 1) / 2 : L.KT;
+        return (int64_t)p.mtiles * p.ntiles;
+    };
+    int64_t tiles = 0;
+    if (T <= 32 || type == OBC_F32) tiles = cut(32, 128);
+    else if (T <= 64 || (tiles = cut(128, 256)) < 192) tiles = cut(64, 128);
+    // two workgroups to a compute unit (fp32, whose planes leave room for one: one), two row tiles at least to a slice
+    int64_t s = p.BM < 128 && tiles > 0 ? (type == OBC_F32 ? 256 : 512) / tiles : 1;
     if (s > p.RT / 2) s = p.RT / 2;
     if (s < 1) s = 1;
     p.per = (int)((p.RT + s - 1) / s);
@@ -331,13 +406,16 @@ template <int TYPE>
 int launch(obc_ctx *ctx, Args a, const Plan &p)
 {
     const int64_t turns = (int64_t)a.KT * a.RT, scale_blocks = ((int64_t)a.NG * a.RT * 128 + 255) / 256;
-    const int64_t lay = turns + scale_blocks + a.T, tiles = (int64_t)p.mtiles * a.KT * p.slices, adds = ((int64_t)a.T * a.d + 255) / 256;
+    const int64_t lay = turns + scale_blocks + a.T, tiles = (int64_t)p.mtiles * p.ntiles * p.slices, adds = ((int64_t)a.T * a.d + 255) / 256;
     if (lay > 0x7fffffff || tiles > 0x7fffffff || (p.slices > 1 && adds > 0x7fffffff))
         return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_product4_grad: too many tiles");
     grad_lay_kernel<TYPE><<<(unsigned)lay, 256, 0, ctx->stream>>>(a, turns, scale_blocks);
     OBC_LAUNCH_CHECK(ctx, "grad_lay_kernel");
-    if (p.BM == 32) grad_tiles_kernel<TYPE, 32, 1><<<(unsigned)tiles, 256, 0, ctx->stream>>>(a, p.mtiles, a.KT);
-    else grad_tiles_kernel<TYPE, TYPE == OBC_F32 ? 64 : 128, 2><<<(unsigned)tiles, 256, 0, ctx->stream>>>(a, p.mtiles, a.KT);
+    if (p.BM == 32) grad_tiles_kernel<TYPE, 32, 128, 1><<<(unsigned)tiles, 256, 0, ctx->stream>>>(a, p.mtiles, p.ntiles);
+    else if constexpr (TYPE != OBC_F32) {
+        if (p.BM == 64) grad_tiles_kernel<TYPE, 64, 128, 1><<<(unsigned)tiles, 256, 0, ctx->stream>>>(a, p.mtiles, p.ntiles);
+        else grad_tiles_kernel<TYPE, 128, 256, 2><<<(unsigned)tiles, 512, 0, ctx->stream>>>(a, p.mtiles, p.ntiles);
+    }
     OBC_LAUNCH_CHECK(ctx, "grad_tiles_kernel");
     if (p.slices > 1) {
         grad_add_kernel<TYPE><<<(unsigned)adds, 256, 0, ctx->stream>>>(a);

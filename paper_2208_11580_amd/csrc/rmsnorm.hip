@@ -60,6 +60,42 @@ __device__ inline void store8(void *p, int64_t at, int left, const float (&v)[8]
     }
 }
 
+// Eight elements on their way, in their own type
+template <int TYPE>
+struct Eight {
+    uintx4 v[TYPE == OBC_F32 ? 2 : 1];
+
+    __device__ void load(const void *p, int64_t at, int left)
+    {
+        if (left >= 8) {
+            if (TYPE == OBC_F32) {
+                v[0] = __builtin_bit_cast(uintx4, (floatx4) * (const floatx4_at4 *)((const float *)p + at));
+                v[TYPE == OBC_F32] = __builtin_bit_cast(uintx4, (floatx4) * (const floatx4_at4 *)((const float *)p + at + 4));
+            } else {
+                v[0] = *(const uintx4_at2 *)((const unsigned short *)p + at);
+            }
+            return;
+        }
+        unsigned e[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            e[j] = j >= left ? 0u : TYPE == OBC_F32 ? ((const unsigned *)p)[at + j] : ((const unsigned short *)p)[at + j];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[0][j] = TYPE == OBC_F32 ? e[j] : e[2 * j] | e[2 * j + 1] << 16;
+            if (TYPE == OBC_F32) v[TYPE == OBC_F32][j] = e[4 + j];
+        }
+    }
+    __device__ void get(float (&f)[8]) const
+    {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const unsigned w = TYPE == OBC_F32 ? v[j >> 2][j & 3] : v[0][j >> 1];
+            f[j] = TYPE == OBC_F32 ? __builtin_bit_cast(float, w) : TYPE == OBC_F16 ? (j & 1 ? half_hi(w) : half_lo(w)) : (j & 1 ? bf16_hi(w) : bf16_lo(w));
+        }
+    }
+};
+
 // Sum (and maximum) over a workgroup, the same value in every thread.
 template <int NT, bool MAX>
 __device__ inline void reduce(float &sum, float &top, float (*buf)[2])
@@ -172,35 +208,46 @@ struct GradArgs {
     int T, d;
 };
 
-// Workgroup b takes the rows b, b + gridDim.x, ... and keeps its columns' share of dgain in registers.
+// Workgroup b takes the rows b, b + gridDim.x, ... and keeps its columns' share of dgain in registers; the next row's
+// loads are on their way while it reduces this one.
 template <int TYPE, int NT, int CH>
 __global__ __launch_bounds__(NT) void rmsnorm_grad_kernel(GradArgs a)
 {
     __shared__ float buf[2][NT / 64][2];
-    float dg[CH][8];
+    float dg[CH][8], gain[CH][8];
+    Eight<TYPE> h[CH], dy[CH];
+    const int tid = threadIdx.x;
 #pragma unroll
-    for (int k = 0; k < CH; ++k)
+    for (int k = 0; k < CH; ++k) {
+        const int c = (k * NT + tid) * 8, left = a.d - c;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) dg[k][j] = 0.f;
+        for (int j = 0; j < 8; ++j) dg[k][j] = gain[k][j] = 0.f;
+        if (left <= 0) continue;
+        load8<OBC_F32>(a.gain, c, left, gain[k]);
+        h[k].load(a.h, (int64_t)blockIdx.x * a.d + c, left);
+        dy[k].load(a.dy, (int64_t)blockIdx.x * a.d + c, left);
+    }
     int turn = 0;
     for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x, turn ^= 1) {
-        const int64_t base = row * a.d;
+        const int64_t base = row * a.d, next = row + gridDim.x < a.T ? base + (int64_t)gridDim.x * a.d : base;
         const float rstd = a.rstd[row];
+        Eight<TYPE> dh[CH];
         float x[CH][8], g[CH][8];
         float sum = 0.f, none = 0.f;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            const int c = (k * NT + (int)threadIdx.x) * 8, left = a.d - c;
+            const int c = (k * NT + tid) * 8, left = a.d - c;
             if (left <= 0) continue;
-            load8<TYPE>(a.h, base + c, left, x[k]);
-            load8<TYPE>(a.dy, base + c, left, g[k]);
-            float w[8];
-            load8<OBC_F32>(a.gain, c, left, w);
+            h[k].get(x[k]);
+            dy[k].get(g[k]);
+            if (a.dh) dh[k].load(a.dh, base + c, left);
+            h[k].load(a.h, next + c, left);
+            dy[k].load(a.dy, next + c, left);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 x[k][j] *= rstd;
                 dg[k][j] = fmaf(g[k][j], x[k][j], dg[k][j]);
-                g[k][j] *= w[j];
+                g[k][j] *= gain[k][j];
                 sum = fmaf(g[k][j], x[k][j], sum);
             }
         }
@@ -208,12 +255,12 @@ __global__ __launch_bounds__(NT) void rmsnorm_grad_kernel(GradArgs a)
         const float mean = sum / (float)a.d;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            const int c = (k * NT + (int)threadIdx.x) * 8, left = a.d - c;
+            const int c = (k * NT + tid) * 8, left = a.d - c;
             if (left <= 0) continue;
             float r[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) r[j] = 0.f;
-            if (a.dh) load8<TYPE>(a.dh, base + c, left, r);
+            if (a.dh) dh[k].get(r);
 #pragma unroll
             for (int j = 0; j < 8; ++j) r[j] = fmaf(rstd, fmaf(-x[k][j], mean, g[k][j]), r[j]);
             store8<TYPE>(a.dx, base + c, left, r);
@@ -221,27 +268,33 @@ __global__ __launch_bounds__(NT) void rmsnorm_grad_kernel(GradArgs a)
     }
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-        const int c = (k * NT + (int)threadIdx.x) * 8, left = a.d - c;
+        const int c = (k * NT + tid) * 8, left = a.d - c;
         if (left > 0) store8<OBC_F32>(a.part, (int64_t)blockIdx.x * a.d + c, left, dg[k]);
     }
 }
 
-// dgain[c] = sum of the workgroups' shares, in their order; 64 columns to a workgroup of 16 waves
+// dgain[c] = sum of the workgroups' shares, in a fixed order; 64 columns to a workgroup of 16 waves
 __global__ __launch_bounds__(1024) void rmsnorm_dgain_kernel(const float *__restrict__ part, int parts, int d,
                                                              float *__restrict__ dgain)
 {
     __shared__ float buf[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int c = blockIdx.x * 64 + lane;
-    float s = 0.f;
-    if (c < d)
-        for (int p = wave; p < parts; p += 16) s += part[(int64_t)p * d + c];
-    buf[wave][lane] = s;
+    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (c < d) {
+        int p = wave;
+        for (; p + 7 * 16 < parts; p += 8 * 16)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[i] += part[(int64_t)(p + i * 16) * d + c];
+        for (; p < parts; p += 16) s[0] += part[(int64_t)p * d + c];
+    }
+    buf[wave][lane] = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
     __syncthreads();
     if (wave == 0 && c < d) {
+        float v = buf[0][lane];
 #pragma unroll
-        for (int w = 1; w < 16; ++w) s += buf[w][lane];
-        dgain[c] = s;
+        for (int w = 1; w < 16; ++w) v += buf[w][lane];
+        dgain[c] = v;
     }
 }
 
@@ -262,8 +315,8 @@ void launch_grad(obc_ctx *ctx, const GradArgs &a)
 {
     const int blocks = grad_parts(a.T);
     if (a.d <= 2048) rmsnorm_grad_kernel<TYPE, 256, 1><<<blocks, 256, 0, ctx->stream>>>(a);
-    else if (a.d <= 4096) rmsnorm_grad_kernel<TYPE, 256, 2><<<blocks, 256, 0, ctx->stream>>>(a);
-    else if (a.d <= 8192) rmsnorm_grad_kernel<TYPE, 512, 2><<<blocks, 512, 0, ctx->stream>>>(a);
+    else if (a.d <= 4096) rmsnorm_grad_kernel<TYPE, 512, 1><<<blocks, 512, 0, ctx->stream>>>(a);
+    else if (a.d <= 8192) rmsnorm_grad_kernel<TYPE, 1024, 1><<<blocks, 1024, 0, ctx->stream>>>(a);
     else if (a.d <= 16384) rmsnorm_grad_kernel<TYPE, 1024, 2><<<blocks, 1024, 0, ctx->stream>>>(a);
     else rmsnorm_grad_kernel<TYPE, 1024, 8><<<blocks, 1024, 0, ctx->stream>>>(a);
 }
