@@ -152,21 +152,22 @@ def _type_of(t, what, i8=False):
     return code
 
 
-def _rows_of(t, what, shape=None):
-    """Address and leading dimension of a device matrix whose rows are contiguous."""
+def _rows_of(t, what):
+    """Address, leading dimension and shape of a device matrix whose rows are contiguous."""
     if not t.is_cuda:
         raise ValueError("libobc takes device tensors")
-    if t.dim() != 2:
+    shape = t.shape
+    if len(shape) != 2:
         raise ValueError("%s must be a matrix" % what)
-    if shape is not None and tuple(t.shape) != shape:
-        raise ValueError("%s must be %d x %d, got %s" % (what, shape[0], shape[1], tuple(t.shape)))
-    rows, cols = t.shape
-    ld = t.stride(0)
-    if rows <= 1:
-        ld = max(ld, cols)
-    if (cols > 1 and t.stride(1) != 1) or ld < cols:
-        raise ValueError("%s must have unit stride along its rows, and rows that do not overlap" % what)
-    return t.data_ptr(), ld
+    rows, cols = shape
+    ld, step = t.stride()
+    if ld < cols:
+        if rows > 1:
+            raise ValueError("%s must have rows that do not overlap" % what)
+        ld = cols
+    if step != 1 and cols > 1:
+        raise ValueError("%s must have unit stride along its rows" % what)
+    return t.data_ptr(), ld, rows, cols
 
 
 def _vector(t, n, what):
@@ -497,33 +498,39 @@ class Context:
     def obc_product4(self, W, x, x_scale=None, out=None, out_dtype=None):
         """y = x W^T (T x rows) of a Packed4.  x: T x cols, fp32, fp16, bf16, or int8 with its scales (T).  y has
         out's type, else out_dtype, else x's (int8: bf16)."""
+        data, R, cols, group = W
         xt = _type_of(x, "x", i8=True)
-        xp, ldx = _rows_of(x, "x")
-        T, d = x.shape
-        if d != W.cols:
-            raise ValueError("x has %d columns, the weights %d" % (d, W.cols))
+        xp, ldx, T, d = _rows_of(x, "x")
+        if d != cols:
+            raise ValueError("x has %d columns, the weights %d" % (d, cols))
         if out is None:
             if out_dtype is None:
                 out_dtype = torch.bfloat16 if xt == I8 else x.dtype
-            out = self._empty((T, W.rows), out_dtype, x.device)
-        yp, ldy = _rows_of(out, "out", (T, W.rows))
-        ws, n = self._need("obc_product4_workspace_bytes", T, W.rows, d, W.group, xt)
-        self._ck(self.lib.obc_product4(self.h, W.data.data_ptr(), W.rows, d, W.group, xp, xt, _vector(x_scale, T, "x_scale"),
-                                       T, ldx, yp, _type_of(out, "out"), ldy, ws, n))
+            out = self._empty((T, R), out_dtype, x.device)
+        yp, ldy, rows, n = _rows_of(out, "out")
+        if rows != T or n != R:
+            raise ValueError("out must be %d x %d" % (T, R))
+        ws, n = self._need("obc_product4_workspace_bytes", T, R, d, group, xt)
+        rc = self.lib.obc_product4(self.h, data.data_ptr(), R, d, group, xp, xt,
+                                   None if x_scale is None else _vector(x_scale, T, "x_scale"), T, ldx, yp, _type_of(out, "out"),
+                                   ldy, ws, n)
+        if rc != OBC_OK:
+            self._ck(rc)
         return out
 
     def obc_product4_grad(self, W, dy, out=None):
         """dx = dy W (T x cols), the gradient of obc_product4's inputs, in dy's type."""
         t = _type_of(dy, "dy")
-        dp, lddy = _rows_of(dy, "dy")
-        T, R = dy.shape
+        dp, lddy, T, R = _rows_of(dy, "dy")
         if R != W.rows:
             raise ValueError("dy has %d columns, the weights %d rows" % (R, W.rows))
         if out is None:
             out = self._empty((T, W.cols), dy.dtype, dy.device)
         if out.dtype != dy.dtype:
             raise ValueError("out must have dy's type")
-        xp, lddx = _rows_of(out, "out", (T, W.cols))
+        xp, lddx, rows, n = _rows_of(out, "out")
+        if rows != T or n != W.cols:
+            raise ValueError("out must be %d x %d" % (T, W.cols))
         ws, n = self._need("obc_product4_grad_workspace_bytes", T, R, W.cols, W.group, t)
         self._ck(self.lib.obc_product4_grad(self.h, W.data.data_ptr(), R, W.cols, W.group, dp, t, T, lddy, xp, lddx, ws, n))
         return out
@@ -578,8 +585,7 @@ class Context:
         """Distillation loss (T) of logits z (T x V) against a teacher's top logits (T x k), and the gradient dz with
         want_grad; out may hold loss and dz (z itself, to overwrite the logits)."""
         t = _type_of(z, "z")
-        zp, ldz = _rows_of(z, "z")
-        T, V = z.shape
+        zp, ldz, T, V = _rows_of(z, "z")
         out = {} if out is None else out
         loss = out.get("loss")
         if loss is None:
@@ -591,7 +597,9 @@ class Context:
         if dz is not None:
             if dz.dtype != z.dtype:
                 raise ValueError("dz must have z's type")
-            gp, ldg = _rows_of(dz, "dz", (T, V))
+            gp, ldg, rows, n = _rows_of(dz, "dz")
+            if rows != T or n != V:
+                raise ValueError("dz must be %d x %d" % (T, V))
         if top_index.shape != top_logit.shape or top_index.dim() != 2 or top_index.shape[0] != T:
             raise ValueError("top_index and top_logit must be T x k")
         k = top_index.shape[1]

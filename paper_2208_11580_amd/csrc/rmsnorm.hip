@@ -273,6 +273,60 @@ __global__ __launch_bounds__(NT) void rmsnorm_grad_kernel(GradArgs a)
     }
 }
 
+// Rows too wide for registers beside their share of dgain: read a second time, from the caches.
+template <int TYPE>
+__global__ __launch_bounds__(1024) void rmsnorm_grad_wide_kernel(GradArgs a)
+{
+    constexpr int NT = 1024, CH = kMaxCols / (NT * 8);
+    __shared__ float buf[2][NT / 64][2];
+    float dg[CH][8];
+#pragma unroll
+    for (int k = 0; k < CH; ++k)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dg[k][j] = 0.f;
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x, turn ^= 1) {
+        const int64_t base = row * a.d;
+        const float rstd = a.rstd[row];
+        float sum = 0.f, none = 0.f;
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            const int c = (k * NT + (int)threadIdx.x) * 8, left = a.d - c;
+            if (left <= 0) continue;
+            float x[8], g[8], w[8];
+            load8<TYPE>(a.h, base + c, left, x);
+            load8<TYPE>(a.dy, base + c, left, g);
+            load8<OBC_F32>(a.gain, c, left, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float t = g[j] * (x[j] * rstd);
+                dg[k][j] += t;
+                sum = fmaf(w[j], t, sum);
+            }
+        }
+        reduce<NT, false>(sum, none, buf[turn]);
+        const float mean = sum / (float)a.d;
+        for (int c = threadIdx.x * 8; c < a.d; c += NT * 8) {
+            const int left = a.d - c;
+            float x[8], g[8], w[8], r[8];
+            load8<TYPE>(a.h, base + c, left, x);
+            load8<TYPE>(a.dy, base + c, left, g);
+            load8<OBC_F32>(a.gain, c, left, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) r[j] = 0.f;
+            if (a.dh) load8<TYPE>(a.dh, base + c, left, r);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) r[j] = fmaf(rstd, fmaf(-x[j] * rstd, mean, g[j] * w[j]), r[j]);
+            store8<TYPE>(a.dx, base + c, left, r);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+        const int c = (k * NT + (int)threadIdx.x) * 8, left = a.d - c;
+        if (left > 0) store8<OBC_F32>(a.part, (int64_t)blockIdx.x * a.d + c, left, dg[k]);
+    }
+}
+
 // dgain[c] = sum of the workgroups' shares, in a fixed order; 64 columns to a workgroup of 16 waves
 __global__ __launch_bounds__(1024) void rmsnorm_dgain_kernel(const float *__restrict__ part, int parts, int d,
                                                              float *__restrict__ dgain)
@@ -317,8 +371,8 @@ void launch_grad(obc_ctx *ctx, const GradArgs &a)
     if (a.d <= 2048) rmsnorm_grad_kernel<TYPE, 256, 1><<<blocks, 256, 0, ctx->stream>>>(a);
     else if (a.d <= 4096) rmsnorm_grad_kernel<TYPE, 512, 1><<<blocks, 512, 0, ctx->stream>>>(a);
     else if (a.d <= 8192) rmsnorm_grad_kernel<TYPE, 1024, 1><<<blocks, 1024, 0, ctx->stream>>>(a);
-    else if (a.d <= 16384) rmsnorm_grad_kernel<TYPE, 1024, 2><<<blocks, 1024, 0, ctx->stream>>>(a);
-    else rmsnorm_grad_kernel<TYPE, 1024, 8><<<blocks, 1024, 0, ctx->stream>>>(a);
+    else if (a.d <= 16384 && TYPE != OBC_F32) rmsnorm_grad_kernel<TYPE == OBC_F32 ? OBC_BF16 : TYPE, 1024, 2><<<blocks, 1024, 0, ctx->stream>>>(a);
+    else rmsnorm_grad_wide_kernel<TYPE><<<blocks, 1024, 0, ctx->stream>>>(a);
 }
 
 }  // namespace
