@@ -151,6 +151,14 @@ struct Sum<OBC_I8> {
     __device__ float operator[](int i) const { return (float)s[i]; }
 };
 
+// What a token's pieces are exchanged by in LDS, so that the 16 tokens of an operand lie in different banks: rows of 16 pieces
+// are as long as the 64 banks, rows of 8 (8-bit inputs) half as long.
+template <int ROW>
+__device__ inline int turned(int t)
+{
+    return ROW == 16 ? t & 15 : (t >> 1) & 7;
+}
+
 // ---- few tokens ------------------------------------------------------------------------------
 constexpr int kRowsTokens = 16;
 constexpr int kRowsLds = 147456;     // of a compute unit, for its workgroups' tokens
@@ -205,8 +213,8 @@ __global__ __launch_bounds__(rows_waves(XT) * 64) void product4_rows_kernel(Args
             }
         }
     };
-    // Operand o (step k, quad) of token t and tile i of the chunk, at place o ^ (t mod 16) of its row; 8-bit inputs: 8 bytes
-    auto place = [&](int i, int p, int t, int o) { return ((i * P + p) * a.T + t) * OPS + (XT == OBC_I8 ? o >> 1 : o ^ (t & 15)); };
+    // Operand o (step k, quad) of token t and tile i of the chunk; 8-bit inputs: 8 bytes
+    auto place = [&](int i, int p, int t, int o) { return ((i * P + p) * a.T + t) * OPS + ((XT == OBC_I8 ? o >> 1 : o) ^ turned<OPS>(t)); };
     auto put = [&](const Operand<XT> &x, int i, int t, int o) {
         if constexpr (XT == OBC_F32) {
 #pragma unroll
@@ -435,14 +443,14 @@ __global__ __launch_bounds__(tile_waves(BN) * 64, 2) void product4_tiles_kernel(
 
     // where this lane's loads come from, at the slice's first tile
     const char *xsrc[C::XL], *wsrc[C::WL], *ssrc[C::SL];
-    // Piece o of token t lies at place o ^ (t mod ROW) of its row, so that the 16 tokens of an operand lie in different
-    // banks.  The lanes of a load to LDS write 64 places in a row: each fetches the piece that belongs to its place.
+    // Piece o of token t lies at place o ^ turned(t) of its row.  The lanes of a load to LDS write 64 places in a row: each
+    // fetches the piece that belongs to its place.
 #pragma unroll
     for (int i = 0; i < C::XL; ++i) {
         const int first = (i * C::WAVES + wave) * (64 / ROW);      // row of the planes, one below the other
         const int p = P > 1 ? first / BM : 0, t = first - p * BM + lane / ROW;
         const int row = t0 + t < a.T ? t0 + t : a.T - 1;
-        xsrc[i] = tok.x + p * tok.plane + row * tok.ld + (int64_t)kt0 * (ROW * 16) + ((lane % ROW) ^ (t % ROW)) * 16;
+        xsrc[i] = tok.x + p * tok.plane + row * tok.ld + (int64_t)kt0 * (ROW * 16) + ((lane % ROW) ^ turned<ROW>(t)) * 16;
     }
 #pragma unroll
     for (int i = 0; i < C::WL; ++i) wsrc[i] = (const char *)a.codes + (row_block(i * C::WAVES + wave) * a.KT + kt0) * 1024 + lane * 16;
@@ -542,7 +550,7 @@ __global__ __launch_bounds__(tile_waves(BN) * 64, 2) void product4_tiles_kernel(
                 // eight columns of step k in the codes' order
                 auto operand = [&](int m, int k) {
                     const int e = 4 * k + quad;
-                    return bytes_like_codes(((const uintx2 *)lds)[((16 * (wm * MF + m) + n) * ROW + ((e >> 1) ^ (n & (ROW - 1)))) * 2 + (e & 1)]);
+                    return bytes_like_codes(((const uintx2 *)lds)[((16 * (wm * MF + m) + n) * ROW + ((e >> 1) ^ turned<ROW>(n))) * 2 + (e & 1)]);
                 };
                 if constexpr (SUB == 4) {
                     uintx2 B[NF];
@@ -596,7 +604,7 @@ __global__ __launch_bounds__(tile_waves(BN) * 64, 2) void product4_tiles_kernel(
                     for (int m = 0; m < MF; ++m)
 #pragma unroll
                         for (int p = P - 1; p >= 0; --p) {
-                            const uintx4 A = lds[(p * BM + 16 * (wm * MF + m) + n) * ROW + ((4 * k + quad) ^ n)];
+                            const uintx4 A = lds[(p * BM + 16 * (wm * MF + m) + n) * ROW + ((4 * k + quad) ^ turned<ROW>(n))];
 #pragma unroll
                             for (int j = 0; j < NF; ++j) S[m][j] = XT == OBC_F16 ? mfma_f16(A, B[j], S[m][j]) : mfma_bf16(A, B[j], S[m][j]);
                         }
