@@ -69,7 +69,8 @@ const char *obc_last_error(const obc_ctx *ctx);
 const char *obc_version(void);
 
 /* Wait for the context's stream and return the first error a kernel latched since the last
- * obc_check (OBC_ERR_NUMERIC, OBC_ERR_NOT_SPD) or OBC_OK; clears the latch. */
+ * obc_check (OBC_ERR_NUMERIC, OBC_ERR_NOT_SPD; OBC_ERR_BAD_ARG from obc_pack4 and obc_distill) or
+ * OBC_OK; clears the latch. */
 int obc_check(obc_ctx *ctx);
 
 /* ---- Measurement support (not part of the method) ---------------------------------------
@@ -320,9 +321,10 @@ int obc_pack4(obc_ctx *ctx, const int32_t *codes, const float *delta, const floa
  *   x   T x d, leading dimension ldx >= d, of x_type; OBC_I8: x stands for x_scale[t] * x[t, c]
  *       (x_scale: T fp32; null for the other types)
  *   y   T x R, leading dimension ldy >= R, of y_type (OBC_F32, OBC_F16 or OBC_BF16)
- * Products and sums have the precision of fp32 (OBC_I8: integer sums, exact) and are rounded once, to y's
- * type.  Rows need no alignment beyond their elements'.  Fixed summation order for a given T, R, d and group.
- * A non-finite input makes its token's outputs non-finite (inf or NaN).  y may not overlap x. */
+ * Products and sums have the precision of fp32 (OBC_I8: integer sums within a group, exact) and are rounded once, to
+ * y's type.  Rows need no alignment beyond their elements'.  Fixed summation order for a given T, R, d and group.
+ * A non-finite input makes its token's outputs non-finite (inf or NaN).  y may not overlap x.
+ * ws: obc_product4_workspace_bytes for this T (0 up to 16 tokens, but for few rows of many columns). */
 int obc_product4_workspace_bytes(int T, int R, int d, int group, int x_type, size_t *bytes);
 int obc_product4(obc_ctx *ctx, const void *packed, int R, int d, int group, const void *x, int x_type,
                  const float *x_scale, int T, int64_t ldx, void *y, int y_type, int64_t ldy, void *ws,
@@ -331,8 +333,10 @@ int obc_product4(obc_ctx *ctx, const void *packed, int R, int d, int group, cons
 /* dx = dy W for T tokens, the gradient of obc_product4's inputs: dx[t, c] = sum_r dy[t, r] W[r, c].
  *   dy  T x R, leading dimension lddy >= R;  dx  T x d, leading dimension lddx >= d; both of `type`
  *       (OBC_F32, OBC_F16 or OBC_BF16)
- * 16-bit types: weights rounded to the type (the steps differ along the sum, so they cannot be taken out of
- * it), products and sums fp32, one rounding of the result.  OBC_F32: the precision of fp32 throughout. */
+ * 16-bit types: weights rounded to half precision (the steps differ along the sum, so they cannot be taken out
+ * of it; a weight beyond 65504 becomes an infinity), products and sums fp32, one rounding of the result.
+ * OBC_F32: the precision of fp32 throughout.  Fixed summation order for a given T, R, d and group.  A non-finite dy makes
+ * its token's outputs non-finite.  dx may not overlap dy. */
 int obc_product4_grad_workspace_bytes(int T, int R, int d, int group, int type, size_t *bytes);
 int obc_product4_grad(obc_ctx *ctx, const void *packed, int R, int d, int group, const void *dy, int type, int T,
                       int64_t lddy, void *dx, int64_t lddx, void *ws, size_t ws_bytes);
@@ -345,7 +349,7 @@ int obc_product4_grad(obc_ctx *ctx, const void *packed, int R, int d, int group,
  *   y        T x d of y_type: x_type or OBC_I8; OBC_I8: y stands for y_scale[t] * y[t, c], y_scale[t] =
  *            max|y| / 127 (1 for a row of zeros; NaN, and codes 0, for a row with a NaN or an infinity)
  *   y_scale  T fp32 out, with OBC_I8;  rstd  nullable, T fp32 out: 1 / sqrt(mean(h^2) + eps)
- * 1 <= d <= 65536. */
+ * Squares are summed in fp32.  1 <= d <= 65536. */
 int obc_rmsnorm(obc_ctx *ctx, const void *x, const void *residual, int x_type, const float *gain, float eps, int T,
                 int d, void *h, void *y, int y_type, float *y_scale, float *rstd);
 

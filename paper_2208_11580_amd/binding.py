@@ -462,7 +462,11 @@ class Context:
             n = self._needs[key] = need.value
         if n == 0:
             return None, 0
-        ws = self.workspace(n)
+        ws = self._ws
+        if ws is None or ws.numel() < n:
+            # like the outputs: memory that the current stream may still use is not for the context's
+            with torch.cuda.stream(self.stream):
+                ws = self.workspace(n)
         return ws.data_ptr(), ws.numel()
 
     def obc_group_grid(self, W, bits=4, group=0, live=None, symmetric=False, zero=False):

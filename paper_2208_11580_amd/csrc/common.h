@@ -99,6 +99,9 @@ static inline int obc_fail(obc_ctx *ctx, int code, const char *fmt, ...)
 
 __host__ __device__ static inline size_t obc_align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
+// A launch holds fewer than 2^32 threads.
+static inline bool obc_grid_fits(int64_t blocks, int threads) { return blocks >= 0 && blocks * threads < ((int64_t)1 << 32); }
+
 // Latch the first error seen by any kernel (device side).
 __device__ static inline void obc_latch(int *status, int code)
 {

@@ -93,8 +93,9 @@ int obc_check(obc_ctx *ctx)
         OBC_HIP(ctx, hipMemsetAsync(ctx->d_status, 0, sizeof(int), ctx->stream));
         OBC_HIP(ctx, hipStreamSynchronize(ctx->stream));
         return obc_fail(ctx, h, "a kernel reported error %d (%s)", h,
-                        h == OBC_ERR_NUMERIC   ? "non-positive or non-finite pivot in a row solver"
+                        h == OBC_ERR_NUMERIC   ? "non-positive or non-finite pivot in a row solver, or a grid beyond half precision"
                         : h == OBC_ERR_NOT_SPD ? "matrix is not positive definite"
+                        : h == OBC_ERR_BAD_ARG ? "a code or an index out of range"
                                                : "unknown");
     }
     return OBC_OK;

@@ -401,6 +401,7 @@ int obc_distill(obc_ctx *ctx, const void *z, int type, int T, int V, int64_t ldz
     if (!z || !loss || (k > 0 && (!top_index || !top_logit))) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_distill: null argument");
     if ((((uintptr_t)z | (uintptr_t)dz) & (size_of_type(type) - 1)) != 0)
         return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_distill: z or dz is not aligned to its elements");
+    if (!obc_grid_fits(T, 1024)) return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_distill: too many rows");
     const Args a = {z, top_index, top_logit, weight, loss, dz, T, V, k, ldz, lddz, temperature, ctx->d_status};
     if (type == OBC_F32) launch<OBC_F32>(ctx, a);
     else if (type == OBC_F16) launch<OBC_F16>(ctx, a);

@@ -165,7 +165,7 @@ int obc_group_grid(obc_ctx *ctx, const float *W, const uint8_t *live, int R, int
     if (R == 0) return OBC_OK;
     if (!W || !delta || !offset) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_group_grid: null argument");
     const int64_t jobs = (int64_t)R * L.NG, blocks = (jobs + 3) / 4;
-    if (blocks > 0x7fffffff) return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_group_grid: too many groups");
+    if (!obc_grid_fits(blocks, 256)) return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_group_grid: too many groups");
     const int G = L.NG == 1 ? d : group;
     group_grid_kernel<<<(unsigned)blocks, 256, 0, ctx->stream>>>(W, live, jobs, d, G, L.NG, maxq, flags, delta, offset,
                                                                  ctx->d_status);
@@ -194,7 +194,7 @@ int obc_pack4(obc_ctx *ctx, const int32_t *codes, const float *delta, const floa
     if (((uintptr_t)packed & 15) != 0) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_pack4: packed is not aligned to 16 bytes");
     const int per_row = L.SUB > 1 ? L.KT * L.SUB : L.NG;
     const int64_t tiles = (int64_t)L.RB * L.KT, entries = (int64_t)L.RB * 16 * per_row;
-    if (tiles > 0x7fffffff || (entries + 255) / 256 > 0x7fffffff)
+    if (!obc_grid_fits(tiles, 256) || !obc_grid_fits((entries + 255) / 256, 256))
         return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_pack4: too many tiles");
     const int G = L.NG == 1 ? d : group;
     pack4_codes_kernel<<<(unsigned)tiles, 256, 0, ctx->stream>>>(codes, delta, offset, L, G, (unsigned *)packed, ctx->d_status);

@@ -778,7 +778,7 @@ int launch(obc_ctx *ctx, const Args &a, int y_type, const Rows *rows, const Plan
     lay.NGP = p.NGP;
     lay.G = SUB > 1 ? 128 / SUB : a.tpg * 128;
     lay.jobs = (int64_t)a.T * a.NG;
-    if (blocks > 0x7fffffff || (p.slices > 1 && adds > 0x7fffffff) || lay.jobs > 0x7fffffff)
+    if (!obc_grid_fits(blocks, tile_waves(p.BN) * 64) || (p.slices > 1 && !obc_grid_fits(adds, 256)) || !obc_grid_fits(lay.jobs, 64))
         return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_product4: too many tiles");
     launch_lay<XT>(ctx, a, lay);
     OBC_LAUNCH_CHECK(ctx, "product4_lay_kernel");

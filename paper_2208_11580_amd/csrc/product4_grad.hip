@@ -415,7 +415,7 @@ int launch(obc_ctx *ctx, Args a, const Plan &p)
 {
     const int64_t turns = (int64_t)a.KT * a.RT, scale_blocks = ((int64_t)a.NG * a.RT * 128 + 255) / 256;
     const int64_t lay = turns + scale_blocks + a.T, tiles = (int64_t)p.mtiles * p.ntiles * p.slices, adds = ((int64_t)a.T * a.d + 255) / 256;
-    if (lay > 0x7fffffff || tiles > 0x7fffffff || (p.slices > 1 && adds > 0x7fffffff))
+    if (!obc_grid_fits(lay, 256) || !obc_grid_fits(tiles, p.BN * 2) || (p.slices > 1 && !obc_grid_fits(adds, 256)))
         return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_product4_grad: too many tiles");
     grad_lay_kernel<TYPE><<<(unsigned)lay, 256, 0, ctx->stream>>>(a, turns, scale_blocks);
     OBC_LAUNCH_CHECK(ctx, "grad_lay_kernel");
@@ -468,7 +468,7 @@ int obc_product4_grad(obc_ctx *ctx, const void *packed, int R, int d, int group,
         return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_product4_grad: dy or dx is not aligned to its elements");
     if (R == 0) {
         const int64_t blocks = ((int64_t)T * d + 255) / 256;
-        if (blocks > 0x7fffffff) return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_product4_grad: too many tiles");
+        if (!obc_grid_fits(blocks, 256)) return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_product4_grad: too many tiles");
         grad_zero_kernel<<<(unsigned)blocks, 256, 0, ctx->stream>>>(dx, lddx, T, d, (int)size_of_type(type));
         OBC_LAUNCH_CHECK(ctx, "grad_zero_kernel");
         return OBC_OK;

@@ -394,12 +394,20 @@ int obc_rmsnorm(obc_ctx *ctx, const void *x, const void *residual, int x_type, c
         return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_rmsnorm: y_scale goes with 8-bit outputs");
     if ((((uintptr_t)x | (uintptr_t)residual | (uintptr_t)h | (y_type == OBC_I8 ? 0 : (uintptr_t)y)) & (size_of_type(x_type) - 1)) != 0)
         return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_rmsnorm: an array is not aligned to its elements");
-    const NormArgs a = {x, residual, gain, h, y, y_scale, rstd, eps, T, d};
     const bool q8 = y_type == OBC_I8;
-    if (x_type == OBC_F32) q8 ? launch_norm<OBC_F32, true>(ctx, a) : launch_norm<OBC_F32, false>(ctx, a);
-    else if (x_type == OBC_F16) q8 ? launch_norm<OBC_F16, true>(ctx, a) : launch_norm<OBC_F16, false>(ctx, a);
-    else q8 ? launch_norm<OBC_BF16, true>(ctx, a) : launch_norm<OBC_BF16, false>(ctx, a);
-    OBC_LAUNCH_CHECK(ctx, "rmsnorm_kernel");
+    const size_t in = size_of_type(x_type), out = size_of_type(y_type);
+    constexpr int kMost = 1 << 21;      // rows of a launch
+    for (int t0 = 0; t0 < T; t0 += kMost) {
+        const size_t at = (size_t)t0 * d;
+        const NormArgs a = {(const char *)x + at * in, residual ? (const char *)residual + at * in : nullptr, gain,
+                            h ? (char *)h + at * in : nullptr, (char *)y + at * out, y_scale ? y_scale + t0 : nullptr,
+                            rstd ? rstd + t0 : nullptr, eps, T - t0 < kMost ? T - t0 : kMost, d};
+        if (x_type == OBC_F32) q8 ? launch_norm<OBC_F32, true>(ctx, a) : launch_norm<OBC_F32, false>(ctx, a);
+        else if (x_type == OBC_F16) q8 ? launch_norm<OBC_F16, true>(ctx, a) : launch_norm<OBC_F16, false>(ctx, a);
+        else q8 ? launch_norm<OBC_BF16, true>(ctx, a) : launch_norm<OBC_BF16, false>(ctx, a);
+        OBC_LAUNCH_CHECK(ctx, "rmsnorm_kernel");
+        if (T - t0 <= kMost) break;
+    }
     return OBC_OK;
 }
 
