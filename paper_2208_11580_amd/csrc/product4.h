@@ -129,5 +129,22 @@ __device__ inline int tile_of(int id, int tiles)
     return die * each + (die < left ? die : left) + (id >> 3);
 }
 
+// The sum of an element's slices, n apart, in their order; several loads on their way at a time.
+__device__ inline float add_slices(const float *part, int64_t n, int slices)
+{
+    constexpr int AT = 8;
+    float v = 0.f;
+    int s = 0;
+    for (; s + AT <= slices; s += AT) {
+        float x[AT];
+#pragma unroll
+        for (int i = 0; i < AT; ++i) x[i] = part[(s + i) * n];
+#pragma unroll
+        for (int i = 0; i < AT; ++i) v += x[i];
+    }
+    for (; s < slices; ++s) v += part[s * n];
+    return v;
+}
+
 static inline bool float_type(int type) { return type == OBC_F32 || type == OBC_F16 || type == OBC_BF16; }
 static inline size_t size_of_type(int type) { return type == OBC_F32 ? 4 : type == OBC_I8 ? 1 : 2; }

@@ -662,8 +662,7 @@ __global__ __launch_bounds__(256) void product4_add_kernel(Args a, const float *
 {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, n = (int64_t)a.T * a.R;
     if (i >= n) return;
-    float v = part[i];
-    for (int s = 1; s < slices; ++s) v += part[s * n + i];
+    float v = add_slices(part + i, n, slices);
     const int64_t t = i / a.R;
     if (a.xs) v *= a.xs[t];
     const int64_t at = t * a.ldy + (i - t * a.R);

@@ -365,8 +365,7 @@ __global__ __launch_bounds__(256) void grad_add_kernel(Args a)
 {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, n = (int64_t)a.T * a.d;
     if (i >= n) return;
-    float v = a.part[i];
-    for (int s = 1; s < a.slices; ++s) v += a.part[s * n + i];
+    const float v = add_slices(a.part + i, n, a.slices);
     const int64_t t = i / a.d;
     store_as<TYPE>(a.dx, t * a.lddx + (i - t * a.d), v);
 }
