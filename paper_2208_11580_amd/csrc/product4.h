@@ -48,12 +48,6 @@ __device__ inline uintx2 bytes_like_codes(uintx2 x)
     return uintx2{__builtin_amdgcn_perm(x.y, x.x, 0x05010400u), __builtin_amdgcn_perm(x.y, x.x, 0x07030602u)};
 }
 
-// and back
-__device__ inline uintx2 natural_bytes(uintx2 c)
-{
-    return uintx2{__builtin_amdgcn_perm(c.y, c.x, 0x06040200u), __builtin_amdgcn_perm(c.y, c.x, 0x07050301u)};
-}
-
 __device__ inline float bf16_lo(unsigned w) { return __builtin_bit_cast(float, w << 16); }
 __device__ inline float bf16_hi(unsigned w) { return __builtin_bit_cast(float, w & 0xffff0000u); }
 

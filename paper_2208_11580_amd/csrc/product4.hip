@@ -4,8 +4,14 @@
 //                                                                           s = sum_{c in g} x[t, c]
 // The codes enter the matrix instructions as the 16-bit numbers 16 + code, exactly (8-bit inputs: as bytes, without
 // the 16), so their products with 16-bit inputs are exact in fp32 and the only roundings are those of the fp32 sums; a
-// group's sums start from zero and are scaled when it ends.  fp32 inputs go in as three bf16 terms.  s comes from one
-// more instruction, against ones, in the very lanes that need it.
+// group's sums start from zero and are scaled when it ends.  fp32 inputs go in as three bf16 terms.
+//
+// Up to 16 tokens: bound by the weights' bytes (product4_rows_kernel).  One token through 8192 x 8192 takes 9.2 us in half
+// precision, 35.7 MB at 3.9 TB/s, where the plain read kernel gives 6.3 for buffers out of cache; through 768 x 768 3.3 us, of which
+// 2.4 are a launch.  More tokens: bound by instruction issue beside the matrix cores (product4_tiles_kernel).  2048 tokens through
+// 4096 x 4096 in bf16 take 77 us, 890 TFLOP/s (a dense library product of that size: 61 us, 1120); of the tiles' 72 us the matrix cores are busy 41 %
+// and the vector units 48 %: 64 matrix instructions of a wave and tile come with 64 multiply-adds that scale groups and 128 that
+// unpack codes.  All captured in a graph.
 #include "product4.h"
 
 namespace {
@@ -169,8 +175,8 @@ constexpr int rows_waves(int XT) { return XT == OBC_F32 ? 8 : 16; }
 constexpr int tile_bytes(int XT) { return XT == OBC_F32 ? 768 : XT == OBC_I8 ? 128 : 256; }
 
 // 16 NF rows of W and up to 16 tokens to a workgroup, whose waves take turns along the columns' tiles and sum in LDS.  The
-// weights' bytes bound it: a wave has its next tile's codes on their way (more than one only costs registers and instructions: 16 waves
-// to a compute unit cover the rest).  Loads come back in order, so the tokens must not be among them: they go through LDS, `chunk`
+// weights' bytes bound it: a wave has its next tile's codes on their way (two or three ahead measured slower, 9.9 and 11.3 us against
+// 9.2 for one token through 8192 x 8192: 16 waves to a compute unit cover the rest, and the copies cost instructions).  Loads come back in order, so the tokens must not be among them: they go through LDS, `chunk`
 // tiles at a time.
 template <int XT, int SUB, int NF>
 __global__ __launch_bounds__(rows_waves(XT) * 64) void product4_rows_kernel(Args a, int y_type, int chunk)
@@ -332,13 +338,21 @@ __global__ __launch_bounds__(rows_waves(XT) * 64) void product4_rows_kernel(Args
 // ---- many tokens ------------------------------------------------------------------------------
 // What the tiles' kernel needs beside x: the sums of every token's groups, as three planes of bf16 terms (T x NGP each, zeros
 // from NG on); and, where x is not laid out like that already, the tokens' rows at multiples of 16 bytes with zeros up to a multiple
-// of 128 columns -- fp32 as three planes of bf16 terms.  A team of TEAM lanes to a token and group.
+// of 128 columns -- fp32 as three planes of bf16 terms, 8-bit ones in the order of the operands (i8_place).  A team of TEAM lanes to a
+// token and group.
 struct Lay {
     unsigned short *sums;
     uintx4 *rows;      // null: x as it lies
     int NGP, G;        // groups of a row, padded to 32; columns of a group
     int64_t jobs;      // T x NG
 };
+
+// Where piece p of eight columns of a laid-out 8-bit token lies: the two that a lane of quad q takes for one instruction of 64
+// columns, 8 q and 32 + 8 q on, side by side, bytes in the codes' order.
+__device__ inline int i8_place(int p)
+{
+    return (p & ~7) | (p & 3) << 1 | (p >> 2 & 1);
+}
 
 template <int XT, int TEAM>
 __global__ __launch_bounds__(256) void product4_lay_kernel(Args a, Lay lay)
@@ -364,11 +378,10 @@ __global__ __launch_bounds__(256) void product4_lay_kernel(Args a, Lay lay)
 #pragma unroll
                 for (int q = 0; q < 3; ++q) lay.rows[q * plane + t * pieces + p] = o.v[q];
         } else if constexpr (XT == OBC_I8) {
-            const uintx2 x = natural_bytes(o.v);
-            int s = __builtin_amdgcn_sdot4((int)x.x, 0x01010101, 0, false);
-            s = __builtin_amdgcn_sdot4((int)x.y, 0x01010101, s, false);
+            int s = __builtin_amdgcn_sdot4((int)o.v.x, 0x01010101, 0, false);
+            s = __builtin_amdgcn_sdot4((int)o.v.y, 0x01010101, s, false);
             sum += (float)s;
-            if (lay.rows) ((uintx2 *)lay.rows)[t * pieces + p] = x;
+            ((uintx2 *)lay.rows)[t * pieces + i8_place(p)] = o.v;
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -405,7 +418,11 @@ struct Tokens {
 
 // BM tokens x BN rows of W to a workgroup of WM x WN waves.  Tokens, codes and steps of STAGES column tiles go through LDS in
 // turn, so that loads have STAGES - 1 tiles' time to arrive; a wave waits for all but its newest ones and then for the others.
-// Within a tile the codes are unpacked step by step between the matrix instructions of the step before.
+//
+// 128 x 256 with eight waves of 64 x 64 where that fills the chip: a wave's unpacked codes serve 64 tokens, its tokens 64 rows.  64 x
+// 128 with waves of 64 x 32 otherwise (2048 tokens through 4096 x 4096: 95 us against 79; 1000 in 8 bits through 4096 x 8192, where 128 x
+// 256 would be 128 workgroups or two slices: 106 us against 116).  Waves of 128 x 64, which unpack half as much, are one to a SIMD
+// and took 106 us then; more stages or operands read a step earlier changed nothing.
 constexpr int tile_waves(int BN) { return BN / 32; }
 
 template <int XT, int SUB, int BM, int BN, int WM, int STAGES>
@@ -547,18 +564,15 @@ __global__ __launch_bounds__(tile_waves(BN) * 64, 2) void product4_tiles_kernel(
                 for (int m = 0; m < MF; ++m)
 #pragma unroll
                     for (int j = 0; j < NF; ++j) S[m][j] = intx4{0, 0, 0, 0};
-                // eight columns of step k in the codes' order
-                auto operand = [&](int m, int k) {
-                    const int e = 4 * k + quad;
-                    return bytes_like_codes(((const uintx2 *)lds)[((16 * (wm * MF + m) + n) * ROW + ((e >> 1) ^ turned<ROW>(n))) * 2 + (e & 1)]);
-                };
+                // the lane's columns of 64 (i8_place)
+                auto place = [&](int m, int k) { return (16 * (wm * MF + m) + n) * ROW + ((4 * k + quad) ^ turned<ROW>(n)); };
                 if constexpr (SUB == 4) {
                     uintx2 B[NF];
 #pragma unroll
                     for (int j = 0; j < NF; ++j) B[j] = codes_i8(w[j][u]);
 #pragma unroll
                     for (int m = 0; m < MF; ++m) {
-                        const uintx2 A = operand(m, u);
+                        const uintx2 A = ((const uintx2 *)lds)[2 * place(m, u >> 1) + (u & 1)];
 #pragma unroll
                         for (int j = 0; j < NF; ++j) S[m][j] = mfma_i8(A, B[j], S[m][j]);
                     }
@@ -573,8 +587,7 @@ __global__ __launch_bounds__(tile_waves(BN) * 64, 2) void product4_tiles_kernel(
                         }
 #pragma unroll
                         for (int m = 0; m < MF; ++m) {
-                            const uintx2 lo = operand(m, 2 * k), hi = operand(m, 2 * k + 1);
-                            const intx4 A = {(int)lo.x, (int)lo.y, (int)hi.x, (int)hi.y};
+                            const intx4 A = ((const intx4 *)lds)[place(m, k)];
 #pragma unroll
                             for (int j = 0; j < NF; ++j) S[m][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(A, B[j], S[m][j], 0, 0, 0);
                         }
@@ -674,7 +687,7 @@ __global__ __launch_bounds__(256) void product4_add_kernel(Args a, const float *
 // True where the tiles' kernel can read x as it lies.
 inline bool laid_out(const void *x, int x_type, int64_t ldx, int d)
 {
-    return x_type != OBC_F32 && d % 128 == 0 && ((uintptr_t)x & 15) == 0 && (ldx * (int64_t)size_of_type(x_type)) % 16 == 0;
+    return (x_type == OBC_F16 || x_type == OBC_BF16) && d % 128 == 0 && ((uintptr_t)x & 15) == 0 && (ldx * (int64_t)size_of_type(x_type)) % 16 == 0;
 }
 
 // What a product with more tokens than the rows' kernel takes is cut into, and its workspace.
@@ -697,7 +710,8 @@ Plan plan_of(const pack4_layout &L, int T, int x_type)
     if (x_type == OBC_F32) tiles = T > 32 ? cut(64, 128) : cut(32, 128);
     else if (T <= 32) tiles = cut(32, 128);
     else if (T <= 64 || (tiles = cut(128, 256)) < 192) tiles = cut(64, 128);
-    // two workgroups to a compute unit (fp32 in tiles of 64: one), two tiles at least to a slice
+    // few tokens leave too few tiles for the chip: slices of the columns, two workgroups to a compute unit (fp32 in tiles of 64: one),
+    // two tiles at least to a slice
     int64_t s = p.BM < 128 && tiles > 0 ? (x_type == OBC_F32 && p.BM == 64 ? 256 : 512) / tiles : 1;
     if (s > 16) s = 16;
     if (s > L.KT / 2) s = L.KT / 2;
