@@ -39,6 +39,23 @@ __device__ inline uintx4 codes_f16(unsigned w)
     return uintx4{((w << 6) & mask) | base, ((w << 2) & mask) | base, ((w >> 2) & mask) | base, ((w >> 6) & mask) | base};
 }
 
+// A code q as 2 q - 15, exactly, in the same order: the sums have no large common part to take out again.  q >= 8 is 2 k + 1 and q < 8
+// its opposite with k = (q & 7) or 7 - q, of which two permutes look up both bytes.
+__device__ inline uintx4 codes_centred_bf16(unsigned w)
+{
+    auto four = [](unsigned q, unsigned &first, unsigned &second) {      // a code to a byte
+        const unsigned neg = ~q & 0x08080808u, k = (q ^ (neg - (neg >> 3))) & 0x07070707u;
+        const unsigned hi = __builtin_amdgcn_perm(0x41414141u, 0x4040403fu, k) | (neg << 4);
+        const unsigned lo = __builtin_amdgcn_perm(0x70503010u, 0xe0a04080u, k);
+        first = __builtin_amdgcn_perm(hi, lo, 0x06020400u);
+        second = __builtin_amdgcn_perm(hi, lo, 0x07030501u);
+    };
+    unsigned v0, v1, v2, v3;
+    four(w & 0x0f0f0f0fu, v0, v2);
+    four((w >> 4) & 0x0f0f0f0fu, v1, v3);
+    return uintx4{v0, v1, v2, v3};
+}
+
 // Eight codes as bytes, in the order of the columns 0 4 1 5 2 6 3 7; bytes_like_codes brings eight 8-bit
 // inputs into the same order.
 __device__ inline uintx2 codes_i8(unsigned w) { return uintx2{w & 0x0f0f0f0fu, (w >> 4) & 0x0f0f0f0fu}; }

@@ -4,7 +4,7 @@
 //                                                                           s = sum_{c in g} x[t, c]
 // The codes enter the matrix instructions as the 16-bit numbers 16 + code, exactly (8-bit inputs: as bytes, without
 // the 16), so their products with 16-bit inputs are exact in fp32 and the only roundings are those of the fp32 sums; a
-// group's sums start from zero and are scaled when it ends.  fp32 inputs go in as three bf16 terms.
+// group's sums start from zero and are scaled when it ends.  fp32 inputs go in as three bf16 terms, against 2 code - 15.
 //
 // Up to 16 tokens: bound by the weights' bytes (product4_rows_kernel).  One token through 8192 x 8192 takes 9.2 us in half
 // precision, 35.7 MB at 3.9 TB/s, where the plain read kernel gives 6.3 for buffers out of cache; through 768 x 768 3.3 us, of which
@@ -106,11 +106,27 @@ struct Operand<OBC_I8> {
     }
 };
 
+// What stands for a code q in XT's operands is q / unit + base.  fp32 inputs: 2 q - 15, which costs their unpacking three times the
+// instructions (22 for eight codes, 8 for 16 + q) but next to six matrix instructions and more: the matrix cores' sums are not rounded to
+// nearest, and their error grows with the sums' size, five times as large with 16 + q.  (100 tokens through 300 x 128: 1.1e-6 off with 16 + q,
+// 1.1e-7 with 2 q - 15; 40 through 512 x 16384 3.4e-6 and 1.6e-7; 500 through 4096 x 4096 take 75 us, 67 with 16 + q.)  16-bit outputs
+// hide either.
+template <int XT>
+constexpr float kUnit = XT == OBC_F32 ? 0.5f : 1.f;
+template <int XT>
+constexpr float kBase = XT == OBC_F32 ? -7.5f : XT == OBC_I8 ? 0.f : kCodeBase;      // base times unit
+
+template <int XT>
+__device__ inline uintx4 codes_of(unsigned w)
+{
+    return XT == OBC_F32 ? codes_centred_bf16(w) : XT == OBC_F16 ? codes_f16(w) : codes_bf16(w);
+}
+
 // Codes of one instruction and ones, as the operand that meets XT's.
 template <int XT>
 struct Codes {
     uintx4 v;
-    __device__ explicit Codes(unsigned w) : v(XT == OBC_F16 ? codes_f16(w) : codes_bf16(w)) {}
+    __device__ explicit Codes(unsigned w) : v(codes_of<XT>(w)) {}
     static __device__ Codes ones()
     {
         Codes c(0);
@@ -195,7 +211,6 @@ __global__ __launch_bounds__(rows_waves(XT) * 64) void product4_rows_kernel(Args
     for (int j = 0; j < NF; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
-    constexpr float base = XT == OBC_I8 ? 0.f : kCodeBase;
     const Codes<XT> ones = Codes<XT>::ones();
     struct Weights {
         uintx4 w[NF];
@@ -295,9 +310,9 @@ __global__ __launch_bounds__(rows_waves(XT) * 64) void product4_rows_kernel(Args
             }
 #pragma unroll
             for (int j = 0; j < NF; ++j) {
-                const float step = half_lo(g.sc[j][u]), off = half_hi(g.sc[j][u]) - base * step;
+                const float step = half_lo(g.sc[j][u]), off = half_hi(g.sc[j][u]) - kBase<XT> * step;
 #pragma unroll
-                for (int v = 0; v < 4; ++v) acc[j][v] = fmaf(step, S[j][v], fmaf(off, s[v], acc[j][v]));
+                for (int v = 0; v < 4; ++v) acc[j][v] = fmaf(step * kUnit<XT>, S[j][v], fmaf(off, s[v], acc[j][v]));
             }
         }
     };
@@ -455,7 +470,6 @@ __global__ __launch_bounds__(tile_waves(BN) * 64, 2) void product4_tiles_kernel(
     const int slice = blockIdx.x / tok.tiles, tile = tile_of(blockIdx.x % tok.tiles, tok.tiles);
     const int t0 = (tile % tok.mtiles) * BM, rb0 = (tile / tok.mtiles) * (BN / 16);
     const int kt0 = slice * tok.per, kt1 = kt0 + tok.per < a.KT ? kt0 + tok.per : a.KT;
-    constexpr float base = XT == OBC_I8 ? 0.f : kCodeBase;
     auto row_block = [&](int j) { return (int64_t)(rb0 + j < a.RB ? rb0 + j : a.RB - 1); };      // beyond the last: not stored
 
     // where this lane's loads come from, at the slice's first tile
@@ -514,7 +528,7 @@ __global__ __launch_bounds__(tile_waves(BN) * 64, 2) void product4_tiles_kernel(
                     const int g = g0 + 8 * quad + e;
                     unsigned sc = 0;
                     if (g < a.NG) sc = SUB > 1 ? a.scales[((rb * a.KT + g / SUB) * 16 + n) * SUB + g % SUB] : a.scales[(rb * a.NG + g) * 16 + n];
-                    v[e] = half_hi(sc) - base * half_lo(sc);
+                    v[e] = half_hi(sc) - kBase<XT> * half_lo(sc);
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -554,7 +568,7 @@ __global__ __launch_bounds__(tile_waves(BN) * 64, 2) void product4_tiles_kernel(
             w[j] = lds[C::XN + (wn * NF + j) * 64 + lane];
 #pragma unroll
             for (int u = 0; u < SUB; ++u)
-                step[j][u] = half_lo(((const unsigned *)(lds + C::XN + C::WN16))[C::step_at(((wn * NF + j) * 16 + n) * SUB + u)]);
+                step[j][u] = kUnit<XT> * half_lo(((const unsigned *)(lds + C::XN + C::WN16))[C::step_at(((wn * NF + j) * 16 + n) * SUB + u)]);
         }
         if constexpr (XT == OBC_I8) {
 #pragma unroll
@@ -612,7 +626,7 @@ __global__ __launch_bounds__(tile_waves(BN) * 64, 2) void product4_tiles_kernel(
                 for (int k = u * 4 / SUB; k < (u + 1) * 4 / SUB; ++k) {
                     uintx4 B[NF];
 #pragma unroll
-                    for (int j = 0; j < NF; ++j) B[j] = XT == OBC_F16 ? codes_f16(w[j][k]) : codes_bf16(w[j][k]);
+                    for (int j = 0; j < NF; ++j) B[j] = codes_of<XT>(w[j][k]);
 #pragma unroll
                     for (int m = 0; m < MF; ++m)
 #pragma unroll

@@ -115,6 +115,19 @@ def test_product_of_strided_and_misaligned_rows(ctx, T, kind):
     assert torch.all(ybuf[:, 0] == 77.0) and torch.all(ybuf[:, 1 + R:] == 77.0)
 
 
+@pytest.mark.parametrize("T,d", [(3, 128), (3, 8192), (40, 300), (40, 8192), (100, 128), (100, 2000)])
+def test_fp32_products_are_as_exact_as_sums_rounded_to_nearest(ctx, T, d):
+    """A sum of d terms in order, each partial sum (of variance i / d of the last) rounded by at most 2^-24 of itself, is off
+    by 2^-24 sqrt(d / 6) of its size in the mean square."""
+    g = _gen(T + d)
+    for group in (0, 32, 128):
+        codes, delta, offset, W, _ = _layer(300, d, group, g)
+        x = torch.randn(T, d, generator=g, device="cuda")
+        want = x.double() @ W.T
+        err = (ctx.obc_product4(ctx.obc_pack4(codes, delta, offset, group), x).double() - want).norm() / want.norm()
+        assert err <= U32 * (d / 6) ** 0.5, (group, float(err))
+
+
 def test_product_sees_cancelling_and_large_inputs(ctx):
     """fp32 inputs over a wide range: the three terms carry all 24 bits."""
     g = _gen(8)
