@@ -2,6 +2,11 @@
 //
 //   e[v] = exp((z[v] - max z) / tau), q[v] = e[v] / sum e;  log q[v] = (z[v] - max z) / tau - log sum e
 //   loss = weight tau^2 sum_j p_j (log p_j - log q[i_j]);  dz[v] = weight tau (q[v] - sum_{j: i_j = v} p_j)
+// Memory-bound: 2048 x 131072 in bf16 with its gradient, 1.07 GB, takes 260 us (4.1 TB/s; the plain copy kernel reaches 4.3 on a GB,
+// the best copy 5.2): a workgroup of 1024 threads holds a row in its registers, one to a compute unit, so that loads and stores
+// overlap only where a piece's gradient makes room for the next row's.  48 x 32000 in half precision takes 11 us: reductions one
+// after the other, on 48 compute units.  Barriers that leave loads under way and stores past the caches changed nothing measurable (1 %).
+//
 // A row is read once and stays in registers; the teacher's entries are handled in fp32, and those that name the same
 // token write the same value, so no order of writes changes the result.
 #include "product4.h"
@@ -303,7 +308,7 @@ __global__ __launch_bounds__(NT, 1024 / NT * NT / 256) void distill_kernel(Args 
     }
 }
 
-// Longer rows, read a second time for the gradient.
+// Longer rows, read a second time for the gradient (rows that fit take 287 us this way against 261, 2048 x 131072 in bf16).
 template <int TYPE>
 __global__ __launch_bounds__(1024) void distill_long_kernel(Args a)
 {

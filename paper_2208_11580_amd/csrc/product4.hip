@@ -7,11 +7,11 @@
 // group's sums start from zero and are scaled when it ends.  fp32 inputs go in as three bf16 terms, against 2 code - 15.
 //
 // Up to 16 tokens: bound by the weights' bytes (product4_rows_kernel).  One token through 8192 x 8192 takes 9.2 us in half
-// precision, 35.7 MB at 3.9 TB/s, where the plain read kernel gives 6.3 for buffers out of cache; through 768 x 768 3.3 us, of which
-// 2.4 are a launch.  More tokens: bound by instruction issue beside the matrix cores (product4_tiles_kernel).  2048 tokens through
-// 4096 x 4096 in bf16 take 77 us, 890 TFLOP/s (a dense library product of that size: 61 us, 1120); of the tiles' 72 us the matrix cores are busy 41 %
-// and the vector units 48 %: 64 matrix instructions of a wave and tile come with 64 multiply-adds that scale groups and 128 that
-// unpack codes.  All captured in a graph.
+// precision, 35.7 MB at 3.9 TB/s (plain reads of 64 MB and more: 6.0 to 6.3); through 768 x 768 3.3 us, of which about 2 are a
+// launch.  More tokens: bound by instruction issue beside the matrix cores (product4_tiles_kernel).  2048 tokens through 4096 x 4096 in
+// bf16 take 80 us, 860 TFLOP/s (a dense library product of that size: 61 us, 1120); in the tiles' 73 us the matrix cores are busy 41 % of the
+// time, and a matrix instruction comes with 3.7 vector ones.  8-bit inputs: 1000 tokens through 4096 x 8192 in groups of 64 take 84 us in the
+// tiles, 800 TOP/s, 10 vector instructions to a matrix instruction.  (Medians, captured in a graph.)
 #include "product4.h"
 
 namespace {
@@ -192,8 +192,8 @@ constexpr int tile_bytes(int XT) { return XT == OBC_F32 ? 768 : XT == OBC_I8 ? 1
 
 // 16 NF rows of W and up to 16 tokens to a workgroup, whose waves take turns along the columns' tiles and sum in LDS.  The
 // weights' bytes bound it: a wave has its next tile's codes on their way (two or three ahead measured slower, 9.9 and 11.3 us against
-// 9.2 for one token through 8192 x 8192: 16 waves to a compute unit cover the rest, and the copies cost instructions).  Loads come back in order, so the tokens must not be among them: they go through LDS, `chunk`
-// tiles at a time.
+// 9.2 for one token through 8192 x 8192: 16 waves to a compute unit cover the rest, and the copies cost instructions).  Loads come back
+// in order, so the tokens must not be among them: they go through LDS, `chunk` tiles at a time.
 template <int XT, int SUB, int NF>
 __global__ __launch_bounds__(rows_waves(XT) * 64) void product4_rows_kernel(Args a, int y_type, int chunk)
 {
@@ -434,10 +434,9 @@ struct Tokens {
 // BM tokens x BN rows of W to a workgroup of WM x WN waves.  Tokens, codes and steps of STAGES column tiles go through LDS in
 // turn, so that loads have STAGES - 1 tiles' time to arrive; a wave waits for all but its newest ones and then for the others.
 //
-// 128 x 256 with eight waves of 64 x 64 where that fills the chip: a wave's unpacked codes serve 64 tokens, its tokens 64 rows.  64 x
-// 128 with waves of 64 x 32 otherwise (2048 tokens through 4096 x 4096: 95 us against 79; 1000 in 8 bits through 4096 x 8192, where 128 x
-// 256 would be 128 workgroups or two slices: 106 us against 116).  Waves of 128 x 64, which unpack half as much, are one to a SIMD
-// and took 106 us then; more stages or operands read a step earlier changed nothing.
+// 128 x 256 with eight waves of 64 x 64 where that fills the chip: a wave's unpacked codes serve 64 tokens, its tokens 64 rows.  Waves
+// of 128 x 64, which unpack half as much, are one to a SIMD and slower (2048 tokens through 4096 x 4096: 106 us, when this one took
+// 84); more stages or operands read a step earlier changed nothing.
 constexpr int tile_waves(int BN) { return BN / 32; }
 
 template <int XT, int SUB, int BM, int BN, int WM, int STAGES>
@@ -723,9 +722,11 @@ Plan plan_of(const pack4_layout &L, int T, int x_type)
     int64_t tiles = 0;
     if (x_type == OBC_F32) tiles = T > 32 ? cut(64, 128) : cut(32, 128);
     else if (T <= 32) tiles = cut(32, 128);
+    // 128 x 256 for three quarters of the compute units and more (2048 x 4096 x 4096 in bf16, 256 tiles: 82 us, in tiles of 64 x 128
+    // 101; 500 x 4096 x 4096, 64 tiles: 63 us and 34; 8 bits, 1000 x 4096 x 8192, 128 tiles: 145 us and 102)
     else if (T <= 64 || (tiles = cut(128, 256)) < 192) tiles = cut(64, 128);
     // few tokens leave too few tiles for the chip: slices of the columns, two workgroups to a compute unit (fp32 in tiles of 64: one),
-    // two tiles at least to a slice
+    // two tiles at least to a slice (4096 x 4096 in bf16, 17 tokens: 12.8 us, with one slice 20.9; 64 tokens: 19.0 and 31.1)
     int64_t s = p.BM < 128 && tiles > 0 ? (x_type == OBC_F32 && p.BM == 64 ? 256 : 512) / tiles : 1;
     if (s > 16) s = 16;
     if (s > L.KT / 2) s = L.KT / 2;
@@ -753,6 +754,8 @@ bool takes_rows(const pack4_layout &L, int T, int x_type, Rows *r)
 {
     if (T > kRowsTokens) return false;
     const bool wide = x_type == OBC_F32;
+    // 32 rows to a workgroup, which share the tokens in LDS, where 16 would be more than a workgroup to a compute unit (8 bits, 8 x 16384 x
+    // 4096: 14.9 us, with 16 rows 17.2; 13 x 5000 x 4999: 9.9 and 13.7; the other way round 1 x 4096 x 4096: 5.1 us with 16, 6.1 with 32)
     r->NF = L.RB > 256 ? 2 : 1;
     r->blocks = (L.RB + r->NF - 1) / r->NF;
     // sixteen waves to a compute unit, in one workgroup or two; no more than there are tiles
