@@ -1,4 +1,4 @@
-// Driver for a host-only sanitizer build of the operators around compressed layers: sizes, plans and the argument
+// Program for a host-only sanitizer build of the operators around compressed layers: sizes, plans and the argument
 // checks that reject a call before anything is launched.  Exit status 0 = clean.
 #include <climits>
 #include <cstdio>
