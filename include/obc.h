@@ -333,10 +333,9 @@ int obc_product4(obc_ctx *ctx, const void *packed, int R, int d, int group, cons
 /* dx = dy W for T tokens, the gradient of obc_product4's inputs: dx[t, c] = sum_r dy[t, r] W[r, c].
  *   dy  T x R, leading dimension lddy >= R;  dx  T x d, leading dimension lddx >= d; both of `type`
  *       (OBC_F32, OBC_F16 or OBC_BF16)
- * 16-bit types: weights rounded to half precision (the steps differ along the sum, so they cannot be taken out
- * of it; a weight beyond 65504 becomes an infinity), products and sums fp32, one rounding of the result.
- * OBC_F32: the precision of fp32 throughout.  Fixed summation order for a given T, R, d and group.  A non-finite dy makes
- * its token's outputs non-finite.  dx may not overlap dy. */
+ * 16-bit types: weights to 22 bits, products and sums fp32, one rounding of the result.  OBC_F32: the precision of
+ * fp32 throughout.  Fixed summation order for a given T, R, d and group.  A non-finite dy makes its token's outputs
+ * non-finite.  dx may not overlap dy. */
 int obc_product4_grad_workspace_bytes(int T, int R, int d, int group, int type, size_t *bytes);
 int obc_product4_grad(obc_ctx *ctx, const void *packed, int R, int d, int group, const void *dy, int type, int T,
                       int64_t lddy, void *dx, int64_t lddx, void *ws, size_t ws_bytes);

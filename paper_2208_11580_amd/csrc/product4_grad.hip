@@ -1,19 +1,19 @@
 // obc_product4_grad: dx = dy W, the gradient of the inputs of a product with 4-bit weights.
 //
 //   dx[t, c] = sum_r dy[t, r] (offset + delta code)[r, c]
-// The sum runs over the rows, whose steps differ, so the weights are formed before the product.  16-bit types: in half
-// precision, whose packed instructions take two weights at a time and which rounds eight times finer than bf16; a
-// token's bf16 gradients, scaled by a power of two so that the largest is near 2^14, are half-precision numbers too (what
+// The sum runs over the rows, whose steps differ, so the weights are formed before the product.  16-bit types: each as two
+// numbers of half precision, 22 bits of it (rounded to one, its 11 bits changed 10 % of the bf16 results and 40 % of the fp16
+// ones); a token's bf16 gradients, scaled by a power of two so that the largest is near 2^14, are half-precision numbers too (what
 // that loses lies 2^-39 below the largest).  fp32: weights and gradients as three bf16 terms each, six of the nine
 // products (what is left out is below 2^-24).
 //
 // A first launch lays out the gradients as the matrix instructions' operands want them and turns the codes, so that the
-// lanes lie along the columns and a dword holds eight rows: 9 of a large product's 90 us.  The product then is like the
+// lanes lie along the columns and a dword holds eight rows: 9 of a large product's 121 us.  The product then is like the
 // forward one: gradients and codes through LDS, weights formed in registers once for a wave's tokens.  Few tokens leave too few
 // tiles for the chip: the rows are cut into slices, whose sums a third launch adds in order.
 //
-// Bound by instruction issue beside the matrix cores: 2048 tokens through 4096 x 4096 in bf16 take 90 us, 760 TFLOP/s, the tiles 80 of
-// them with the matrix cores busy 35 %; 77 tokens through 2304 x 1283 in fp32 18.6 us (12 the tiles, 3 the layout, 4 the sum of slices).
+// Bound by the matrix cores and the forming of weights, one after the other: 2048 tokens through 4096 x 4096 in bf16 take 121 us,
+// 570 TFLOP/s of the product and twice that in the matrix cores, the tiles 112 of them; 77 tokens through 2304 x 1283 in fp32 18.6 us (12 the tiles, 3 the layout, 4 the sum of slices).
 #include "product4.h"
 
 namespace {
@@ -31,6 +31,7 @@ struct Args {
     float *back;                // T: what undoes a token's power of two
     unsigned *turned;           // codes: tile (column block cb, row tile rt) at (cb * RT + rt) * 256, as in pack4.h
     unsigned short *steps;      // NG x 2 x RT * 128: a group's steps, then its offsets
+    unsigned char *wide;        // NG x RT * 2: whether a group has a weight beyond half precision among 64 rows
     float *part;                // slices x T x d
     int slices, per;            // slices of the rows, row tiles of a slice
 };
@@ -93,6 +94,9 @@ __global__ __launch_bounds__(256) void grad_lay_kernel(Args a, int64_t turns, in
             w = a.SUB > 1 ? a.scales[(((r >> 4) * a.KT + g / a.SUB) * 16 + (r & 15)) * a.SUB + g % a.SUB] : a.scales[((r >> 4) * a.NG + g) * 16 + (r & 15)];
         a.steps[2 * g * len + r] = (unsigned short)w;
         a.steps[(2 * g + 1) * len + r] = (unsigned short)(w >> 16);
+        const float first = half_hi(w), last = fmaf(15.f, half_lo(w), first);
+        const bool wide = __any(!(fmaxf(fabsf(first), fabsf(last)) <= 65504.f));      // (a wave's 64 rows belong to one group)
+        if ((tid & 63) == 0) a.wide[i >> 6] = wide;
         return;
     }
     const int64_t t = (int64_t)blockIdx.x - turns - scale_blocks;
@@ -189,16 +193,30 @@ __global__ __launch_bounds__(256) void grad_lay_kernel(Args a, int64_t turns, in
 }
 
 // ---- product ------------------------------------------------------------------------------------------------------
-// Eight weights of a lane's column, of the eight rows that `steps` and `offsets` (half precision) belong to.
-__device__ inline uintx4 weights_f16(unsigned w, uintx4 steps, uintx4 offsets)
+// Eight weights of a lane's column, of the eight rows that `steps` and `offsets` (half precision) belong to, each as two numbers of
+// half precision: the first cut off, the second what it leaves, so that a weight is exact below 1 and off by 2^-22 above.  WIDE: a 32nd
+// of them, for weights beyond half precision (which end below 2^20).
+template <bool WIDE>
+__device__ inline void weights_f16(unsigned w, uintx4 steps, uintx4 offsets, uintx4 (&r)[2])
 {
     const uintx4 c = codes_f16(w);
-    const halfx2 base = {(_Float16)-16.f, (_Float16)-16.f};
-    uintx4 r;
+    const _Float16 b = (_Float16)-16.f, s = (_Float16)(1.f / 32.f);
+    const halfx2 base = {b, b}, part = {s, s};
+    // (not known to be -1, or the mixed-precision multiply-add becomes a conversion and a subtraction)
+    float minus = -1.f;
+    asm("" : "+s"(minus));
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        r[j] = bits_of(__builtin_elementwise_fma(half_pair(steps[j]), half_pair(c[j]) + base, half_pair(offsets[j])));
-    return r;
+    for (int j = 0; j < 4; ++j) {
+        halfx2 q = half_pair(c[j]) + base, step = half_pair(steps[j]), off = half_pair(offsets[j]);
+        if (WIDE) {
+            q *= part;
+            off *= part;
+        }
+        const float v0 = fmaf((float)step.x, (float)q.x, (float)off.x), v1 = fmaf((float)step.y, (float)q.y, (float)off.y);
+        const halfx2 hi = __builtin_bit_cast(halfx2, __builtin_amdgcn_cvt_pkrtz(v0, v1));
+        r[0][j] = bits_of(hi);
+        r[1][j] = bits_of(halfx2{(_Float16)fmaf(minus, (float)hi.x, v0), (_Float16)fmaf(minus, (float)hi.y, v1)});
+    }
 }
 
 // The same in three bf16 terms, eight bits of the weight after the other: cut off rather than rounded, which is as exact and half
@@ -220,9 +238,15 @@ __device__ inline void weights_split(unsigned w, uintx4 steps, uintx4 offsets, u
     }
 }
 
-template <int TYPE, int BM, int BN, int WM>
+template <bool V>
+struct Flag {
+    static constexpr bool value = V;
+};
+
+template <int TYPE, int BM, int BN>
 struct Tile {
-    static constexpr int P = TYPE == OBC_F32 ? 3 : 1, WAVES = BN / 32, WN = WAVES / WM, MF = BM / WM / 16, NF = BN / WN / 16;
+    // planes of the gradients, terms of a weight; a wave takes all tokens and 32 columns, so that every weight is formed once
+    static constexpr int P = TYPE == OBC_F32 ? 3 : 1, TERMS = TYPE == OBC_F32 ? 3 : 2, WAVES = BN / 32, MF = BM / 16, NF = 2;
     static constexpr int XN = P * BM * 16, CN = BN * 4;      // 16-byte places of a stage: gradients, codes; then steps
     static constexpr int PLACES = XN + CN + WAVES * 32;
     // loads of a wave for a stage: 64 places each, and twice 64 times 4 bytes of steps and offsets, a quarter of a tile's columns
@@ -231,17 +255,16 @@ struct Tile {
     static_assert(XN % (64 * WAVES) == 0 && CN % (64 * WAVES) == 0, "whole loads");
 };
 
-// BM tokens x BN columns to a workgroup of WM x WN waves: gradients, codes and steps of 128 rows go through two or three stages of LDS
+// BM tokens x BN columns to a workgroup: gradients, codes and steps of 128 rows go through two or three stages of LDS
 // in turn, as in the forward product.
-template <int TYPE, int BM, int BN, int WM>
+template <int TYPE, int BM, int BN>
 __global__ __launch_bounds__(BN * 2, 2) void grad_tiles_kernel(Args a, int mtiles, int ntiles)
 {
-    using C = Tile<TYPE, BM, BN, WM>;
-    constexpr int P = C::P, MF = C::MF, NF = C::NF, STAGES = C::STAGES;
+    using C = Tile<TYPE, BM, BN>;
+    constexpr int P = C::P, TERMS = C::TERMS, MF = C::MF, NF = C::NF, STAGES = C::STAGES;
     __shared__ uintx4 lds0[C::PLACES], lds1[C::PLACES], lds2[STAGES > 2 ? C::PLACES : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 15, quad = lane >> 4;
-    const int wm = wave % WM, wn = wave / WM;
     const int tiles = mtiles * ntiles, slice = blockIdx.x / tiles, tile = tile_of(blockIdx.x % tiles, tiles);
     const int t0 = (tile % mtiles) * BM, kt = tile / mtiles * (BN / 128);      // first token, first tile of 128 columns
     const int rt0 = slice * a.per, rt1 = rt0 + a.per < a.RT ? rt0 + a.per : a.RT;
@@ -262,11 +285,14 @@ __global__ __launch_bounds__(BN * 2, 2) void grad_tiles_kernel(Args a, int mtile
         if (cb >= a.KT * 8) cb = a.KT * 8 - 1;      // beyond the last column: not stored
         csrc[i] = (const char *)a.turned + ((int64_t)cb * a.RT + rt0) * 1024 + lane * 16;
     }
+    bool beyond = false;      // weights of this wave's columns, in the slice's rows, that half precision does not hold
     {
         const int own = kt + (wave >> 2);      // the tile of this wave's 32 columns
         int g = a.SUB > 1 ? own * a.SUB + (wave & 3) * a.SUB / 4 : own / a.tpg;
         if (g >= a.NG) g = a.NG - 1;
         ssrc = (const char *)(a.steps + 2 * g * len + rt0 * 128) + lane * 4;
+        if (TYPE != OBC_F32)
+            for (int i = 2 * rt0 + lane; i < 2 * rt1; i += 64) beyond |= a.wide[(int64_t)g * a.RT * 2 + i] != 0;
     }
     auto fetch = [&](int rt, uintx4 *lds) __attribute__((always_inline)) {
         const int64_t k = (rt < rt1 ? rt : rt1 - 1) - rt0;      // (behind the last: its tile again, for the count of loads)
@@ -287,33 +313,28 @@ __global__ __launch_bounds__(BN * 2, 2) void grad_tiles_kernel(Args a, int mtile
         for (int j = 0; j < NF; ++j) acc[m][j] = floatx4{0.f, 0.f, 0.f, 0.f};
     fetch(rt0, lds0);
     if (STAGES > 2) fetch(rt0 + 1, lds1);
+    const bool wide = __any(beyond);
     __builtin_amdgcn_s_waitcnt(wait_loads(0));
     stage_barrier();
-    auto turn = [&](const int rt, const uintx4 *lds, uintx4 *lds_next) __attribute__((always_inline)) {
+    auto turn = [&](auto flag, const int rt, const uintx4 *lds, uintx4 *lds_next) __attribute__((always_inline)) {
         fetch(rt + STAGES - 1, lds_next);
         uintx4 w[NF];
 #pragma unroll
-        for (int j = 0; j < NF; ++j) w[j] = lds[C::XN + (wn * NF + j) * 64 + lane];
+        for (int j = 0; j < NF; ++j) w[j] = lds[C::XN + (wave * NF + j) * 64 + lane];
+        const uintx4 *const steps = lds + C::XN + C::CN + wave * 32;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            uintx4 B[P][NF];
+            const uintx4 step = steps[4 * k + quad], off = steps[16 + 4 * k + quad];
+            uintx4 B[NF][TERMS];
 #pragma unroll
             for (int j = 0; j < NF; ++j) {
-                const uintx4 *const steps = lds + C::XN + C::CN + ((wn * NF + j) >> 1) * 32;
-                const uintx4 step = steps[4 * k + quad], off = steps[16 + 4 * k + quad];
-                if constexpr (P == 3) {
-                    uintx4 r[3];
-                    weights_split(w[j][k], step, off, r);
-#pragma unroll
-                    for (int p = 0; p < 3; ++p) B[p][j] = r[p];
-                } else {
-                    B[0][j] = weights_f16(w[j][k], step, off);
-                }
+                if constexpr (TYPE == OBC_F32) weights_split(w[j][k], step, off, B[j]);
+                else weights_f16<decltype(flag)::value>(w[j][k], step, off, B[j]);
             }
 #pragma unroll
             for (int m = 0; m < MF; ++m) {
-                const int t = (wm * MF + m) * 16 + n;
-                if constexpr (P == 3) {
+                const int t = m * 16 + n;
+                if constexpr (TYPE == OBC_F32) {
                     uintx4 A[3];
 #pragma unroll
                     for (int p = 0; p < 3; ++p) A[p] = lds[(p * BM + t) * 16 + ((4 * k + quad) ^ n)];
@@ -322,39 +343,46 @@ __global__ __launch_bounds__(BN * 2, 2) void grad_tiles_kernel(Args a, int mtile
 #pragma unroll
                         for (int p = 0; p <= o; ++p)
 #pragma unroll
-                            for (int j = 0; j < NF; ++j) acc[m][j] = mfma_bf16(A[p], B[o - p][j], acc[m][j]);
+                            for (int j = 0; j < NF; ++j) acc[m][j] = mfma_bf16(A[p], B[j][o - p], acc[m][j]);
                 } else {
                     const uintx4 A = lds[t * 16 + ((4 * k + quad) ^ n)];
 #pragma unroll
-                    for (int j = 0; j < NF; ++j) acc[m][j] = mfma_f16(A, B[0][j], acc[m][j]);
+                    for (int o = 1; o >= 0; --o)
+#pragma unroll
+                        for (int j = 0; j < NF; ++j) acc[m][j] = mfma_f16(A, B[j][o], acc[m][j]);
                 }
             }
         }
         __builtin_amdgcn_s_waitcnt(wait_loads(STAGES > 2 ? C::LOADS : 0));      // the next tile is in LDS
         stage_barrier();
     };
-    for (int rt = rt0;;) {
-        turn(rt, lds0, STAGES > 2 ? lds2 : lds1);
-        if (++rt >= rt1) break;
-        turn(rt, lds1, lds0);
-        if (++rt >= rt1) break;
-        if (STAGES > 2) {
-            turn(rt, lds2, lds1);
+    auto all = [&](auto flag) __attribute__((always_inline)) {
+        for (int rt = rt0;;) {
+            turn(flag, rt, lds0, STAGES > 2 ? lds2 : lds1);
             if (++rt >= rt1) break;
+            turn(flag, rt, lds1, lds0);
+            if (++rt >= rt1) break;
+            if (STAGES > 2) {
+                turn(flag, rt, lds2, lds1);
+                if (++rt >= rt1) break;
+            }
         }
-    }
+    };
+    // (the waves of a workgroup may part here: either way they pass the same number of barriers)
+    if (TYPE != OBC_F32 && wide) all(Flag<true>());
+    else all(Flag<false>());
     // (loads behind the last tile still write to LDS: they are waited for before it can be another workgroup's)
     __builtin_amdgcn_s_waitcnt(wait_loads(0));
 #pragma unroll
     for (int m = 0; m < MF; ++m)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int t = t0 + (wm * MF + m) * 16 + 4 * quad + i;
+            const int t = t0 + m * 16 + 4 * quad + i;
             if (t >= a.T) continue;
-            const float back = TYPE == OBC_BF16 ? a.back[t] : 1.f;
+            const float back = (TYPE == OBC_BF16 ? a.back[t] : 1.f) * (wide ? 32.f : 1.f);
 #pragma unroll
             for (int j = 0; j < NF; ++j) {
-                const int c = kt * 128 + (wn * NF + j) * 16 + n;
+                const int c = kt * 128 + (wave * NF + j) * 16 + n;
                 if (c >= a.d) continue;
                 const float v = acc[m][j][i] * back;
                 if (a.slices > 1) a.part[((int64_t)slice * a.T + t) * a.d + c] = v;
@@ -376,7 +404,7 @@ __global__ __launch_bounds__(256) void grad_add_kernel(Args a)
 // ---- host ---------------------------------------------------------------------------------------------------------
 struct Plan {
     int BM, BN, mtiles, ntiles, slices, per, RT;
-    size_t rows, back, turned, steps, part, bytes;
+    size_t rows, back, turned, steps, wide, part, bytes;
 };
 
 Plan plan_of(const pack4_layout &L, int T, int type)
@@ -394,11 +422,11 @@ Plan plan_of(const pack4_layout &L, int T, int type)
     // (fp32: 77 tokens through 2304 x 1283 take 19.4 us in tiles of 32, 20.2 in tiles of 64; 500 through 4096 x 4096 151 and 115)
     if (T <= 32 || (type == OBC_F32 && T <= 96)) tiles = cut(32, 128);
     else if (type == OBC_F32) tiles = cut(64, 128);
-    // 128 x 256 for three quarters of the compute units and more (2048 x 4096 x 4096 in bf16: 92 us, in tiles of 64 x 128 106; 500 x 4096 x
-    // 4096: 76 us and 45)
+    // 128 x 256 for three quarters of the compute units and more (2048 x 4096 x 4096 in bf16: 121 us, in tiles of 64 x 128 145; 500 x 4096 x
+    // 4096: 105 us and 53)
     else if (T <= 64 || (tiles = cut(128, 256)) < 192) tiles = cut(64, 128);
     // few tokens: slices of the rows, two workgroups to a compute unit (fp32, whose planes leave room for one: one), two row tiles
-    // at least to a slice (77 x 2304 x 1283 in fp32: 19 us, with one slice 46; 64 x 4096 x 4096 in bf16: 25 and 37)
+    // at least to a slice (77 x 2304 x 1283 in fp32: 19 us, with one slice 46; 64 x 4096 x 4096 in bf16: 24 and 48)
     int64_t s = p.BM < 128 && tiles > 0 ? (type == OBC_F32 ? 256 : 512) / tiles : 1;
     if (s > p.RT / 2) s = p.RT / 2;
     if (s < 1) s = 1;
@@ -410,6 +438,7 @@ Plan plan_of(const pack4_layout &L, int T, int type)
     p.back = take((size_t)T * 4);
     p.turned = take((size_t)L.KT * 8 * p.RT * 1024);
     p.steps = take((size_t)L.NG * p.RT * 512);
+    p.wide = take((size_t)L.NG * p.RT * 2);
     p.part = take(p.slices > 1 ? (size_t)p.slices * T * L.d * 4 : 0);
     p.bytes = at;
     return p;
@@ -424,9 +453,9 @@ int launch(obc_ctx *ctx, Args a, const Plan &p)
         return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_product4_grad: too many tiles");
     grad_lay_kernel<TYPE><<<(unsigned)lay, 256, 0, ctx->stream>>>(a, turns, scale_blocks);
     OBC_LAUNCH_CHECK(ctx, "grad_lay_kernel");
-    if (p.BM == 32) grad_tiles_kernel<TYPE, 32, 128, 1><<<(unsigned)tiles, 256, 0, ctx->stream>>>(a, p.mtiles, p.ntiles);
-    else if (p.BM == 64) grad_tiles_kernel<TYPE, 64, 128, 1><<<(unsigned)tiles, 256, 0, ctx->stream>>>(a, p.mtiles, p.ntiles);
-    else if constexpr (TYPE != OBC_F32) grad_tiles_kernel<TYPE, 128, 256, 2><<<(unsigned)tiles, 512, 0, ctx->stream>>>(a, p.mtiles, p.ntiles);
+    if (p.BM == 32) grad_tiles_kernel<TYPE, 32, 128><<<(unsigned)tiles, 256, 0, ctx->stream>>>(a, p.mtiles, p.ntiles);
+    else if (p.BM == 64) grad_tiles_kernel<TYPE, 64, 128><<<(unsigned)tiles, 256, 0, ctx->stream>>>(a, p.mtiles, p.ntiles);
+    else if constexpr (TYPE != OBC_F32) grad_tiles_kernel<TYPE, 128, 256><<<(unsigned)tiles, 512, 0, ctx->stream>>>(a, p.mtiles, p.ntiles);
     OBC_LAUNCH_CHECK(ctx, "grad_tiles_kernel");
     if (p.slices > 1) {
         grad_add_kernel<TYPE><<<(unsigned)adds, 256, 0, ctx->stream>>>(a);
@@ -493,6 +522,7 @@ int obc_product4_grad(obc_ctx *ctx, const void *packed, int R, int d, int group,
     a.back = (float *)(w + p.back);
     a.turned = (unsigned *)(w + p.turned);
     a.steps = (unsigned short *)(w + p.steps);
+    a.wide = (unsigned char *)(w + p.wide);
     a.part = (float *)(w + p.part);
     a.slices = p.slices; a.per = p.per;
     return type == OBC_F32 ? launch<OBC_F32>(ctx, a, p) : type == OBC_F16 ? launch<OBC_F16>(ctx, a, p) : launch<OBC_BF16>(ctx, a, p);

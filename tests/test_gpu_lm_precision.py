@@ -1,0 +1,52 @@
+"""What the operators around compressed layers hold in how many bits: gradients of 16-bit products against their weights in
+full, fp32 results over long sums, grids and norms at the ends of their ranges."""
+import pytest
+import torch
+
+from .test_gpu_lm import ROUND, TINY, TYPES, U32, _gen, _layer, _within, ctx  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("T,R,d,group", [(7, 300, 257, 32), (50, 512, 640, 128), (64, 100, 1000, 0), (300, 512, 384, 64), (2000, 260, 3100, 128)])
+def test_gradients_of_16_bits_are_rounded_once(ctx, T, R, d, group, kind):
+    """A sum of R products of two terms each, partial sums cut off at 2^-23, is off by 2^-23 sqrt(R / 3) of its size in the mean
+    square.  That takes a value to its neighbour if it lies that near to the middle of two, which is 2 / eps of that share
+    of the values, and more of those that came out small by cancellation: 8 / eps in all.  A weight rounded to half precision,
+    2^-13 off in the mean, would move tens of per cent."""
+    g = _gen(T + R)
+    codes, delta, offset, W, _ = _layer(R, d, group, g)
+    dy = torch.randn(T, R, generator=g, device="cuda").to(TYPES[kind])
+    dx = ctx.obc_product4_grad(ctx.obc_pack4(codes, delta, offset, group), dy)
+    ctx.obc_check()
+    want = (dy.double() @ W).to(TYPES[kind])
+    moved = float((dx != want).double().mean())
+    assert moved <= 8 * 2.0 ** -23 * (R / 3) ** 0.5 / torch.finfo(TYPES[kind]).eps, moved
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T,R,d,group", [(3, 40, 300, 128), (50, 300, 300, 32), (100, 700, 129, 0), (2000, 300, 3100, 64)])
+def test_weights_beyond_half_precision(ctx, T, R, d, group, kind):
+    """Steps and offsets are numbers of half precision; the weights they stand for reach 2^20.  Some groups of some rows go
+    there, the others stay as they are."""
+    g = _gen(T + R + d)
+    codes, delta, offset, _, _ = _layer(R, d, group, g)
+    n = delta.shape[1]
+    delta[R // 2, n - 1], offset[R // 2, n - 1] = 65504.0, 65504.0
+    delta[1, 0], offset[1, 0] = 8368.0, -60000.0                  # -60000 .. 65520
+    G = d if group <= 0 or group >= d else group
+    col = torch.arange(d, device="cuda") // G
+    W = offset.double()[:, col] + delta.double()[:, col] * codes.double()
+    P = ctx.obc_pack4(codes, delta, offset, group)
+    dy = (torch.randn(T, R, generator=g, device="cuda") * 1e-3).to(TYPES[kind])
+    dx = ctx.obc_product4_grad(P, dy)
+    ctx.obc_check()
+    want = dy.double() @ W
+    total = dy.double().abs() @ W.abs()
+    assert torch.isfinite(dx[torch.isfinite(want.to(TYPES[kind]))].float()).all()
+    # sums as in the gradients' other tests, weights to 2^-22 and, a 32nd of them being held, 2^-20 of the columns that go there
+    far = (W.abs().amax(0) > 65504.0).double()
+    tiny = 2.0 ** -20 * far * dy.double().abs().sum(1, keepdim=True)
+    bound = (2.0 ** -22 * 1.01 + (6 * R + 64) * U32) * total + tiny + ROUND[kind] * 1.01 * want.abs() + TINY[kind]
+    _within(torch.where(torch.isfinite(dx), dx.double(), want), want, bound)
