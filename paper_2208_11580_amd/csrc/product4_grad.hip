@@ -322,6 +322,14 @@ __global__ __launch_bounds__(BN * 2, 2) void grad_tiles_kernel(Args a, int mtile
 #pragma unroll
         for (int j = 0; j < NF; ++j) w[j] = lds[C::XN + (wave * NF + j) * 64 + lane];
         const uintx4 *const steps = lds + C::XN + C::CN + wave * 32;
+        // fp32: a sum of its own for these 128 rows, added with an fp32 addition: the matrix cores' sums are not rounded to nearest, and
+        // their error grows with the instructions on one sum (500 tokens through 4096 x 2048: 6.4e-7 off in one sum over all rows)
+        floatx4 S[MF][NF];
+        if constexpr (TYPE == OBC_F32)
+#pragma unroll
+            for (int m = 0; m < MF; ++m)
+#pragma unroll
+                for (int j = 0; j < NF; ++j) S[m][j] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const uintx4 step = steps[4 * k + quad], off = steps[16 + 4 * k + quad];
@@ -343,7 +351,7 @@ __global__ __launch_bounds__(BN * 2, 2) void grad_tiles_kernel(Args a, int mtile
 #pragma unroll
                         for (int p = 0; p <= o; ++p)
 #pragma unroll
-                            for (int j = 0; j < NF; ++j) acc[m][j] = mfma_bf16(A[p], B[j][o - p], acc[m][j]);
+                            for (int j = 0; j < NF; ++j) S[m][j] = mfma_bf16(A[p], B[j][o - p], S[m][j]);
                 } else {
                     const uintx4 A = lds[t * 16 + ((4 * k + quad) ^ n)];
 #pragma unroll
@@ -353,6 +361,13 @@ __global__ __launch_bounds__(BN * 2, 2) void grad_tiles_kernel(Args a, int mtile
                 }
             }
         }
+        if constexpr (TYPE == OBC_F32)
+#pragma unroll
+            for (int m = 0; m < MF; ++m)
+#pragma unroll
+                for (int j = 0; j < NF; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[m][j][i] += S[m][j][i];
         __builtin_amdgcn_s_waitcnt(wait_loads(STAGES > 2 ? C::LOADS : 0));      // the next tile is in LDS
         stage_barrier();
     };
@@ -419,7 +434,8 @@ Plan plan_of(const pack4_layout &L, int T, int type)
         return (int64_t)p.mtiles * p.ntiles;
     };
     int64_t tiles = 0;
-    // (fp32: 77 tokens through 2304 x 1283 take 19.4 us in tiles of 32, 20.2 in tiles of 64; 500 through 4096 x 4096 151 and 115)
+    // (fp32 in tiles of 32 and of 64: 77 tokens through 768 x 768 13.7 and 16.3 us, 96 through 700 x 3100 16.7 and 19.3, 77 through
+    // 2304 x 1283 19.4 and 19.2, 96 through 4096 x 4096 48 and 40, 500 151 and 114)
     if (T <= 32 || (type == OBC_F32 && T <= 96)) tiles = cut(32, 128);
     else if (type == OBC_F32) tiles = cut(64, 128);
     // 128 x 256 for three quarters of the compute units and more (2048 x 4096 x 4096 in bf16: 121 us, in tiles of 64 x 128 145; 500 x 4096 x

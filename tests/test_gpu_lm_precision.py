@@ -50,3 +50,16 @@ def test_weights_beyond_half_precision(ctx, T, R, d, group, kind):
     tiny = 2.0 ** -20 * far * dy.double().abs().sum(1, keepdim=True)
     bound = (2.0 ** -22 * 1.01 + (6 * R + 64) * U32) * total + tiny + ROUND[kind] * 1.01 * want.abs() + TINY[kind]
     _within(torch.where(torch.isfinite(dx), dx.double(), want), want, bound)
+
+
+@pytest.mark.parametrize("T,R,d", [(40, 4096, 300), (500, 4096, 2048), (600, 4096, 4096), (1000, 16384, 1024), (64, 16384, 384)])
+def test_fp32_gradients_are_as_exact_as_sums_of_sums_of_128_rows(ctx, T, R, d):
+    """Sums of 128 rows, then the sum of those, each addition rounded to nearest: off by 2^-24 sqrt(128 / 6) and by 2^-24 sqrt(R / 128 / 6)
+    in the mean square."""
+    g = _gen(T + R)
+    for group in (0, 128):
+        codes, delta, offset, W, _ = _layer(R, d, group, g)
+        dy = torch.randn(T, R, generator=g, device="cuda")
+        want = dy.double() @ W
+        err = float((ctx.obc_product4_grad(ctx.obc_pack4(codes, delta, offset, group), dy).double() - want).norm() / want.norm())
+        assert err <= U32 * ((128 / 6) ** 0.5 + (R / 128 / 6) ** 0.5), (group, err)
