@@ -179,7 +179,10 @@ def _vector(t, n, what):
 
 
 class Context:
-    """An obc_ctx bound to a torch stream (default: the current one)."""
+    """An obc_ctx bound to a torch stream (default: the current one).
+
+    Calls that a CUDA graph captures on that stream have their workspaces in the graph's own memory; a graph must not
+    be replayed after the context it was captured from is closed."""
 
     def __init__(self, stream: torch.cuda.Stream | None = None):
         self.lib = load_library()
@@ -207,9 +210,21 @@ class Context:
         if rc != OBC_OK:
             raise ObcError(rc, self.lib.obc_last_error(self.h).decode())
 
+    def _capturing(self):
+        """Whether the context's stream is being captured into a graph."""
+        if torch.cuda.current_stream(self.stream.device) == self.stream:
+            return torch.cuda.is_current_stream_capturing()
+        with torch.cuda.stream(self.stream):
+            return torch.cuda.is_current_stream_capturing()
+
     def workspace(self, nbytes: int) -> torch.Tensor:
-        """A cached device byte buffer of at least nbytes (device memory is torch's job)."""
+        """A cached device byte buffer of at least nbytes (device memory is torch's job).  While the stream is captured: one
+        from the graph's memory, for the caller alone -- a graph keeps its addresses, and the cached buffer is replaced
+        when a later call needs more, or used by eager calls beside a replay."""
         nbytes = max(int(nbytes), 256)
+        if self._capturing():
+            with torch.cuda.stream(self.stream):
+                return torch.empty(nbytes, dtype=torch.uint8, device=self.stream.device)
         if self._ws is None or self._ws.numel() < nbytes:
             if self._ws is not None:
                 # earlier calls queued on the context's stream may still use the old buffer: the
@@ -449,7 +464,7 @@ class Context:
             return torch.empty(shape, dtype=dtype, device=device)
 
     def _need(self, query, *sizes):
-        """Workspace of one of the queries (asked once for each set of sizes): address and bytes."""
+        """Workspace of one of the queries (asked once for each set of sizes): address, bytes, and what keeps it."""
         key = (query,) + sizes
         n = self._needs.get(key)
         if n is None:
@@ -461,13 +476,13 @@ class Context:
                 self._needs.clear()
             n = self._needs[key] = need.value
         if n == 0:
-            return None, 0
+            return None, 0, None
         ws = self._ws
-        if ws is None or ws.numel() < n:
+        if ws is None or ws.numel() < n or self._capturing():
             # like the outputs: memory that the current stream may still use is not for the context's
             with torch.cuda.stream(self.stream):
                 ws = self.workspace(n)
-        return ws.data_ptr(), ws.numel()
+        return ws.data_ptr(), ws.numel(), ws
 
     def obc_group_grid(self, W, bits=4, group=0, live=None, symmetric=False, zero=False):
         """Steps and offsets (R x groups) of a grid of 2^bits values, bits <= 4; group 0: one per row, which
@@ -514,7 +529,7 @@ class Context:
         yp, ldy, rows, n = _rows_of(out, "out")
         if rows != T or n != R:
             raise ValueError("out must be %d x %d" % (T, R))
-        ws, n = self._need("obc_product4_workspace_bytes", T, R, d, group, xt)
+        ws, n, _held = self._need("obc_product4_workspace_bytes", T, R, d, group, xt)
         rc = self.lib.obc_product4(self.h, data.data_ptr(), R, d, group, xp, xt,
                                    None if x_scale is None else _vector(x_scale, T, "x_scale"), T, ldx, yp, _type_of(out, "out"),
                                    ldy, ws, n)
@@ -535,7 +550,7 @@ class Context:
         xp, lddx, rows, n = _rows_of(out, "out")
         if rows != T or n != W.cols:
             raise ValueError("out must be %d x %d" % (T, W.cols))
-        ws, n = self._need("obc_product4_grad_workspace_bytes", T, R, W.cols, W.group, t)
+        ws, n, _held = self._need("obc_product4_grad_workspace_bytes", T, R, W.cols, W.group, t)
         self._ck(self.lib.obc_product4_grad(self.h, W.data.data_ptr(), R, W.cols, W.group, dp, t, T, lddy, xp, lddx, ws, n))
         return out
 
@@ -580,7 +595,7 @@ class Context:
         for other in (dy, dh, dx):
             if other is not None and other.shape != h.shape:
                 raise ValueError("dy, dh and dx must have h's shape")
-        ws, n = self._need("obc_rmsnorm_grad_workspace_bytes", T, d)
+        ws, n, _held = self._need("obc_rmsnorm_grad_workspace_bytes", T, d)
         self._ck(self.lib.obc_rmsnorm_grad(self.h, _ptr(h), _vector(gain, d, "gain"), _vector(rstd, T, "rstd"), _ptr(dy, h.dtype),
                                            _ptr(dh, h.dtype), t, T, d, _ptr(dx, h.dtype), _vector(dgain, d, "dgain"), ws, n))
         return dict(dx=dx, dgain=dgain)
