@@ -321,8 +321,9 @@ int obc_pack4(obc_ctx *ctx, const int32_t *codes, const float *delta, const floa
  *   x   T x d, leading dimension ldx >= d, of x_type; OBC_I8: x stands for x_scale[t] * x[t, c]
  *       (x_scale: T fp32; null for the other types)
  *   y   T x R, leading dimension ldy >= R, of y_type (OBC_F32, OBC_F16 or OBC_BF16)
- * Products and sums have the precision of fp32 (OBC_I8: integer sums within a group, exact) and are rounded once, to
- * y's type.  Rows need no alignment beyond their elements'.  Fixed summation order for a given T, R, d and group.
+ * Products are exact and sums have the precision of fp32 (OBC_I8: integer sums over up to 128 columns of a group, exact;
+ * those are joined in fp32); one rounding, to y's type.  Codes enter the sums as up to 31 times an input: these are to stay
+ * below fp32's 3.4e38.  Rows need no alignment beyond their elements'.  Fixed summation order for a given T, R, d and group.
  * A non-finite input makes its token's outputs non-finite (inf or NaN).  y may not overlap x.
  * ws: obc_product4_workspace_bytes for this T (0 up to 16 tokens, but for few rows of many columns). */
 int obc_product4_workspace_bytes(int T, int R, int d, int group, int x_type, size_t *bytes);

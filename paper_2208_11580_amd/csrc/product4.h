@@ -41,12 +41,13 @@ __device__ inline uintx4 codes_f16(unsigned w)
 
 // A code q as 2 q - 15, exactly, in the same order: the sums have no large common part to take out again.  q >= 8 is 2 k + 1 and q < 8
 // its opposite with k = (q & 7) or 7 - q, of which two permutes look up both bytes.
-__device__ inline uintx4 codes_centred_bf16(unsigned w)
+template <bool HALF>
+__device__ inline uintx4 codes_centred(unsigned w)
 {
     auto four = [](unsigned q, unsigned &first, unsigned &second) {      // a code to a byte
         const unsigned neg = ~q & 0x08080808u, k = (q ^ (neg - (neg >> 3))) & 0x07070707u;
-        const unsigned hi = __builtin_amdgcn_perm(0x41414141u, 0x4040403fu, k) | (neg << 4);
-        const unsigned lo = __builtin_amdgcn_perm(0x70503010u, 0xe0a04080u, k);
+        const unsigned hi = (HALF ? __builtin_amdgcn_perm(0x4b4a4948u, 0x4745423cu, k) : __builtin_amdgcn_perm(0x41414141u, 0x4040403fu, k)) | (neg << 4);
+        const unsigned lo = HALF ? __builtin_amdgcn_perm(0x80808080u, 0u, k) : __builtin_amdgcn_perm(0x70503010u, 0xe0a04080u, k);
         first = __builtin_amdgcn_perm(hi, lo, 0x06020400u);
         second = __builtin_amdgcn_perm(hi, lo, 0x07030501u);
     };

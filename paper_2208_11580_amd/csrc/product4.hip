@@ -4,7 +4,8 @@
 //                                                                           s = sum_{c in g} x[t, c]
 // The codes enter the matrix instructions as the 16-bit numbers 16 + code, exactly (8-bit inputs: as bytes, without
 // the 16), so their products with 16-bit inputs are exact in fp32 and the only roundings are those of the fp32 sums; a
-// group's sums start from zero and are scaled when it ends.  fp32 inputs go in as three bf16 terms, against 2 code - 15.
+// group's sums start from zero and are scaled when it ends.  fp32 inputs go in as three bf16 terms, against 2 code - 15, which also
+// 16-bit inputs meet where the output is fp32.
 //
 // Up to 16 tokens: bound by the weights' bytes (product4_rows_kernel).  One token through 8192 x 8192 takes 9.2 us in half
 // precision, 35.7 MB at 3.9 TB/s (plain reads of 64 MB and more: 6.0 to 6.3); through 768 x 768 3.3 us, of which about 2 are a
@@ -34,6 +35,21 @@ template <int V>
 struct Type {
     static constexpr int value = V;
 };
+
+constexpr bool is_16_bit(int type) { return type == OBC_F16 || type == OBC_BF16; }
+
+// f(Type<y_type>()), for the types that XT and CENTRED come with: 16-bit inputs are centred where the output is fp32
+template <int XT, bool CENTRED, class F>
+__device__ inline void with_output_type(int y_type, F f)
+{
+    if constexpr (is_16_bit(XT) && CENTRED) {
+        f(Type<OBC_F32>());
+    } else {
+        if (!is_16_bit(XT) && y_type == OBC_F32) f(Type<OBC_F32>());
+        else if (y_type == OBC_F16) f(Type<OBC_F16>());
+        else f(Type<OBC_BF16>());
+    }
+}
 
 // One 16x16x32 operand of token rows: the lane's eight columns from `c` on of row `row`, zeros from d on.
 template <int XT>
@@ -106,27 +122,28 @@ struct Operand<OBC_I8> {
     }
 };
 
-// What stands for a code q in XT's operands is q / unit + base.  fp32 inputs: 2 q - 15, which costs their unpacking three times the
-// instructions (22 for eight codes, 8 for 16 + q) but next to six matrix instructions and more: the matrix cores' sums are not rounded to
-// nearest, and their error grows with the sums' size, five times as large with 16 + q.  (100 tokens through 300 x 128: 1.1e-6 off with 16 + q,
-// 1.1e-7 with 2 q - 15; 40 through 512 x 16384 3.4e-6 and 1.6e-7; 500 through 4096 x 4096 take 75 us, 67 with 16 + q.)  16-bit outputs
-// hide either.
-template <int XT>
-constexpr float kUnit = XT == OBC_F32 ? 0.5f : 1.f;
-template <int XT>
-constexpr float kBase = XT == OBC_F32 ? -7.5f : XT == OBC_I8 ? 0.f : kCodeBase;      // base times unit
+// What stands for a code q in XT's operands is q / unit + base.  CENTRED, for fp32 inputs and fp32 outputs: 2 q - 15, which costs the
+// unpacking three times the instructions (22 for eight codes, 8 for 16 + q): the matrix cores' sums are not rounded to nearest, and their
+// error grows with the sums' size, five times as large with 16 + q.  (fp32 inputs, 100 tokens through 300 x 128: 1.1e-6 off with 16 + q,
+// 1.1e-7 with 2 q - 15; 40 through 512 x 16384 3.4e-6 and 1.6e-7; 500 through 4096 x 4096 take 75 us, 67 with 16 + q.  fp16
+// inputs, fp32 outputs, 40 through 512 x 16384: 1.0e-7 off, with 16 + q six times as much; one token through 8192 x 8192 takes 11.3 us,
+// with 16 + q 9.4, 2048 through 4096 x 4096 90 and 77.)  16-bit outputs hide either.
+template <int XT, bool CENTRED>
+constexpr float kUnit = CENTRED ? 0.5f : 1.f;
+template <int XT, bool CENTRED>
+constexpr float kBase = CENTRED ? -7.5f : XT == OBC_I8 ? 0.f : kCodeBase;      // base times unit
 
-template <int XT>
+template <int XT, bool CENTRED>
 __device__ inline uintx4 codes_of(unsigned w)
 {
-    return XT == OBC_F32 ? codes_centred_bf16(w) : XT == OBC_F16 ? codes_f16(w) : codes_bf16(w);
+    return CENTRED ? codes_centred<XT == OBC_F16>(w) : XT == OBC_F16 ? codes_f16(w) : codes_bf16(w);
 }
 
 // Codes of one instruction and ones, as the operand that meets XT's.
-template <int XT>
+template <int XT, bool CENTRED>
 struct Codes {
     uintx4 v;
-    __device__ explicit Codes(unsigned w) : v(codes_of<XT>(w)) {}
+    __device__ explicit Codes(unsigned w) : v(codes_of<XT, CENTRED>(w)) {}
     static __device__ Codes ones()
     {
         Codes c(0);
@@ -137,7 +154,7 @@ struct Codes {
 };
 
 template <>
-struct Codes<OBC_I8> {
+struct Codes<OBC_I8, false> {
     uintx2 v;
     __device__ explicit Codes(unsigned w) : v(codes_i8(w)) {}
     static __device__ Codes ones()
@@ -151,7 +168,8 @@ struct Codes<OBC_I8> {
 template <int XT>
 struct Sum {
     floatx4 s = {0.f, 0.f, 0.f, 0.f};
-    __device__ void add(const Operand<XT> &a, const Codes<XT> &b)
+    template <bool CENTRED>
+    __device__ void add(const Operand<XT> &a, const Codes<XT, CENTRED> &b)
     {
         if constexpr (XT == OBC_F32) {
             s = mfma_bf16(a.v[2], b.v, s);
@@ -169,7 +187,7 @@ struct Sum {
 template <>
 struct Sum<OBC_I8> {
     intx4 s = {0, 0, 0, 0};
-    __device__ void add(const Operand<OBC_I8> &a, const Codes<OBC_I8> &b) { s = mfma_i8(a.v, b.v, s); }
+    __device__ void add(const Operand<OBC_I8> &a, const Codes<OBC_I8, false> &b) { s = mfma_i8(a.v, b.v, s); }
     __device__ float operator[](int i) const { return (float)s[i]; }
 };
 
@@ -194,7 +212,7 @@ constexpr int tile_bytes(int XT) { return XT == OBC_F32 ? 768 : XT == OBC_I8 ? 1
 // weights' bytes bound it: a wave has its next tile's codes on their way (two or three ahead measured slower, 9.9 and 11.3 us against
 // 9.2 for one token through 8192 x 8192: 16 waves to a compute unit cover the rest, and the copies cost instructions).  Loads come back
 // in order, so the tokens must not be among them: they go through LDS, `chunk` tiles at a time.
-template <int XT, int SUB, int NF>
+template <int XT, bool CENTRED, int SUB, int NF>
 __global__ __launch_bounds__(rows_waves(XT) * 64) void product4_rows_kernel(Args a, int y_type, int chunk)
 {
     constexpr int P = XT == OBC_F32 ? 3 : 1, OPS = XT == OBC_I8 ? 8 : 16;      // planes; 16-byte places of a token's tile
@@ -211,7 +229,7 @@ __global__ __launch_bounds__(rows_waves(XT) * 64) void product4_rows_kernel(Args
     for (int j = 0; j < NF; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
-    const Codes<XT> ones = Codes<XT>::ones();
+    const auto ones = Codes<XT, CENTRED>::ones();
     struct Weights {
         uintx4 w[NF];
         unsigned sc[NF][SUB];
@@ -306,13 +324,13 @@ __global__ __launch_bounds__(rows_waves(XT) * 64) void product4_rows_kernel(Args
             for (int k = u * 4 / SUB; k < (u + 1) * 4 / SUB; ++k) {
                 s.add(x[k], ones);
 #pragma unroll
-                for (int j = 0; j < NF; ++j) S[j].add(x[k], Codes<XT>(g.w[j][k]));
+                for (int j = 0; j < NF; ++j) S[j].add(x[k], Codes<XT, CENTRED>(g.w[j][k]));
             }
 #pragma unroll
             for (int j = 0; j < NF; ++j) {
-                const float step = half_lo(g.sc[j][u]), off = half_hi(g.sc[j][u]) - kBase<XT> * step;
+                const float step = half_lo(g.sc[j][u]), off = half_hi(g.sc[j][u]) - kBase<XT, CENTRED> * step;
 #pragma unroll
-                for (int v = 0; v < 4; ++v) acc[j][v] = fmaf(step * kUnit<XT>, S[j][v], fmaf(off, s[v], acc[j][v]));
+                for (int v = 0; v < 4; ++v) acc[j][v] = fmaf(step * kUnit<XT, CENTRED>, S[j][v], fmaf(off, s[v], acc[j][v]));
             }
         }
     };
@@ -344,9 +362,7 @@ __global__ __launch_bounds__(rows_waves(XT) * 64) void product4_rows_kernel(Args
         for (int w = 0; w < waves; ++w) v += part[w * (NF * 256) + e];
         if (XT == OBC_I8) v *= a.xs[to];
         const int64_t at = (int64_t)to * a.ldy + r;
-        if (y_type == OBC_F32) store_as<OBC_F32>(a.y, at, v);
-        else if (y_type == OBC_F16) store_as<OBC_F16>(a.y, at, v);
-        else store_as<OBC_BF16>(a.y, at, v);
+        with_output_type<XT, CENTRED>(y_type, [&](auto type) { store_as<decltype(type)::value>(a.y, at, v); });
     }
 }
 
@@ -456,11 +472,11 @@ struct Tile {
     static_assert(XN % (64 * WAVES) == 0 && WN16 % (64 * WAVES) == 0, "whole loads");
 };
 
-template <int XT, int SUB, int BM, int BN, int WM, int STAGES>
+template <int XT, bool CENTRED, int SUB, int BM, int BN, int WM, int STAGES>
 __global__ __launch_bounds__(tile_waves(BN) * 64, 2) void product4_tiles_kernel(Args a, Tokens tok, int y_type)
 {
     using C = Tile<XT, SUB, BM, BN, WM, STAGES>;
-    constexpr int P = C::P, MF = C::MF, NF = C::NF, ROW = C::ROW, WN = C::WN;
+    constexpr int P = C::P, MF = C::MF, NF = C::NF, ROW = C::ROW;
     // separate arrays: the compiler then knows that reading one does not wait for loads to another
     __shared__ uintx4 lds0[C::PLACES], lds1[C::PLACES], lds2[STAGES > 2 ? C::PLACES : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -527,7 +543,7 @@ __global__ __launch_bounds__(tile_waves(BN) * 64, 2) void product4_tiles_kernel(
                     const int g = g0 + 8 * quad + e;
                     unsigned sc = 0;
                     if (g < a.NG) sc = SUB > 1 ? a.scales[((rb * a.KT + g / SUB) * 16 + n) * SUB + g % SUB] : a.scales[(rb * a.NG + g) * 16 + n];
-                    v[e] = half_hi(sc) - kBase<XT> * half_lo(sc);
+                    v[e] = half_hi(sc) - kBase<XT, CENTRED> * half_lo(sc);
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -567,7 +583,7 @@ __global__ __launch_bounds__(tile_waves(BN) * 64, 2) void product4_tiles_kernel(
             w[j] = lds[C::XN + (wn * NF + j) * 64 + lane];
 #pragma unroll
             for (int u = 0; u < SUB; ++u)
-                step[j][u] = kUnit<XT> * half_lo(((const unsigned *)(lds + C::XN + C::WN16))[C::step_at(((wn * NF + j) * 16 + n) * SUB + u)]);
+                step[j][u] = kUnit<XT, CENTRED> * half_lo(((const unsigned *)(lds + C::XN + C::WN16))[C::step_at(((wn * NF + j) * 16 + n) * SUB + u)]);
         }
         if constexpr (XT == OBC_I8) {
 #pragma unroll
@@ -625,7 +641,7 @@ __global__ __launch_bounds__(tile_waves(BN) * 64, 2) void product4_tiles_kernel(
                 for (int k = u * 4 / SUB; k < (u + 1) * 4 / SUB; ++k) {
                     uintx4 B[NF];
 #pragma unroll
-                    for (int j = 0; j < NF; ++j) B[j] = codes_of<XT>(w[j][k]);
+                    for (int j = 0; j < NF; ++j) B[j] = codes_of<XT, CENTRED>(w[j][k]);
 #pragma unroll
                     for (int m = 0; m < MF; ++m)
 #pragma unroll
@@ -678,9 +694,7 @@ __global__ __launch_bounds__(tile_waves(BN) * 64, 2) void product4_tiles_kernel(
                 }
             }
     };
-    if (y_type == OBC_F32) put(Type<OBC_F32>());
-    else if (y_type == OBC_F16) put(Type<OBC_F16>());
-    else put(Type<OBC_BF16>());
+    with_output_type<XT, CENTRED>(y_type, put);
 }
 
 // The slices' sums, in their order.
@@ -777,26 +791,26 @@ void launch_lay(obc_ctx *ctx, const Args &a, const Lay &lay)
     else product4_lay_kernel<XT, 64><<<blocks(64), 256, 0, ctx->stream>>>(a, lay);
 }
 
-template <int XT, int SUB, int BM, int BN, int WM, int STAGES>
+template <int XT, bool CENTRED, int SUB, int BM, int BN, int WM, int STAGES>
 void launch_tiles(obc_ctx *ctx, const Args &a, const Tokens &tok, int y_type, int slices)
 {
-    product4_tiles_kernel<XT, SUB, BM, BN, WM, STAGES>
+    product4_tiles_kernel<XT, CENTRED, SUB, BM, BN, WM, STAGES>
         <<<(unsigned)(tok.tiles * slices), tile_waves(BN) * 64, 0, ctx->stream>>>(a, tok, y_type);
 }
 
-template <int XT, int SUB, int NF>
+template <int XT, bool CENTRED, int SUB, int NF>
 void launch_rows(obc_ctx *ctx, const Args &a, int y_type, int waves, int chunk)
 {
     const size_t tokens = (size_t)chunk * a.T * tile_bytes(XT), sums = (size_t)waves * NF * 1024;
-    product4_rows_kernel<XT, SUB, NF><<<(a.RB + NF - 1) / NF, waves * 64, tokens > sums ? tokens : sums, ctx->stream>>>(a, y_type, chunk);
+    product4_rows_kernel<XT, CENTRED, SUB, NF><<<(a.RB + NF - 1) / NF, waves * 64, tokens > sums ? tokens : sums, ctx->stream>>>(a, y_type, chunk);
 }
 
-template <int XT, int SUB>
+template <int XT, bool CENTRED, int SUB>
 int launch(obc_ctx *ctx, const Args &a, int y_type, const Rows *rows, const Plan &p, void *ws)
 {
     if (rows) {
-        if (rows->NF == 2) launch_rows<XT, SUB, 2>(ctx, a, y_type, rows->waves, rows->chunk);
-        else launch_rows<XT, SUB, 1>(ctx, a, y_type, rows->waves, rows->chunk);
+        if (rows->NF == 2) launch_rows<XT, CENTRED, SUB, 2>(ctx, a, y_type, rows->waves, rows->chunk);
+        else launch_rows<XT, CENTRED, SUB, 1>(ctx, a, y_type, rows->waves, rows->chunk);
         OBC_LAUNCH_CHECK(ctx, "product4_rows_kernel");
         return OBC_OK;
     }
@@ -823,12 +837,12 @@ int launch(obc_ctx *ctx, const Args &a, int y_type, const Rows *rows, const Plan
     tok.per = p.per;
     tok.part = p.slices > 1 ? (float *)((char *)ws + p.part) : nullptr;
     if constexpr (XT == OBC_F32) {
-        if (p.BM == 32) launch_tiles<XT, SUB, 32, 128, 1, 2>(ctx, a, tok, y_type, p.slices);
-        else launch_tiles<XT, SUB, 64, 128, 1, 2>(ctx, a, tok, y_type, p.slices);
+        if (p.BM == 32) launch_tiles<XT, CENTRED, SUB, 32, 128, 1, 2>(ctx, a, tok, y_type, p.slices);
+        else launch_tiles<XT, CENTRED, SUB, 64, 128, 1, 2>(ctx, a, tok, y_type, p.slices);
     } else {
-        if (p.BM == 32) launch_tiles<XT, SUB, 32, 128, 1, 3>(ctx, a, tok, y_type, p.slices);
-        else if (p.BM == 64) launch_tiles<XT, SUB, 64, 128, 1, 3>(ctx, a, tok, y_type, p.slices);
-        else launch_tiles<XT, SUB, 128, 256, 2, 3>(ctx, a, tok, y_type, p.slices);
+        if (p.BM == 32) launch_tiles<XT, CENTRED, SUB, 32, 128, 1, 3>(ctx, a, tok, y_type, p.slices);
+        else if (p.BM == 64) launch_tiles<XT, CENTRED, SUB, 64, 128, 1, 3>(ctx, a, tok, y_type, p.slices);
+        else launch_tiles<XT, CENTRED, SUB, 128, 256, 2, 3>(ctx, a, tok, y_type, p.slices);
     }
     OBC_LAUNCH_CHECK(ctx, "product4_tiles_kernel");
     if (p.slices > 1) {
@@ -838,10 +852,12 @@ int launch(obc_ctx *ctx, const Args &a, int y_type, const Rows *rows, const Plan
     return OBC_OK;
 }
 
-template <int XT>
+template <int XT, bool CENTRED>
 int launch_sub(obc_ctx *ctx, const Args &a, int sub, int y_type, const Rows *rows, const Plan &p, void *ws)
 {
-    return sub == 1 ? launch<XT, 1>(ctx, a, y_type, rows, p, ws) : sub == 2 ? launch<XT, 2>(ctx, a, y_type, rows, p, ws) : launch<XT, 4>(ctx, a, y_type, rows, p, ws);
+    return sub == 1   ? launch<XT, CENTRED, 1>(ctx, a, y_type, rows, p, ws)
+           : sub == 2 ? launch<XT, CENTRED, 2>(ctx, a, y_type, rows, p, ws)
+                      : launch<XT, CENTRED, 4>(ctx, a, y_type, rows, p, ws);
 }
 
 }  // namespace
@@ -893,11 +909,12 @@ int obc_product4(obc_ctx *ctx, const void *packed, int R, int d, int group, cons
     a.tpg_inv = L.tpg > 1 ? (unsigned)(0x100000000ull / (unsigned)L.tpg) + 1u : 0u;
     a.tpg_one = L.tpg > 1 ? 0u : ~0u;
     a.ldx = ldx; a.ldy = ldy;
+    const bool fp32 = y_type == OBC_F32;
     switch (x_type) {
-    case OBC_F32: return launch_sub<OBC_F32>(ctx, a, L.SUB, y_type, rows, p, ws);
-    case OBC_F16: return launch_sub<OBC_F16>(ctx, a, L.SUB, y_type, rows, p, ws);
-    case OBC_BF16: return launch_sub<OBC_BF16>(ctx, a, L.SUB, y_type, rows, p, ws);
-    default: return launch_sub<OBC_I8>(ctx, a, L.SUB, y_type, rows, p, ws);
+    case OBC_F32: return launch_sub<OBC_F32, true>(ctx, a, L.SUB, y_type, rows, p, ws);
+    case OBC_F16: return fp32 ? launch_sub<OBC_F16, true>(ctx, a, L.SUB, y_type, rows, p, ws) : launch_sub<OBC_F16, false>(ctx, a, L.SUB, y_type, rows, p, ws);
+    case OBC_BF16: return fp32 ? launch_sub<OBC_BF16, true>(ctx, a, L.SUB, y_type, rows, p, ws) : launch_sub<OBC_BF16, false>(ctx, a, L.SUB, y_type, rows, p, ws);
+    default: return launch_sub<OBC_I8, false>(ctx, a, L.SUB, y_type, rows, p, ws);
     }
 }
 

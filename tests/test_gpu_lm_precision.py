@@ -3,7 +3,7 @@ full, fp32 results over long sums, grids and norms at the ends of their ranges."
 import pytest
 import torch
 
-from .test_gpu_lm import ROUND, TINY, TYPES, U32, _gen, _layer, _within, ctx  # noqa: F401
+from .test_gpu_lm import ROUND, TINY, TYPES, U32, _gen, _layer, _product_bound, _within, ctx  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -63,3 +63,20 @@ def test_fp32_gradients_are_as_exact_as_sums_of_sums_of_128_rows(ctx, T, R, d):
         want = dy.double() @ W
         err = float((ctx.obc_product4_grad(ctx.obc_pack4(codes, delta, offset, group), dy).double() - want).norm() / want.norm())
         assert err <= U32 * ((128 / 6) ** 0.5 + (R / 128 / 6) ** 0.5), (group, err)
+
+
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("T,d", [(1, 128), (3, 8192), (16, 1000), (40, 300), (40, 8192), (100, 128), (100, 2000)])
+def test_16_bit_inputs_with_fp32_outputs_are_as_exact_as_fp32(ctx, T, d, kind):
+    """Sums of 128 columns, then the sum of those, each addition rounded to nearest: off by 2^-24 sqrt(128 / 6) and by
+    2^-24 sqrt(d / 128 / 6) in the mean square."""
+    g = _gen(T + d)
+    for R, group in ((300, 0), (300, 32), (300, 64), (4500, 128)):
+        codes, delta, offset, W, mag = _layer(R, d, group, g)
+        x = torch.randn(T, d, generator=g, device="cuda").to(TYPES[kind])
+        want = x.double() @ W.T
+        y = ctx.obc_product4(ctx.obc_pack4(codes, delta, offset, group), x, out_dtype=torch.float32)
+        err = float((y.double() - want).norm() / want.norm())
+        assert err <= U32 * ((128 / 6) ** 0.5 + (d / 128 / 6) ** 0.5), (R, group, err)
+        _within(y, want, _product_bound(x, mag, want, "f32", d))
+    ctx.obc_check()
