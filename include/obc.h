@@ -324,7 +324,8 @@ int obc_pack4(obc_ctx *ctx, const int32_t *codes, const float *delta, const floa
  * Products are exact and sums have the precision of fp32 (OBC_I8: integer sums over up to 128 columns of a group, exact;
  * those are joined in fp32); one rounding, to y's type.  Codes enter the sums as up to 31 times an input: these are to stay
  * below fp32's 3.4e38.  Rows need no alignment beyond their elements'.  Fixed summation order for a given T, R, d and group.
- * A non-finite input makes its token's outputs non-finite (inf or NaN).  y may not overlap x.
+ * A non-finite input makes its token's outputs non-finite (inf or NaN).  y may not overlap x.  Where a row has several
+ * groups, ceil(d / 128) * (group / 128) has to be below 2^32 (OBC_ERR_BAD_SHAPE).
  * ws: obc_product4_workspace_bytes for this T (0 up to 16 tokens, but for few rows of many columns). */
 int obc_product4_workspace_bytes(int T, int R, int d, int group, int x_type, size_t *bytes);
 int obc_product4(obc_ctx *ctx, const void *packed, int R, int d, int group, const void *x, int x_type,

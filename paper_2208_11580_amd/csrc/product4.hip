@@ -24,10 +24,10 @@ struct Args {
     const float *xs;
     void *y;
     int T, R, d, RB, KT, NG, tpg;
-    unsigned tpg_inv, tpg_one;      // floor(2^32 / tpg) + 1 and 0; for tpg = 1, 0 and all ones
+    unsigned tpg_inv, tpg_one;      // floor(2^32 / tpg) + 1 and 0; for tpg = 1, 0 and all ones; for one group, 0 and 0
     int64_t ldx, ldy;
 
-    // kt / tpg: exact while kt tpg < 2^32 (a row of 8 million columns)
+    // kt / tpg: exact while kt tpg < 2^32, beyond which a call with several groups is refused (rows of 8 million columns and more)
     __device__ int group_of(int kt) const { return (int)(__umulhi((unsigned)kt, tpg_inv) + ((unsigned)kt & tpg_one)); }
 };
 
@@ -884,6 +884,8 @@ int obc_product4(obc_ctx *ctx, const void *packed, int R, int d, int group, cons
     pack4_layout L;
     if (!pack4_layout_of(R, d, group, &L))
         return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_product4: group (%d) is not 0, 32, 64 or a multiple of 128", group);
+    if (L.NG > 1 && (int64_t)L.KT * L.tpg >= (int64_t)1 << 32)
+        return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_product4: groups of %d columns in rows of %d", group, d);
     if (ldx < d || ldy < R) return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_product4: leading dimension below the row's length");
     if (T == 0 || R == 0) return OBC_OK;
     if (!packed || !x || !y) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_product4: null argument");
@@ -906,8 +908,8 @@ int obc_product4(obc_ctx *ctx, const void *packed, int R, int d, int group, cons
     a.scales = (const unsigned *)((const char *)packed + L.scales);
     a.x = x; a.xs = x_scale; a.y = y;
     a.T = T; a.R = R; a.d = d; a.RB = L.RB; a.KT = L.KT; a.NG = L.NG; a.tpg = L.tpg;
-    a.tpg_inv = L.tpg > 1 ? (unsigned)(0x100000000ull / (unsigned)L.tpg) + 1u : 0u;
-    a.tpg_one = L.tpg > 1 ? 0u : ~0u;
+    a.tpg_inv = L.tpg > 1 && L.NG > 1 ? (unsigned)(0x100000000ull / (unsigned)L.tpg) + 1u : 0u;
+    a.tpg_one = L.tpg > 1 || L.NG == 1 ? 0u : ~0u;
     a.ldx = ldx; a.ldy = ldy;
     const bool fp32 = y_type == OBC_F32;
     switch (x_type) {
