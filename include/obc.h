@@ -348,9 +348,11 @@ int obc_product4_grad(obc_ctx *ctx, const void *packed, int R, int d, int group,
  *            nullable (not written), h == x or h == residual allowed.  The norm is of the unrounded sum.
  *   gain     d, fp32
  *   y        T x d of y_type: x_type or OBC_I8; OBC_I8: y stands for y_scale[t] * y[t, c], y_scale[t] =
- *            max|y| / 127 (1 for a row of zeros; NaN, and codes 0, for a row with a NaN or an infinity)
+ *            max|y| / 127 (1 for a row of zeros; NaN, and codes 0, for a row with a NaN or an infinity, also where
+ *            the gain brings it in)
  *   y_scale  T fp32 out, with OBC_I8;  rstd  nullable, T fp32 out: 1 / sqrt(mean(h^2) + eps)
- * Squares are summed in fp32.  1 <= d <= 65536. */
+ * Squares are summed in fp32: values beyond about 1e19 give a row of zeros, in 8 bits scale NaN and codes 0.
+ * 1 <= d <= 65536. */
 int obc_rmsnorm(obc_ctx *ctx, const void *x, const void *residual, int x_type, const float *gain, float eps, int T,
                 int d, void *h, void *y, int y_type, float *y_scale, float *rstd);
 

@@ -100,14 +100,21 @@ struct Eight {
     }
 };
 
-// Sum (and maximum) over a workgroup, the same value in every thread.
+// The larger of two magnitudes; an infinity or a NaN is larger than any number (as their bits are), where fmaxf would drop the NaN.
+__device__ inline float larger(float top, float v)
+{
+    const unsigned a = __builtin_bit_cast(unsigned, top), b = __builtin_bit_cast(unsigned, v) & 0x7fffffffu;
+    return __builtin_bit_cast(float, a > b ? a : b);
+}
+
+// Sum (and largest magnitude) over a workgroup, the same value in every thread.
 template <int NT, bool MAX>
 __device__ inline void reduce(float &sum, float &top, float (*buf)[2])
 {
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) {
         sum += __shfl_xor(sum, off, 64);
-        if (MAX) top = fmaxf(top, __shfl_xor(top, off, 64));
+        if (MAX) top = larger(top, __shfl_xor(top, off, 64));
     }
     if (NT == 64) return;
     const int wave = threadIdx.x >> 6;
@@ -121,7 +128,7 @@ __device__ inline void reduce(float &sum, float &top, float (*buf)[2])
 #pragma unroll
     for (int w = 1; w < NT / 64; ++w) {
         sum += buf[w][0];
-        if (MAX) top = fmaxf(top, buf[w][1]);
+        if (MAX) top = larger(top, buf[w][1]);
     }
 }
 
@@ -159,7 +166,7 @@ __global__ __launch_bounds__(NT) void rmsnorm_kernel(NormArgs a)
         for (int j = 0; j < 8; ++j) {
             sum = fmaf(v[k][j], v[k][j], sum);
             v[k][j] *= g[j];
-            if (Q8) top = fmaxf(top, fabsf(v[k][j]));
+            if (Q8) top = larger(top, v[k][j]);
         }
     }
     reduce<NT, Q8>(sum, top, buf);

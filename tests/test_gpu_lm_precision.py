@@ -80,3 +80,17 @@ def test_16_bit_inputs_with_fp32_outputs_are_as_exact_as_fp32(ctx, T, d, kind):
         assert err <= U32 * ((128 / 6) ** 0.5 + (d / 128 / 6) ** 0.5), (R, group, err)
         _within(y, want, _product_bound(x, mag, want, "f32", d))
     ctx.obc_check()
+
+
+def test_8_bit_norm_of_a_gain_that_is_not_finite(ctx):
+    """A NaN in the gain (or an infinite gain, also where h is zero) leaves no 8-bit values: scale NaN, codes 0."""
+    for kind in TYPES:
+        for d in (8, 500, 5000, 20000):
+            for value in (float("nan"), float("inf")):
+                g = _gen(d)
+                x = torch.randn(4, d, generator=g, device="cuda").to(TYPES[kind])
+                x[2, d - 3] = 0
+                gain = torch.ones(d, device="cuda")
+                gain[d - 3] = value
+                q = ctx.obc_rmsnorm(x, gain, quant8=True)
+                assert torch.isnan(q["scale"]).all() and not q["y"].any(), (kind, d, value)
