@@ -5,12 +5,16 @@
 
 namespace {
 
+__device__ inline _Float16 next_half(_Float16 h)
+{
+    return __builtin_bit_cast(_Float16, (unsigned short)(__builtin_bit_cast(unsigned short, h) + 1));
+}
+
 // |v| in half precision, rounded away from zero or towards it
 __device__ inline float half_up(float v)
 {
-    _Float16 h = (_Float16)v;
-    if ((float)h < v) h = __builtin_bit_cast(_Float16, (unsigned short)(__builtin_bit_cast(unsigned short, h) + 1));
-    return (float)h;
+    const _Float16 h = (_Float16)v;
+    return (float)((float)h < v ? next_half(h) : h);
 }
 
 __device__ inline float half_down(float v)
@@ -82,7 +86,11 @@ __global__ __launch_bounds__(256) void group_grid_kernel(const float *__restrict
             }
         } else {
             off = lo < 0.f ? -half_up(-lo) : half_down(lo);
-            if (hi > off) step = half_up((hi - off) / q);
+            if (hi > off) {
+                step = half_up((hi - off) / q);
+                // (the range, rounded down, may have been such a number times q)
+                if ((double)off + (double)q * step < (double)hi) step = (float)next_half((_Float16)step);
+            }
         }
         bad = !(step <= 65504.f) || !(fabsf(off) <= 65504.f);
     }

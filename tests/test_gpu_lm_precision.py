@@ -94,3 +94,15 @@ def test_8_bit_norm_of_a_gain_that_is_not_finite(ctx):
                 gain[d - 3] = value
                 q = ctx.obc_rmsnorm(x, gain, quant8=True)
                 assert torch.isnan(q["scale"]).all() and not q["y"].any(), (kind, d, value)
+
+
+def test_grids_cover_weights_whose_range_rounds_down(ctx):
+    """The range of these groups is rounded down in fp32, to fifteen times a number of half precision."""
+    W = torch.tensor([[-1.0, 0.875 + 2.0 ** -24], [-1.0, 0.875 - 2.0 ** -24], [-2.0, 1.75 + 2.0 ** -23], [0.0, 1.875 + 2.0 ** -23]],
+                     device="cuda")
+    for group in (0, 32):
+        delta, offset, maxq = ctx.obc_group_grid(W, 4, group)
+        ctx.obc_check()
+        top = offset.double() + maxq * delta.double()
+        assert (offset.double() <= W.double()).all() and (W.double() <= top).all(), (W.double() - top)
+        assert (delta <= 0.1252 * torch.tensor([[1.0], [1.0], [2.0], [1.0]], device="cuda")).all()
