@@ -178,6 +178,15 @@ def _vector(t, n, what):
     return t.data_ptr()
 
 
+def _no_grad(*tensors):
+    """Results are new to autograd, which would take a gradient that ends here for none."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError("an argument requires a gradient, which these calls do not record: detach it, or call under "
+                                 "torch.no_grad(), and call the operator's own gradient")
+
+
 class Context:
     """An obc_ctx bound to a torch stream (default: the current one).
 
@@ -518,6 +527,7 @@ class Context:
         """y = x W^T (T x rows) of a Packed4.  x: T x cols, fp32, fp16, bf16, or int8 with its scales (T).  y has
         out's type, else out_dtype, else x's (int8: bf16)."""
         data, R, cols, group = W
+        _no_grad(x, x_scale, out)
         xt = _type_of(x, "x", i8=True)
         xp, ldx, T, d = _rows_of(x, "x")
         if d != cols:
@@ -539,6 +549,7 @@ class Context:
 
     def obc_product4_grad(self, W, dy, out=None):
         """dx = dy W (T x cols), the gradient of obc_product4's inputs, in dy's type."""
+        _no_grad(dy, out)
         t = _type_of(dy, "dy")
         dp, lddy, T, R = _rows_of(dy, "dy")
         if R != W.rows:
@@ -560,6 +571,7 @@ class Context:
         T, d = x.shape
         t = _type_of(x, "x")
         out = {} if out is None else out
+        _no_grad(x, gain, residual, *out.values())
         h = out.get("h")
         if h is None and residual is not None:
             h = self._empty((T, d), x.dtype, x.device)
@@ -586,6 +598,7 @@ class Context:
         T, d = h.shape
         t = _type_of(h, "h")
         out = {} if out is None else out
+        _no_grad(h, gain, rstd, dy, dh, *out.values())
         dx = out.get("dx")
         if dx is None:
             dx = self._empty((T, d), h.dtype, h.device)
@@ -606,6 +619,7 @@ class Context:
         t = _type_of(z, "z")
         zp, ldz, T, V = _rows_of(z, "z")
         out = {} if out is None else out
+        _no_grad(z, top_logit, weight, *out.values())
         loss = out.get("loss")
         if loss is None:
             loss = self._empty((T,), torch.float32, z.device)
