@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from . import test_gpu_lm as lm
-from .test_gpu_lm import ROUND, TINY, U32, _gen, _logits, _within, ctx  # noqa: F401
+from .test_gpu_lm import ROUND, TINY, TYPES, U32, _gen, _layer, _logits, _product_bound, _within, ctx  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -57,13 +57,39 @@ def test_products_of_8_bit_prompts(ctx, d, group, out):
 
 @pytest.mark.parametrize("kind", ["f32", "f16", "bf16", "i8"])
 @pytest.mark.parametrize("T,R,d,group", [(1, 4200, 1283, 128), (5, 4200, 1283, 64), (16, 5000, 1283, 32), (7, 5000, 640, 0), (3, 4100, 2049, 256),
-                                         (16, 6500, 1283, 128), (16, 6500, 8192, 32), (13, 6500, 5000, 64)])
+                                         (16, 6500, 1283, 128), (16, 6500, 8192, 32), (13, 6500, 5000, 64), (16, 6500, 9300, 64)])
 def test_few_tokens_through_many_rows(ctx, T, R, d, group, kind):
-    """32 rows of weights to a workgroup; the last three also with tokens that do not fit in LDS at once (fp32, 16 bits)."""
+    """32 rows of weights to a workgroup; the last four also with tokens that do not fit in LDS at once (the last in any type)."""
     if kind == "i8":
         lm.test_product_of_8_bit_inputs(ctx, T, R, d, group, "f32")
     else:
         lm.test_product(ctx, T, R, d, group, kind)
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16", "i8"])
+@pytest.mark.parametrize("T,R,d,group", [(30, 500, 1283, 32), (18, 333, 1290, 64), (31, 200, 2049, 128)])
+def test_up_to_32_tokens(ctx, T, R, d, group, kind):
+    if kind == "i8":
+        lm.test_product_of_8_bit_inputs(ctx, T, R, d, group, "f16")
+    else:
+        lm.test_product(ctx, T, R, d, group, kind)
+
+
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("T,R,d,group", [(2000, 3300, 1283, 0), (2000, 3300, 1283, 32), (2000, 3300, 1290, 64), (2000, 3300, 1280, 128),
+                                         (100, 500, 1283, 32), (100, 500, 1283, 64), (30, 500, 1283, 32), (30, 500, 1283, 64),
+                                         (16, 6500, 8192, 32), (5, 4200, 1283, 64), (7, 5000, 640, 0), (3, 300, 1283, 64), (3, 300, 1283, 32)])
+def test_16_bit_inputs_into_fp32(ctx, T, R, d, group, kind):
+    g = _gen(T + R + d)
+    codes, delta, offset, W, mag = _layer(R, d, group, g)
+    x = torch.randn(T, d, generator=g, device="cuda").to(TYPES[kind])
+    y = ctx.obc_product4(ctx.obc_pack4(codes, delta, offset, group), x, out_dtype=torch.float32)
+    ctx.obc_check()
+    want = x.double() @ W.T
+    _within(y, want, _product_bound(x, mag, want, "f32", d))
+    # sums of 128 columns, and the sum of those, each addition rounded to nearest
+    err = float((y.double() - want).norm() / want.norm())
+    assert err <= U32 * ((128 / 6) ** 0.5 + (d / 128 / 6) ** 0.5), err
 
 
 @pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
