@@ -1,6 +1,6 @@
 // obc_group_grid and obc_pack4: the grid of every group of a layer's columns, and the layer's codes in the
-// order in which the products' matrix instructions take them (pack4.h).  Once per layer; bound by the 32-bit codes that are read
-// (8192 x 8192: 167 us, 1.8 TB/s; the grid of its groups of 128 155 us).
+// order in which the products' matrix instructions take them (pack4.h).  Once per layer, at a third of the
+// rate of a copy: loads of four bytes, few of them on their way (8192 x 8192: 167 us, 1.8 TB/s; the grid of its groups of 128 160 us).
 #include "pack4.h"
 
 namespace {

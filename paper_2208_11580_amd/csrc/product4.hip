@@ -9,10 +9,10 @@
 //
 // Up to 16 tokens: bound by the weights' bytes (product4_rows_kernel).  One token through 8192 x 8192 takes 9.2 us in half
 // precision, 35.7 MB at 3.9 TB/s (plain reads of 64 MB and more: 6.0 to 6.3); through 768 x 768 3.3 us, of which about 2 are a
-// launch.  More tokens: bound by instruction issue beside the matrix cores (product4_tiles_kernel).  2048 tokens through 4096 x 4096 in
-// bf16 take 80 us, 860 TFLOP/s (a dense library product of that size: 61 us, 1120); in the tiles' 73 us the matrix cores are busy 41 % of the
-// time, and a matrix instruction comes with 3.7 vector ones.  8-bit inputs: 1000 tokens through 4096 x 8192 in groups of 64 take 84 us in the
-// tiles, 800 TOP/s, 10 vector instructions to a matrix instruction.  (Medians, captured in a graph.)
+// launch.  More tokens (product4_tiles_kernel): the matrix cores and the unpacking, neither of which fills the time.  2048 tokens through
+// 4096 x 4096 in bf16 take 80 us, 860 TFLOP/s (a dense library product of that size: 61 us, 1120); in the tiles' 73 us the matrix cores are
+// busy 41 % of the time and the vector instructions issue 38 % of it, 3.7 to a matrix instruction.  8-bit inputs: 1000 tokens through 4096
+// x 8192 in groups of 64 take 84 us in the tiles, 800 TOP/s, 19 % and 48 %, 10 vector instructions to a matrix instruction.  (Medians, captured in a graph.)
 #include "product4.h"
 
 namespace {

@@ -12,8 +12,9 @@
 // forward one: gradients and codes through LDS, weights formed in registers once for a wave's tokens.  Few tokens leave too few
 // tiles for the chip: the rows are cut into slices, whose sums a third launch adds in order.
 //
-// Bound by the matrix cores and the forming of weights, one after the other: 2048 tokens through 4096 x 4096 in bf16 take 121 us,
-// 570 TFLOP/s of the product and twice that in the matrix cores, the tiles 112 of them; 77 tokens through 2304 x 1283 in fp32 18.6 us (12 the tiles, 3 the layout, 4 the sum of slices).
+// Bound by the matrix cores and the forming of weights, neither of which fills the time: 2048 tokens through 4096 x 4096 in bf16 take
+// 121 us, 570 TFLOP/s of the product and twice that in the matrix cores, which in the tiles' 112 us are busy 50 % of the time, where the
+// vector instructions issue 32 % of it; 77 tokens through 2304 x 1283 in fp32 19.4 us (12 the tiles, 4 the layout, 3 the sum of slices).
 #include "product4.h"
 
 namespace {
