@@ -9,7 +9,7 @@
 //
 // A row is read once and stays in registers; the teacher's entries are handled in fp32, and those that name the same
 // token write the same value, so no order of writes changes the result.
-#include "product4.h"
+#include "row_io.h"
 
 namespace {
 
@@ -26,72 +26,6 @@ struct Args {
     int64_t ldz, lddz;
     float tau;
     int *status;
-};
-
-template <int TYPE>
-__device__ inline float load_as(const void *p, int64_t at)
-{
-    return TYPE == OBC_F32 ? ((const float *)p)[at] : TYPE == OBC_F16 ? (float)((const _Float16 *)p)[at] : (float)((const __bf16 *)p)[at];
-}
-
-// Logits of a 16-byte piece
-template <int TYPE>
-struct Piece {
-    static constexpr int E = TYPE == OBC_F32 ? 4 : 8;
-    uintx4 v;
-
-    // From logit `c` of the row at z on.  (A row's address is the same for all threads, and 32 bits of offset to it take half
-    // the registers of an address.)
-    __device__ void load(const char *z, int c)
-    {
-        const char *at = z + (unsigned)c * (16u / E);
-        if (TYPE == OBC_F32) v = __builtin_bit_cast(uintx4, (floatx4) * (const floatx4_at4 *)at);
-        else v = *(const uintx4_at2 *)at;
-    }
-    // the same at the end of a row of V: -inf beyond it
-    __device__ void load_end(const char *z, int c, int V)
-    {
-        if (c + E <= V) return load(z, c);
-        constexpr unsigned low = TYPE == OBC_F32 ? 0xff800000u : TYPE == OBC_F16 ? 0xfc00u : 0xff80u;
-        unsigned e[E];
-#pragma unroll
-        for (int j = 0; j < E; ++j)
-            e[j] = c + j >= V ? low : TYPE == OBC_F32 ? ((const unsigned *)z)[(unsigned)(c + j)] : ((const unsigned short *)z)[(unsigned)(c + j)];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = TYPE == OBC_F32 ? e[j] : e[2 * j % E] | e[(2 * j + 1) % E] << 16;
-    }
-    __device__ float operator[](int j) const
-    {
-        if (TYPE == OBC_F32) {
-            const unsigned w = v[j & 3];
-            return __builtin_bit_cast(float, w);
-        }
-        const unsigned w = v[j >> 1];
-        if (TYPE == OBC_F16) return j & 1 ? half_hi(w) : half_lo(w);
-        return __builtin_bit_cast(float, j & 1 ? w & 0xffff0000u : w << 16);
-    }
-    // keeps the compiler from carrying the piece's fp32 values, twice its registers, from one pass over the row to the next
-    __device__ void forget() { asm volatile("" : "+v"(v)); }
-    static __device__ void store(char *p, int c, const float (&g)[E])
-    {
-        char *at = p + (unsigned)c * (16u / E);
-        if (TYPE == OBC_F32) {
-            *(floatx4_at4 *)at = floatx4{g[0], g[1], g[2], g[3]};
-        } else {
-            uintx4 w;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                w[j] = TYPE == OBC_F16 ? pair_f16(g[2 * j % E], g[(2 * j + 1) % E]) : pair_bf16(g[2 * j % E], g[(2 * j + 1) % E]);
-            *(uintx4_at2 *)at = w;
-        }
-    }
-    static __device__ void store_end(char *p, int c, int V, const float (&g)[E])
-    {
-        if (c + E <= V) return store(p, c, g);
-#pragma unroll
-        for (int j = 0; j < E; ++j)
-            if (c + j < V) store_as<TYPE>(p, c + j, g[j]);
-    }
 };
 
 // N values reduced over a workgroup at a time, the first M by their maximum, the others by their sum; every thread gets

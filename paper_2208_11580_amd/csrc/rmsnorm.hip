@@ -5,107 +5,11 @@
 // Memory-bound: 4096 x 8192 in bf16 with residual and sum, 268 MB, takes 54 us (4.9 TB/s; a large copy reaches 5.2), one row of 4096
 // 2.7 us.  The backward pass keeps each workgroup's share of the gain's gradient in registers over its rows and has the next row's loads
 // under way: 4096 x 4096 in bf16 with the residual's gradient, 134 MB, takes 33 us, 27 of them the rows (5.0 TB/s), the rest the sum of the shares.
-#include "product4.h"
+#include "row_io.h"
 
 namespace {
 
 constexpr int kMaxCols = 65536;
-
-// Eight elements of a row as fp32; only the first `left` are touched.
-template <int TYPE>
-__device__ inline void load8(const void *p, int64_t at, int left, float (&v)[8])
-{
-    if (TYPE == OBC_F32) {
-        const float *q = (const float *)p + at;
-        if (left >= 8) {
-            const floatx4 a = *(const floatx4_at4 *)q, b = *(const floatx4_at4 *)(q + 4);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) { v[j] = a[j]; v[4 + j] = b[j]; }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = j < left ? q[j] : 0.f;
-        }
-    } else {
-        const unsigned short *q = (const unsigned short *)p + at;
-        unsigned short e[8];
-        if (left >= 8) {
-            const uintx4 w = *(const uintx4_at2 *)q;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) e[j] = (unsigned short)(w[j >> 1] >> (16 * (j & 1)));
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) e[j] = j < left ? q[j] : (unsigned short)0;
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            v[j] = TYPE == OBC_F16 ? (float)__builtin_bit_cast(_Float16, e[j]) : (float)__builtin_bit_cast(__bf16, e[j]);
-    }
-}
-
-template <int TYPE>
-__device__ inline void store8(void *p, int64_t at, int left, const float (&v)[8])
-{
-    if (left >= 8) {
-        if (TYPE == OBC_F32) {
-            float *q = (float *)p + at;
-            *(floatx4_at4 *)q = floatx4{v[0], v[1], v[2], v[3]};
-            *(floatx4_at4 *)(q + 4) = floatx4{v[4], v[5], v[6], v[7]};
-        } else {
-            uintx4 w;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                w[j] = TYPE == OBC_F16 ? pair_f16(v[2 * j], v[2 * j + 1]) : pair_bf16(v[2 * j], v[2 * j + 1]);
-            *(uintx4_at2 *)((unsigned short *)p + at) = w;
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j < left) store_as<TYPE>(p, at + j, v[j]);
-    }
-}
-
-// Eight elements on their way, in their own type
-template <int TYPE>
-struct Eight {
-    uintx4 v[TYPE == OBC_F32 ? 2 : 1];
-
-    __device__ void load(const void *p, int64_t at, int left)
-    {
-        if (left >= 8) {
-            if (TYPE == OBC_F32) {
-                v[0] = __builtin_bit_cast(uintx4, (floatx4) * (const floatx4_at4 *)((const float *)p + at));
-                v[TYPE == OBC_F32] = __builtin_bit_cast(uintx4, (floatx4) * (const floatx4_at4 *)((const float *)p + at + 4));
-            } else {
-                v[0] = *(const uintx4_at2 *)((const unsigned short *)p + at);
-            }
-            return;
-        }
-        unsigned e[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            e[j] = j >= left ? 0u : TYPE == OBC_F32 ? ((const unsigned *)p)[at + j] : ((const unsigned short *)p)[at + j];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            v[0][j] = TYPE == OBC_F32 ? e[j] : e[2 * j] | e[2 * j + 1] << 16;
-            if (TYPE == OBC_F32) v[TYPE == OBC_F32][j] = e[4 + j];
-        }
-    }
-    __device__ void get(float (&f)[8]) const
-    {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const unsigned w = TYPE == OBC_F32 ? v[j >> 2][j & 3] : v[0][j >> 1];
-            f[j] = TYPE == OBC_F32 ? __builtin_bit_cast(float, w) : TYPE == OBC_F16 ? (j & 1 ? half_hi(w) : half_lo(w)) : (j & 1 ? bf16_hi(w) : bf16_lo(w));
-        }
-    }
-};
-
-// The larger of two magnitudes; an infinity or a NaN is larger than any number (as their bits are), where fmaxf would drop the NaN.
-__device__ inline float larger(float top, float v)
-{
-    const unsigned a = __builtin_bit_cast(unsigned, top), b = __builtin_bit_cast(unsigned, v) & 0x7fffffffu;
-    return __builtin_bit_cast(float, a > b ? a : b);
-}
 
 // Sum (and largest magnitude) over a workgroup, the same value in every thread.
 template <int NT, bool MAX>
