@@ -217,8 +217,10 @@ def _prepare_adamw(case, gen, s):
         at = lambda name, i: s[name][i] if s[name] else None  # noqa: E731
         s["states"] = [obc.AdamState(s["m"][i], s["v"][i], at("m_scale", i), at("v_scale", i), s["master"][i])
                        for i in range(case["tensors"])]
-        s["out"] = ([torch.empty_like(p) for p in s["p"]],
-                    [obc.AdamState(*[None if t is None else torch.empty_like(t) for t in st]) for st in s["states"]])
+        # out of place, as a program does that keeps the last step's weights to go back to
+        s["plan"] = s["ctx"].obc_adamw_plan(s["p"], s["g"], s["states"], decay=DECAY, out=(
+            [torch.empty_like(p) for p in s["p"]],
+            [obc.AdamState(*[None if t is None else torch.empty_like(t) for t in st]) for st in s["states"]]))
     return s
 
 
@@ -238,9 +240,8 @@ def _run_own(s):
         r = ctx.obc_layernorm(s["x"], s["gain"], s["bias"], eps=EPS, residual=s["residual"], quant8=case["bits8"], out=s["out"])
         # (8 bits: the values that they stand for)
         return {"h": r["h"], "y": (r["y"] * r["scale"][:, None]).to(r["h"].dtype) if case["bits8"] else r["y"]}
-    # out of place, as a program does that keeps the last step's weights to go back to
-    p, states = ctx.obc_adamw(s["p"], s["g"], s["states"], s["step"], LR, beta1=BETA1, beta2=BETA2, eps=ADAM_EPS, decay=DECAY,
-                              grad_scale=s["grad_scale"], seed=s["seed"], out=s["out"])
+    p, states = ctx.obc_adamw(s["plan"], s["step"], LR, beta1=BETA1, beta2=BETA2, eps=ADAM_EPS, grad_scale=s["grad_scale"],
+                              seed=s["seed"])
     return _adamw_outputs(p, [st.m for st in states], [st.v for st in states], [st.m_scale for st in states],
                           [st.v_scale for st in states], [st.master for st in states])
 
