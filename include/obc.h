@@ -69,7 +69,8 @@ const char *obc_last_error(const obc_ctx *ctx);
 const char *obc_version(void);
 
 /* Wait for the context's stream and return the first error a kernel latched since the last
- * obc_check (OBC_ERR_NUMERIC, OBC_ERR_NOT_SPD; OBC_ERR_BAD_ARG from obc_pack4 and obc_distill) or
+ * obc_check (OBC_ERR_NUMERIC, OBC_ERR_NOT_SPD; OBC_ERR_BAD_ARG from obc_pack4, obc_distill, obc_score,
+ * obc_embed, obc_embed_grad and obc_adamw) or
  * OBC_OK; clears the latch. */
 int obc_check(obc_ctx *ctx);
 
@@ -380,6 +381,89 @@ int obc_rmsnorm_grad(obc_ctx *ctx, const void *h, const float *gain, const float
 int obc_distill(obc_ctx *ctx, const void *z, int type, int T, int V, int64_t ldz, const int32_t *top_index,
                 const float *top_logit, int k, float temperature, const float *weight, float *loss, void *dz,
                 int64_t lddz);
+
+/* ---- Judging and tuning compressed models -------------------------------------------------
+ * The dense model's side of the distillation and the judgement of the compressed one's answers, and what is tuned around the
+ * packed layers: layer norms, embedding tables, and the step that applies their gradients.  All asynchronous. */
+
+/* Scores of T rows of logits at a temperature, with d = z / temperature:
+ *   lse[t] = log sum_v exp(d[v]),  logp[t] = d[target[t]] - lse[t],  entropy[t] = -sum_v p[v] log p[v],  p = exp(d - lse)
+ *   top_index, top_logit   the k largest logits z, largest first, the lowest index first among equal ones; top_logit holds them
+ *                          as they are, so that they are what obc_distill takes
+ *   z          T x V of `type`, leading dimension ldz >= V;  target  nullable, T int32: negative: none, logp 0
+ *   logp (goes with target), entropy, lse   nullable, T fp32 out
+ *   top_index, top_logit   T x k int32 and fp32 out; null with k = 0.  0 <= k <= 1024, V <= 2^30
+ * A logit of -inf has probability 0, adds nothing and is never among the largest; entries that are left over have index -1 and
+ * logit -inf.  A row of -inf alone has lse and logp -inf and entropy 0.  A row with a NaN or +inf has NaN for all its numbers and
+ * indices of -1 (a logp of 0 where it has no target).  A target >= V latches OBC_ERR_BAD_ARG and counts as none. */
+int obc_score_workspace_bytes(int T, int V, int type, int k, size_t *bytes);
+int obc_score(obc_ctx *ctx, const void *z, int type, int T, int V, int64_t ldz, const int32_t *target, float temperature, int k,
+              float *logp, float *entropy, float *lse, int32_t *top_index, float *top_logit, void *ws, size_t ws_bytes);
+
+/* Layer norm of T rows with the residual's addition:
+ *   h = x + residual,  y = (h - mean(h)) rstd gain + bias,  rstd = 1 / sqrt(mean((h - mean(h))^2) + eps)
+ *   gain, bias   d, fp32; bias nullable (0);  mean, rstd  nullable, T fp32 out
+ * The rest as in obc_rmsnorm.  Sums are fp32: a row with deviations beyond about 1e19 gives its bias or NaN, in 8 bits scale NaN and
+ * codes 0. */
+int obc_layernorm(obc_ctx *ctx, const void *x, const void *residual, int x_type, const float *gain, const float *bias, float eps, int T,
+                  int d, void *h, void *y, int y_type, float *y_scale, float *mean, float *rstd);
+
+/* Its backward pass (8-bit outputs: straight through the rounding), from the saved sum h, mean and rstd:
+ *   w = gain dy,  dx = dh + rstd (w - mean(w) - xhat mean(w xhat)),  dgain = sum_t dy xhat,  dbias = sum_t dy,
+ *   xhat = (h - mean) rstd
+ *   dgain, dbias   d fp32 out; dbias nullable.  The rest as in obc_rmsnorm_grad. */
+int obc_layernorm_grad_workspace_bytes(int T, int d, size_t *bytes);
+int obc_layernorm_grad(obc_ctx *ctx, const void *h, const float *gain, const float *mean, const float *rstd, const void *dy,
+                       const void *dh, int type, int T, int d, void *dx, float *dgain, float *dbias, void *ws, size_t ws_bytes);
+
+/* y[t] = scale table[ids[t]] for T tokens, T x d.
+ *   table   V x d of `type`, leading dimension ldt >= d;  y  of y_type, leading dimension ldy >= d (OBC_F32, OBC_F16, OBC_BF16 each)
+ *   ids     T int32; negative: no token, a row of zeros
+ * The product is fp32, rounded once.  An id >= V latches OBC_ERR_BAD_ARG and counts as no token.  1 <= d <= 2^20. */
+int obc_embed(obc_ctx *ctx, const void *table, int type, int V, int d, int64_t ldt, const int32_t *ids, int T, float scale, void *y,
+              int y_type, int64_t ldy);
+
+/* The table's gradient: dtable[v] = scale sum over the tokens t with ids[t] = v of dy[t]; every row is written, with zeros where it
+ * has no token.  accumulate != 0: dtable[v] += that, rows without a token are not touched.
+ *   dy      T x d of `type`, leading dimension lddy >= d;  dtable  V x d of dtable_type, leading dimension lddt >= d
+ * Sums are fp32, over an id's tokens in a fixed order; one rounding.  Ids as in obc_embed.  T <= 2^30. */
+int obc_embed_grad_workspace_bytes(int T, int V, int d, size_t *bytes);
+int obc_embed_grad(obc_ctx *ctx, const int32_t *ids, int T, const void *dy, int type, int64_t lddy, float scale, int V, int d,
+                   int accumulate, void *dtable, int dtable_type, int64_t lddt, void *ws, size_t ws_bytes);
+
+/* A tensor of obc_adamw: n elements each, contiguous.  Inputs and outputs may be the same arrays (the usual case) or others that
+ * do not overlap. */
+typedef struct obc_adamw_tensor {
+    const void *p;                  /* parameters, of `type` */
+    void *p_out;
+    const void *g;                  /* gradients, of `type` */
+    const void *m;                  /* first moment: fp32, or 8-bit numbers (sign, 4 bits of exponent, 3 of mantissa: up to 448) */
+    void *m_out;
+    const void *v;                  /* second moment: fp32, or its root in 8-bit numbers */
+    void *v_out;
+    const float *m_scale, *v_scale; /* 8 bits: ceil(n / 256) factors of 256 consecutive numbers each */
+    float *m_scale_out, *v_scale_out;
+    const float *master;            /* nullable: the parameters in fp32, which p is a rounded copy of */
+    float *master_out;
+    int64_t n;
+    float decay;
+} obc_adamw_tensor;
+
+/* One step of AdamW over `count` tensors:
+ *   g' = g grad_scale,  m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2
+ *   p = p (1 - lr decay) - lr m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps)
+ * in fp32, on master where there is one; p is rounded to nearest from that.
+ *   tensors   HOST array; it may go when the call returns
+ *   bits      of the moments: 32 or 8.  8: m and sqrt(v) are divided by their block's scale, its largest magnitude / 448, and rounded
+ *             up or down with the chances that keep them on average, by a hash of seed, step, the tensor's place in the list and the
+ *             element's in the tensor; sqrt(v) > 0 is never rounded to 0.  A block whose largest is below 1e-30 becomes zeros.
+ *             A block with a NaN or an infinity gets scale NaN.
+ *   step      1 for the first; step_at (device, nullable) is read in its place.  lr_at (device, nullable) in lr's place.
+ *             Neither is changed.  A step_at below 1 latches OBC_ERR_BAD_ARG and leaves all values as they are.
+ *   grad_scale  device, nullable (1): a loss scale's reciprocal or a clipping factor.  Infinite or NaN: all values stay as they are.
+ * 0 <= beta < 1, eps > 0.  Results do not depend on how tensors are listed, but for the hash. */
+int obc_adamw(obc_ctx *ctx, const obc_adamw_tensor *tensors, int count, int type, int bits, int64_t step, const int64_t *step_at,
+              float lr, const float *lr_at, double beta1, double beta2, float eps, const float *grad_scale, uint32_t seed);
 
 #ifdef __cplusplus
 }

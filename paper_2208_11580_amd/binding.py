@@ -39,6 +39,9 @@ EXPORTS = [
     "obc_group_grid", "obc_pack4_bytes", "obc_pack4",
     "obc_product4_workspace_bytes", "obc_product4", "obc_product4_grad_workspace_bytes", "obc_product4_grad",
     "obc_rmsnorm", "obc_rmsnorm_grad_workspace_bytes", "obc_rmsnorm_grad", "obc_distill",
+    "obc_score_workspace_bytes", "obc_score",
+    "obc_layernorm", "obc_layernorm_grad_workspace_bytes", "obc_layernorm_grad",
+    "obc_embed", "obc_embed_grad_workspace_bytes", "obc_embed_grad", "obc_adamw",
 ]
 
 _TYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16, torch.int8: I8}
@@ -58,6 +61,22 @@ class Packed4(NamedTuple):
     rows: int
     cols: int
     group: int
+
+
+class AdamState(NamedTuple):
+    """What obc_adamw keeps for a parameter tensor (of its shape, or as many values): moments in fp32, or m and the root of v in
+    8-bit floating-point numbers with an fp32 scale for every 256 of them; master: the parameters in fp32, or None."""
+    m: torch.Tensor
+    v: torch.Tensor
+    m_scale: torch.Tensor | None = None
+    v_scale: torch.Tensor | None = None
+    master: torch.Tensor | None = None
+
+
+class AdamTensor(ctypes.Structure):
+    # as obc_adamw_tensor
+    _fields_ = [(name, c_void_p) for name in ("p", "p_out", "g", "m", "m_out", "v", "v_out", "m_scale", "v_scale", "m_scale_out",
+                                              "v_scale_out", "master", "master_out")] + [("n", c_int64), ("decay", c_float)]
 
 
 class ObcError(RuntimeError):
@@ -125,6 +144,16 @@ def load_library():
     lib.obc_rmsnorm_grad_workspace_bytes.argtypes = [c_int, c_int, sp]
     lib.obc_rmsnorm_grad.argtypes = [vp, vp, vp, vp, vp, vp, c_int, c_int, c_int, vp, vp, vp, c_size_t]
     lib.obc_distill.argtypes = [vp, vp, c_int, c_int, c_int, i64, vp, vp, c_int, c_float, vp, vp, vp, i64]
+    lib.obc_score_workspace_bytes.argtypes = [c_int, c_int, c_int, c_int, sp]
+    lib.obc_score.argtypes = [vp, vp, c_int, c_int, c_int, i64, vp, c_float, c_int, vp, vp, vp, vp, vp, vp, c_size_t]
+    lib.obc_layernorm.argtypes = [vp, vp, vp, c_int, vp, vp, c_float, c_int, c_int, vp, vp, c_int, vp, vp, vp]
+    lib.obc_layernorm_grad_workspace_bytes.argtypes = [c_int, c_int, sp]
+    lib.obc_layernorm_grad.argtypes = [vp, vp, vp, vp, vp, vp, vp, c_int, c_int, c_int, vp, vp, vp, vp, c_size_t]
+    lib.obc_embed.argtypes = [vp, vp, c_int, c_int, c_int, i64, vp, c_int, c_float, vp, c_int, i64]
+    lib.obc_embed_grad_workspace_bytes.argtypes = [c_int, c_int, c_int, sp]
+    lib.obc_embed_grad.argtypes = [vp, vp, c_int, vp, c_int, i64, c_float, c_int, c_int, c_int, vp, c_int, i64, vp, c_size_t]
+    lib.obc_adamw.argtypes = [vp, vp, c_int, c_int, c_int, i64, vp, c_float, vp, ctypes.c_double, ctypes.c_double, c_float, vp,
+                              ctypes.c_uint32]
     for name in EXPORTS:
         fn = getattr(lib, name)
         if name not in ("obc_last_error", "obc_version"):
@@ -178,6 +207,14 @@ def _vector(t, n, what):
     return t.data_ptr()
 
 
+def _ints(t, n, what):
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype != torch.int32 or t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s must be %d contiguous int32 values on the device" % (what, n))
+    return t.data_ptr()
+
+
 def _no_grad(*tensors):
     """Results are new to autograd, which would take a gradient that ends here for none."""
     if torch.is_grad_enabled():
@@ -185,6 +222,55 @@ def _no_grad(*tensors):
             if t is not None and t.requires_grad:
                 raise ValueError("an argument requires a gradient, which these calls do not record: detach it, or call under "
                                  "torch.no_grad(), and call the operator's own gradient")
+
+
+class AdamPlan:
+    """The tensors of obc_adamw, which it keeps, and their addresses as the C entry point takes them."""
+
+    def __init__(self, params, grads, states, decay=0.01, out=None):
+        params, states = list(params), list(states)
+        self.params, self.states = params, states
+        self.new = (params, states) if out is None else (list(out[0]), list(out[1]))
+        self.count = count = len(params)
+        if not len(states) == len(self.new[0]) == len(self.new[1]) == count:
+            raise ValueError("there must be as many states and outputs as parameters")
+        decays = list(decay) if isinstance(decay, (list, tuple)) else [decay] * count
+        if len(decays) != count:
+            raise ValueError("there must be as many decays as parameters")
+        self.type = _type_of(params[0], "params") if count else F32
+        self.bits = 8 if count and states[0].m.dtype == torch.float8_e4m3fn else 32
+        kind = torch.float8_e4m3fn if self.bits == 8 else torch.float32
+        self.tensors = (AdamTensor * max(count, 1))()
+        for i in range(count):
+            d, p, st, new = self.tensors[i], params[i], states[i], self.new[1][i]
+            _no_grad(p, self.new[0][i], *st, *new)
+            n = d.n = p.numel()
+            d.decay = float(decays[i])
+            d.p, d.p_out = self._at(i, p, params[0].dtype, n), self._at(i, self.new[0][i], params[0].dtype, n)
+            if (st.master is None) != (new.master is None) or (self.bits == 8) != (st.m_scale is not None):
+                raise ValueError("tensor %d: states of 8 bits have scales, and outputs what the states have" % i)
+            blocks = -(-n // 256)
+            for name, dtype, size in (("m", kind, n), ("v", kind, n), ("m_scale", torch.float32, blocks), ("v_scale", torch.float32, blocks),
+                                      ("master", torch.float32, n)):
+                setattr(d, name, self._at(i, getattr(st, name), dtype, size))
+                setattr(d, name + "_out", self._at(i, getattr(new, name), dtype, size))
+        self.use(grads)
+
+    @staticmethod
+    def _at(i, t, dtype, n):
+        if t is not None and t.numel() != n:
+            raise ValueError("tensor %d: gradients, states and outputs must be as large as the parameters" % i)
+        return _ptr(t, dtype)
+
+    def use(self, grads):
+        """Other gradients from the next step on."""
+        grads = list(grads)
+        if len(grads) != self.count:
+            raise ValueError("there must be as many gradients as parameters")
+        for i, g in enumerate(grads):
+            _no_grad(g)
+            self.tensors[i].g = self._at(i, g, self.params[0].dtype, self.params[i].numel())
+        self.grads = grads
 
 
 class Context:
@@ -639,3 +725,159 @@ class Context:
         self._ck(self.lib.obc_distill(self.h, zp, t, T, V, ldz, _ptr(top_index, torch.int32), _ptr(top_logit, torch.float32), k,
                                       float(temperature), _vector(weight, T, "weight"), _vector(loss, T, "loss"), gp, ldg))
         return dict(loss=loss, dz=dz)
+
+    # ------------------------------------------------------- judging and tuning them
+    def obc_score(self, z, target=None, top=0, temperature=1.0, out=None):
+        """Log-sum-exp and entropy (T) of logits z (T x V) at a temperature, the log probabilities of target (T int32; negative:
+        none) and the `top` largest logits with their indices, which obc_distill takes.  out may hold logp, entropy, lse, top_index
+        and top_logit."""
+        t = _type_of(z, "z")
+        zp, ldz, T, V = _rows_of(z, "z")
+        out = {} if out is None else out
+        _no_grad(z, *out.values())
+        k = int(top)
+        if k < 0:
+            raise ValueError("top must not be negative")
+        r = {}
+        for name, shape, dtype in (("logp", (T,), torch.float32), ("entropy", (T,), torch.float32), ("lse", (T,), torch.float32),
+                                   ("top_index", (T, k), torch.int32), ("top_logit", (T, k), torch.float32)):
+            r[name] = None
+            if (target is None and name == "logp") or (k == 0 and len(shape) == 2):
+                continue
+            r[name] = out.get(name)
+            if r[name] is None:
+                r[name] = self._empty(shape, dtype, z.device)
+            elif r[name].shape != shape:
+                raise ValueError("%s must have the shape %s" % (name, shape))
+        ws, n, _held = self._need("obc_score_workspace_bytes", T, V, t, k)
+        self._ck(self.lib.obc_score(self.h, zp, t, T, V, ldz, _ints(target, T, "target"), float(temperature), k,
+                                    _vector(r["logp"], T, "logp"), _vector(r["entropy"], T, "entropy"), _vector(r["lse"], T, "lse"),
+                                    _ints(r["top_index"], T * k, "top_index"), _vector(r["top_logit"], T * k, "top_logit"), ws, n))
+        return r
+
+    def obc_layernorm(self, x, gain, bias=None, eps=1e-5, residual=None, quant8=False, want_stats=False, out=None):
+        """h = x + residual and its layer norm y.  out may hold h, y, scale (quant8), mean and rstd; without a residual, h is x
+        itself."""
+        T, d = x.shape
+        t = _type_of(x, "x")
+        out = {} if out is None else out
+        _no_grad(x, gain, bias, residual, *out.values())
+        h = out.get("h")
+        if h is None and residual is not None:
+            h = self._empty((T, d), x.dtype, x.device)
+        y = out.get("y")
+        if y is None:
+            y = self._empty((T, d), torch.int8 if quant8 else x.dtype, x.device)
+        scale = out.get("scale")
+        if scale is None and quant8:
+            scale = self._empty((T,), torch.float32, x.device)
+        mean, rstd = out.get("mean"), out.get("rstd")
+        if want_stats:
+            mean = self._empty((T,), torch.float32, x.device) if mean is None else mean
+            rstd = self._empty((T,), torch.float32, x.device) if rstd is None else rstd
+        for other in (residual, h, y):
+            if other is not None and other.shape != x.shape:
+                raise ValueError("residual, h and y must have x's shape")
+        self._ck(self.lib.obc_layernorm(self.h, _ptr(x), _ptr(residual, x.dtype), t, _vector(gain, d, "gain"), _vector(bias, d, "bias"),
+                                        float(eps), T, d, _ptr(h, x.dtype), _ptr(y, torch.int8 if quant8 else x.dtype),
+                                        I8 if quant8 else t, _vector(scale, T, "scale") if quant8 else None, _vector(mean, T, "mean"),
+                                        _vector(rstd, T, "rstd")))
+        return dict(h=x if h is None else h, y=y, scale=scale, mean=mean, rstd=rstd)
+
+    def obc_layernorm_grad(self, h, gain, mean, rstd, dy, dh=None, out=None):
+        """Gradients of x (and of the residual), the gain and the bias, from what the forward pass left; out may hold dx, dgain and
+        dbias."""
+        T, d = h.shape
+        t = _type_of(h, "h")
+        out = {} if out is None else out
+        _no_grad(h, gain, mean, rstd, dy, dh, *out.values())
+        dx = out.get("dx")
+        if dx is None:
+            dx = self._empty((T, d), h.dtype, h.device)
+        dgain = out.get("dgain")
+        if dgain is None:
+            dgain = self._empty((d,), torch.float32, h.device)
+        dbias = out.get("dbias")
+        if dbias is None:
+            dbias = self._empty((d,), torch.float32, h.device)
+        for other in (dy, dh, dx):
+            if other is not None and other.shape != h.shape:
+                raise ValueError("dy, dh and dx must have h's shape")
+        ws, n, _held = self._need("obc_layernorm_grad_workspace_bytes", T, d)
+        self._ck(self.lib.obc_layernorm_grad(self.h, _ptr(h), _vector(gain, d, "gain"), _vector(mean, T, "mean"), _vector(rstd, T, "rstd"),
+                                             _ptr(dy, h.dtype), _ptr(dh, h.dtype), t, T, d, _ptr(dx, h.dtype),
+                                             _vector(dgain, d, "dgain"), _vector(dbias, d, "dbias"), ws, n))
+        return dict(dx=dx, dgain=dgain, dbias=dbias)
+
+    def obc_embed(self, table, ids, scale=1.0, out=None, out_dtype=None):
+        """y[t] = scale table[ids[t]] (T x d); ids: T int32, negative: a row of zeros.  y has out's type, else out_dtype, else the
+        table's."""
+        _no_grad(table, out)
+        t = _type_of(table, "table")
+        tp, ldt, V, d = _rows_of(table, "table")
+        T = ids.numel()
+        if out is None:
+            out = self._empty((T, d), table.dtype if out_dtype is None else out_dtype, table.device)
+        yp, ldy, rows, n = _rows_of(out, "out")
+        if rows != T or n != d:
+            raise ValueError("out must be %d x %d" % (T, d))
+        rc = self.lib.obc_embed(self.h, tp, t, V, d, ldt, _ints(ids, T, "ids"), T, float(scale), yp, _type_of(out, "out"), ldy)
+        if rc != OBC_OK:
+            self._ck(rc)
+        return out
+
+    def obc_embed_grad(self, ids, dy, rows, scale=1.0, out=None, out_dtype=None, accumulate=False):
+        """The gradient (rows x d) of a table of so many rows that obc_embed read, from dy (T x d).  out's type, else out_dtype, else
+        dy's; accumulate: added to out."""
+        _no_grad(dy, out)
+        t = _type_of(dy, "dy")
+        dp, lddy, T, d = _rows_of(dy, "dy")
+        if out is None:
+            if accumulate:
+                raise ValueError("accumulate adds to out, which is missing")
+            out = self._empty((int(rows), d), dy.dtype if out_dtype is None else out_dtype, dy.device)
+        gp, ldt, V, n = _rows_of(out, "out")
+        if V != rows or n != d:
+            raise ValueError("out must be %d x %d" % (rows, d))
+        ws, n, _held = self._need("obc_embed_grad_workspace_bytes", T, V, d)
+        self._ck(self.lib.obc_embed_grad(self.h, _ints(ids, T, "ids"), T, dp, t, lddy, float(scale), V, d, int(bool(accumulate)), gp,
+                                         _type_of(out, "out"), ldt, ws, n))
+        return out
+
+    def obc_adamw_state(self, p, bits=32, master=False):
+        """Moments of zero for a parameter tensor, in 32 or 8 bits, and an fp32 copy of it with master."""
+        n = p.numel()
+        if bits not in (8, 32):
+            raise ValueError("moments have 8 or 32 bits")
+        with torch.no_grad(), torch.cuda.stream(self.stream):
+            def zeros(m, dtype):
+                return torch.zeros(m, dtype=dtype, device=p.device)
+
+            copy = p.detach().to(torch.float32, copy=True, memory_format=torch.contiguous_format) if master else None
+            if bits == 32:
+                return AdamState(zeros(p.shape, torch.float32), zeros(p.shape, torch.float32), None, None, copy)
+            blocks = -(-n // 256)
+            return AdamState(zeros(p.shape, torch.float8_e4m3fn), zeros(p.shape, torch.float8_e4m3fn), zeros(blocks, torch.float32),
+                             zeros(blocks, torch.float32), copy)
+
+    def obc_adamw_plan(self, params, grads, states, decay=0.01, out=None):
+        """The lists of parameters, gradients of their type, and AdamStates (all of 32 or all of 8 bits) that obc_adamw goes over, as it
+        takes them; kept from step to step.  decay: a float or one for each tensor.  Steps are in place, unless out holds other
+        parameters and states."""
+        return AdamPlan(params, grads, states, decay, out)
+
+    def obc_adamw(self, plan, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=None, seed=0):
+        """A step of AdamW over an AdamPlan's tensors.  step: an int, 1 for the first, or an int64 tensor on the device; lr: a float or
+        an fp32 tensor on the device; grad_scale: an fp32 tensor on the device.  Returns the new parameters and states."""
+        step_at = lr_at = None
+        if torch.is_tensor(step):
+            if step.numel() != 1:
+                raise ValueError("step must be one value")
+            step_at, step = _ptr(step, torch.int64), 0
+        if torch.is_tensor(lr):
+            lr_at, lr = _vector(lr, 1, "lr"), 0.0
+        rc = self.lib.obc_adamw(self.h, plan.tensors, plan.count, plan.type, plan.bits, int(step), step_at, float(lr), lr_at,
+                                float(beta1), float(beta2), float(eps), _vector(grad_scale, 1, "grad_scale"), int(seed) & 0xffffffff)
+        if rc != OBC_OK:
+            self._ck(rc)
+        return plan.new

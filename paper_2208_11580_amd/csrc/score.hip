@@ -1,0 +1,511 @@
+// obc_score: log probabilities of given tokens, entropy and the largest logits of rows of logits.
+//
+//   d[v] = (z[v] - max z) / tau,  S = sum exp d,  D = sum exp(d) d:  lse = max z / tau + log S,  logp = d[target] - log S,
+//   entropy = log S - D / S
+// A workgroup reads its part of a row once, into registers: the maximum, then S and D (kept in powers and logarithms of 2).  The k
+// largest come from the same registers: the r-th largest of each wave's lanes' own maxima, r waves = k, is a bound that at least k
+// logits reach and few more do; those that do go to LDS as whole numbers (logit, then index) and are sorted there.  Where too many
+// reach it (equal logits, mostly), the k-th largest is found exactly, by bisection, and equal ones are taken in their order.  Rows
+// of several parts are joined by a second kernel.
+#include "row_io.h"
+
+namespace {
+
+typedef unsigned long long Key;      // a logit's order above its index's opposite; 0: none
+
+constexpr int kMaxTop = 1024, kMaxCols = 1 << 30;
+constexpr int kCap = 2048;      // candidates in LDS
+constexpr int NT = 256, WAVES = NT / 64;
+constexpr float kLn2 = 0.693147180559945f;
+
+struct Stats {
+    float top, sum, dot, unused;
+};
+
+struct Args {
+    const void *z;
+    const int32_t *target;
+    float *logp, *entropy, *lse;
+    int32_t *top_index;
+    float *top_logit;
+    int T, V, k, parts, len;      // columns of a part
+    int64_t ldz;
+    float tau;
+    Stats *stats;                 // per part, with parts > 1
+    Key *lists;                   // k per part, largest first
+    int *status;
+};
+
+// Numbers in the order of floats, and back.  Bits below SHIFT are the same for all of a type's positive numbers; a bound made from
+// a shifted number lies between two of the type's (or on one), which is all that comparing with it needs.
+__device__ inline unsigned ordered(float f)
+{
+    const unsigned b = __builtin_bit_cast(unsigned, f);
+    return b ^ ((int)b >> 31 | 0x80000000u);
+}
+__device__ inline float unordered(unsigned o) { return __builtin_bit_cast(float, o & 0x80000000u ? o ^ 0x80000000u : ~o); }
+
+template <int TYPE>
+struct Order {
+    static constexpr int SHIFT = TYPE == OBC_F32 ? 0 : TYPE == OBC_F16 ? 13 : 16;
+    static __device__ unsigned of(float f) { return ordered(f) >> SHIFT; }
+    static __device__ float bound(unsigned o) { return unordered(o << SHIFT); }
+};
+
+template <int N>
+__device__ inline void block_sums(float (&v)[N], float (*buf)[N])
+{
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], off, 64);
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i) buf[threadIdx.x >> 6][i] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        v[i] = buf[0][i];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) v[i] += buf[w][i];
+    }
+}
+
+__device__ inline int block_count(int n, int *buf)
+{
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off, 64);
+    __syncthreads();      // buf is read by all before it is written again
+    if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = n;
+    __syncthreads();
+    n = buf[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) n += buf[w];
+    return __builtin_amdgcn_readfirstlane(n);
+}
+
+__device__ inline Key key_of(float z, int index) { return (Key)ordered(z + 0.f) << 32 | ~(unsigned)index; }
+
+// keys[0 .. n) in LDS, n <= kCap, largest first; all threads of the workgroup.  `out` gets the first k.
+template <typename OUT>
+__device__ inline void sort_keys(Key *keys, int n, int k, OUT out)
+{
+    const int tid = threadIdx.x;
+    if (n <= NT) {
+        const Key own = tid < n ? keys[tid] : 0;
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += keys[j] > own;
+        if (tid < n && rank < k) out(rank, own);
+        return;
+    }
+    int size = 512;
+    while (size < n) size *= 2;
+    for (int i = n + tid; i < size; i += NT) keys[i] = 0;
+    __syncthreads();
+    for (int run = 2; run <= size; run *= 2)
+        for (int gap = run / 2; gap > 0; gap /= 2) {
+            for (int i = tid; i < size / 2; i += NT) {
+                const int lo = 2 * i - (i & (gap - 1)), hi = lo + gap;
+                const Key x = keys[lo], y = keys[hi];
+                if ((x < y) == ((lo & run) == 0)) {
+                    keys[lo] = y;
+                    keys[hi] = x;
+                }
+            }
+            __syncthreads();
+        }
+    for (int i = tid; i < n && i < k; i += NT) out(i, keys[i]);
+}
+
+// The results of a row; one thread
+__device__ inline void finish(const Args &a, int64_t row, float top, float sum, float dot, float zt, int target)
+{
+    // (an empty row: sum 0, top taken as 0)
+    const bool none = sum == 0.f;
+    const float ln = logf(sum);
+    if (a.lse) a.lse[row] = none ? -__builtin_inff() : top / a.tau + ln;
+    if (a.entropy) a.entropy[row] = none ? 0.f : fmaf(-kLn2, dot / sum, ln);
+    if (a.logp) a.logp[row] = target < 0 ? 0.f : none ? -__builtin_inff() : (zt - top) / a.tau - ln;
+}
+
+__device__ inline int target_of(const Args &a, int64_t row)
+{
+    int t = a.target ? a.target[row] : -1;
+    if (t >= a.V) {
+        obc_latch(a.status, OBC_ERR_BAD_ARG);
+        t = -1;
+    }
+    return t;
+}
+
+template <int TYPE, int CH>
+__global__ __launch_bounds__(NT, 4) void score_kernel(Args a)
+{
+    constexpr int E = Piece<TYPE>::E;
+    typedef Order<TYPE> O;
+    __shared__ float buf1[WAVES], buf2[WAVES][2], buf3[WAVES];
+    __shared__ int buf4[WAVES], found;
+    __shared__ Key keys[kCap];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t row = blockIdx.x / a.parts;
+    const int part = (int)(blockIdx.x - row * a.parts), from = part * a.len, n = max(0, min(a.len, a.V - from));
+    const char *const z = (const char *)a.z + (row * a.ldz + from) * (16 / E);
+    const float c2 = 1.44269504088896f / a.tau;
+    // pieces 0 .. whole - 1 are whole in every thread; the part ends inside the next one, x[CH] wherever that is
+    const int whole = n / (NT * E);
+    Piece<TYPE> x[CH + 1];
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+        if (i < whole) x[i].load(z, (i * NT + tid) * E);
+    x[CH].load_end(z, (whole * NT + tid) * E, n);
+    int target = -1;
+    float zt = 0.f;
+    if (a.parts == 1 && tid == 0) {
+        target = target_of(a, row);
+        if (target >= 0) zt = load_as<TYPE>(a.z, row * a.ldz + target);
+    }
+    if (tid == 0) found = 0;
+    // the largest of each piece and of them all
+    float most[CH + 1], own = -__builtin_inff();
+#pragma unroll
+    for (int i = 0; i <= CH; ++i) {
+        most[i] = -__builtin_inff();
+        if (i < whole || i == CH) {
+#pragma unroll
+            for (int j = 0; j < E; ++j) most[i] = fmaxf(most[i], x[i][j]);
+            own = fmaxf(own, most[i]);
+        }
+    }
+    float wave_top = own;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) wave_top = fmaxf(wave_top, __shfl_xor(wave_top, off, 64));
+    // what at least r of this wave's lanes (or of their pieces) reach, and not many more
+    float bound = -__builtin_inff();
+    if (a.k > 0) {
+        const int r = (a.k + WAVES - 1) / WAVES;
+        auto count = [&](float b) {
+            if (r <= 32) return (int)__popcll(__ballot(own >= b));
+            int c = 0;
+#pragma unroll
+            for (int i = 0; i <= CH; ++i)
+                if (i < whole || i == CH) c += __popcll(__ballot(most[i] >= b));
+            return c;
+        };
+        unsigned lo = O::of(-__builtin_inff()), hi = __builtin_amdgcn_readfirstlane(O::of(wave_top));
+        if (wave_top < __builtin_inff() && count(O::bound(lo + 1)) >= r) {
+            ++lo;
+            while (lo < hi) {
+                const unsigned mid = lo + (hi - lo + 1) / 2;
+                const int c = count(O::bound(mid));
+                if (c >= r) lo = mid;
+                else hi = mid - 1;
+                if (c >= r && c <= r + (r >> 3) + 1) break;
+            }
+            bound = O::bound(lo);
+        }
+    }
+    if (lane == 0) {
+        buf1[wave] = wave_top;
+        buf3[wave] = bound;
+    }
+    __syncthreads();
+    float top = buf1[0];
+    bound = buf3[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) {
+        top = fmaxf(top, buf1[w]);
+        bound = fminf(bound, buf3[w]);
+    }
+    const float base = top == -__builtin_inff() ? 0.f : top;
+    float s[2] = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i <= CH; ++i)
+        if (i < whole || i == CH) {
+            x[i].forget();
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                const float d = (x[i][j] - base) * c2, e = __builtin_amdgcn_exp2f(d);
+                s[0] += e;
+                s[1] = fmaf(e, fmaxf(d, -1e30f), s[1]);      // (a logit of -inf adds nothing)
+            }
+        }
+    block_sums<2>(s, buf2);
+    if (tid == 0) {
+        if (a.parts == 1) finish(a, row, base, s[0], s[1], zt, target);
+        else a.stats[blockIdx.x] = Stats{base, s[0], s[1], 0.f};
+    }
+    if (a.k == 0) return;
+
+    // the logits that reach `b` go to LDS, as far as there is room; the bound's are above -inf
+    auto each = [&](int i, float b, auto f) {
+        if (most[i] >= b) {
+            const int c = from + ((i == CH ? whole : i) * NT + tid) * E;
+#pragma unroll
+            for (int j = 0; j < E; ++j)
+                if (x[i][j] >= b) f(x[i][j], c + j);
+        }
+    };
+    auto collect = [&](float b) {
+        int mine = 0;
+#pragma unroll
+        for (int i = 0; i <= CH; ++i)
+            if (i < whole || i == CH) {
+                x[i].forget();
+                each(i, b, [&](float, int) { ++mine; });
+            }
+        int at = mine;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int o = __shfl_up(at, off, 64);
+            if (lane >= off) at += o;
+        }
+        int first = 0;
+        if (lane == 63) first = atomicAdd(&found, at);
+        at += __shfl(first, 63, 64) - mine;
+        if (mine > 0)
+#pragma unroll
+            for (int i = 0; i <= CH; ++i)
+                if (i < whole || i == CH) {
+                    x[i].forget();
+                    each(i, b, [&](float v, int c) {
+                        if (at < kCap) keys[at] = key_of(v, c);
+                        ++at;
+                    });
+                }
+    };
+    const float least = O::bound(O::of(-__builtin_inff()) + 1);      // above -inf
+    collect(fmaxf(bound, least));
+    __syncthreads();
+    int have = found;
+    __syncthreads();      // (found is set again below)
+    if (have > kCap) {
+        // Exactly: the largest bound that k logits reach, those above it, and of those on it the first
+        auto count = [&](float b) {
+            int c = 0;
+#pragma unroll
+            for (int i = 0; i <= CH; ++i)
+                if (i < whole || i == CH) {
+                    x[i].forget();
+#pragma unroll
+                    for (int j = 0; j < E; ++j) c += x[i][j] >= b;
+                }
+            return block_count(c, buf4);
+        };
+        unsigned lo = __builtin_amdgcn_readfirstlane(O::of(fmaxf(bound, least))), hi = __builtin_amdgcn_readfirstlane(O::of(top));
+        while (lo < hi) {
+            const unsigned mid = lo + (hi - lo + 1) / 2;
+            if (count(O::bound(mid)) >= a.k) lo = mid;
+            else hi = mid - 1;
+        }
+        const float at_least = O::bound(lo), above = O::bound(lo + 1);
+        int need = a.k;
+        if (lo < O::of(top)) need -= count(above);
+        if (tid == 0) found = 0;
+        __syncthreads();
+        if (lo < O::of(top)) collect(above);
+        __syncthreads();
+        int filled = found;
+#pragma unroll
+        for (int i = 0; i <= CH; ++i)
+            if ((i < whole || i == CH) && need > 0) {
+                auto on = [&](float v) { return v >= at_least && !(lo < O::of(top) && v >= above); };
+                int mine = 0;
+#pragma unroll
+                for (int j = 0; j < E; ++j) mine += on(x[i][j]);
+                int at = mine;
+#pragma unroll
+                for (int off = 1; off < 64; off <<= 1) {
+                    const int o = __shfl_up(at, off, 64);
+                    if (lane >= off) at += o;
+                }
+                __syncthreads();
+                if (lane == 63) buf4[wave] = at;
+                __syncthreads();
+                at -= mine;
+                int all = 0;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) {
+                    at += w < wave ? buf4[w] : 0;
+                    all += buf4[w];
+                }
+                const int c = from + ((i == CH ? whole : i) * NT + tid) * E;
+#pragma unroll
+                for (int j = 0; j < E; ++j)
+                    if (on(x[i][j])) {
+                        if (at < need) keys[filled + at] = key_of(x[i][j], c + j);
+                        ++at;
+                    }
+                filled += min(all, need);
+                need -= min(all, need);
+            }
+        __syncthreads();
+        have = filled;
+    }
+    if (a.parts == 1) {
+        const bool lost = !(s[0] == s[0]);
+        sort_keys(keys, have, a.k, [&](int i, Key key) {
+            a.top_index[row * a.k + i] = lost ? -1 : (int)~(unsigned)key;
+            a.top_logit[row * a.k + i] = lost ? __builtin_nanf("") : unordered((unsigned)(key >> 32));
+        });
+        for (int i = have + tid; i < a.k; i += NT) {
+            a.top_index[row * a.k + i] = -1;
+            a.top_logit[row * a.k + i] = lost ? __builtin_nanf("") : -__builtin_inff();
+        }
+    } else {
+        Key *const list = a.lists + (int64_t)blockIdx.x * a.k;
+        sort_keys(keys, have, a.k, [&](int i, Key key) { list[i] = key; });
+        for (int i = have + tid; i < a.k; i += NT) list[i] = 0;
+    }
+}
+
+// Rows of several parts: sums brought to the largest maximum; an entry's place is its own in its list and the number of larger ones
+// in each of the others.
+template <int TYPE, bool LDS>
+__global__ __launch_bounds__(NT) void score_join_kernel(Args a)
+{
+    extern __shared__ Key held[];
+    const int tid = threadIdx.x;
+    const int64_t row = blockIdx.x;
+    const Stats *const st = a.stats + row * a.parts;
+    const Key *const lists = a.lists + row * a.parts * a.k;
+    const int n = a.parts * a.k;
+    if (LDS)
+        for (int i = tid; i < n; i += NT) held[i] = lists[i];
+    const Key *const from = LDS ? held : lists;
+    int target = -1;
+    float zt = 0.f;
+    if (tid == 0) {
+        target = target_of(a, row);
+        if (target >= 0) zt = load_as<TYPE>(a.z, row * a.ldz + target);
+    }
+    const float c2 = 1.44269504088896f / a.tau;
+    float top = -__builtin_inff(), sum = 0.f, dot = 0.f;
+    for (int p = 0; p < a.parts; ++p) top = st[p].sum == 0.f ? top : fmaxf(top, st[p].top);
+    if (top == -__builtin_inff()) top = 0.f;
+    for (int p = 0; p < a.parts; ++p) {
+        const Stats s = st[p];
+        if (s.sum == 0.f) continue;
+        const float d = (s.top - top) * c2, w = __builtin_amdgcn_exp2f(d);
+        sum = fmaf(s.sum, w, sum);
+        dot = fmaf(fmaf(s.sum, fmaxf(d, -1e30f), s.dot), w, dot);
+    }
+    if (tid == 0) finish(a, row, top, sum, dot, zt, target);
+    if (a.k == 0) return;
+    const bool lost = !(sum == sum);
+    __syncthreads();
+    int entries = 0;
+    for (int p = 0; p < a.parts; ++p) {
+        // the entries of a list end where the first 0 is
+        const Key *const l = from + p * a.k;
+        int lo = 0, hi = a.k;
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (l[mid] != 0) lo = mid + 1;
+            else hi = mid;
+        }
+        entries = min(entries + lo, a.k);
+    }
+    for (int e = tid; e < n; e += NT) {
+        const Key key = from[e];
+        if (key == 0) continue;
+        const int own = e / a.k;
+        int rank = e - own * a.k;
+        for (int p = 0; p < a.parts && rank < a.k; ++p) {
+            if (p == own) continue;
+            const Key *const l = from + p * a.k;
+            int lo = 0, hi = a.k;
+            while (lo < hi) {
+                const int mid = (lo + hi) / 2;
+                if (l[mid] > key) lo = mid + 1;
+                else hi = mid;
+            }
+            rank += lo;
+        }
+        if (rank >= a.k) continue;
+        a.top_index[row * a.k + rank] = lost ? -1 : (int)~(unsigned)key;
+        a.top_logit[row * a.k + rank] = lost ? __builtin_nanf("") : unordered((unsigned)(key >> 32));
+    }
+    for (int i = entries + tid; i < a.k; i += NT) {
+        a.top_index[row * a.k + i] = -1;
+        a.top_logit[row * a.k + i] = lost ? __builtin_nanf("") : -__builtin_inff();
+    }
+}
+
+struct Plan {
+    int pieces, parts, len;
+    size_t lists, bytes;
+};
+
+inline Plan plan_of(int T, int V, int type, int k)
+{
+    const int E = type == OBC_F32 ? 4 : 8;
+    Plan p;
+    const int64_t large = (int64_t)NT * 16 * E;
+    p.pieces = k > 256 || (int64_t)T * ((V + large - 1) / large) >= 512 ? 16 : 4;
+    const int64_t most = (int64_t)NT * p.pieces * E;
+    p.parts = (int)((V + most - 1) / most);
+    p.len = (int)(((int64_t)V + p.parts - 1) / p.parts);
+    p.len = (p.len + E - 1) / E * E;
+    p.lists = p.bytes = 0;
+    if (p.parts > 1) {
+        p.lists = obc_align_up((size_t)T * p.parts * sizeof(Stats), 256);
+        p.bytes = p.lists + (size_t)T * p.parts * k * sizeof(Key);
+    }
+    return p;
+}
+
+template <int TYPE>
+void launch(obc_ctx *ctx, const Args &a, int pieces)
+{
+    const unsigned blocks = (unsigned)((int64_t)a.T * a.parts);
+    if (pieces == 16) score_kernel<TYPE, 16><<<blocks, NT, 0, ctx->stream>>>(a);
+    else score_kernel<TYPE, 4><<<blocks, NT, 0, ctx->stream>>>(a);
+    if (a.parts == 1) return;
+    const size_t held = (size_t)a.parts * a.k * sizeof(Key);
+    if (held <= 32768) score_join_kernel<TYPE, true><<<a.T, NT, held, ctx->stream>>>(a);
+    else score_join_kernel<TYPE, false><<<a.T, NT, 0, ctx->stream>>>(a);
+}
+
+}  // namespace
+
+extern "C" {
+
+int obc_score_workspace_bytes(int T, int V, int type, int k, size_t *bytes)
+{
+    if (!bytes || T < 0 || V <= 0 || k < 0 || k > kMaxTop || !float_type(type)) return OBC_ERR_BAD_ARG;
+    *bytes = plan_of(T, V, type, k).bytes;
+    return OBC_OK;
+}
+
+int obc_score(obc_ctx *ctx, const void *z, int type, int T, int V, int64_t ldz, const int32_t *target, float temperature, int k, float *logp,
+              float *entropy, float *lse, int32_t *top_index, float *top_logit, void *ws, size_t ws_bytes)
+{
+    if (!ctx) return OBC_ERR_BAD_ARG;
+    if (T < 0 || V <= 0 || k < 0) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_score: bad size");
+    if (k > kMaxTop || V > kMaxCols)
+        return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_score: k (%d) > %d or V (%d) > %d", k, kMaxTop, V, kMaxCols);
+    if (!float_type(type)) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_score: type %d is not a floating type", type);
+    if (!(temperature > 0.f) || !(temperature < __builtin_inff()) || !(1.44269504088896f / temperature < __builtin_inff()))
+        return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_score: temperature or its reciprocal is not positive and finite");
+    if (ldz < V) return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_score: leading dimension below the row's length");
+    if (T == 0) return OBC_OK;
+    if ((logp != nullptr) != (target != nullptr)) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_score: logp goes with target");
+    if ((k > 0) != (top_index != nullptr) || (k > 0) != (top_logit != nullptr))
+        return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_score: top_index and top_logit go with k > 0");
+    if (!z) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_score: null z");
+    if (((uintptr_t)z & (size_of_type(type) - 1)) != 0) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_score: z is not aligned to its elements");
+    const Plan p = plan_of(T, V, type, k);
+    if (!obc_grid_fits((int64_t)T * p.parts, NT) || (int64_t)p.parts * k >= (int64_t)1 << 30)
+        return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_score: too many rows or columns");
+    if (p.bytes > 0 && (!ws || ((uintptr_t)ws & 15) != 0 || ws_bytes < p.bytes))
+        return obc_fail(ctx, OBC_ERR_WORKSPACE, "obc_score: workspace of %zu bytes needed", p.bytes);
+    const Args a = {z, target, logp, entropy, lse, top_index, top_logit, T, V, k, p.parts, p.len, ldz, temperature, (Stats *)ws,
+                    (Key *)((char *)ws + p.lists), ctx->d_status};
+    if (type == OBC_F32) launch<OBC_F32>(ctx, a, p.pieces);
+    else if (type == OBC_F16) launch<OBC_F16>(ctx, a, p.pieces);
+    else launch<OBC_BF16>(ctx, a, p.pieces);
+    OBC_LAUNCH_CHECK(ctx, "score_kernel");
+    return OBC_OK;
+}
+
+}  // extern "C"
