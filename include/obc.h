@@ -426,7 +426,7 @@ int obc_embed(obc_ctx *ctx, const void *table, int type, int V, int d, int64_t l
 /* The table's gradient: dtable[v] = scale sum over the tokens t with ids[t] = v of dy[t]; every row is written, with zeros where it
  * has no token.  accumulate != 0: dtable[v] += that, rows without a token are not touched.
  *   dy      T x d of `type`, leading dimension lddy >= d;  dtable  V x d of dtable_type, leading dimension lddt >= d
- * Sums are fp32, over an id's tokens in a fixed order; one rounding.  Ids as in obc_embed.  T <= 2^30. */
+ * Sums are fp32, over an id's tokens in a fixed order; one rounding.  Ids as in obc_embed.  T <= 2^26. */
 int obc_embed_grad_workspace_bytes(int T, int V, int d, size_t *bytes);
 int obc_embed_grad(obc_ctx *ctx, const int32_t *ids, int T, const void *dy, int type, int64_t lddy, float scale, int V, int d,
                    int accumulate, void *dtable, int dtable_type, int64_t lddt, void *ws, size_t ws_bytes);

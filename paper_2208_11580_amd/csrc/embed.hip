@@ -5,6 +5,8 @@
 // for its own, counts them per id and per wave, and so knows every one's place (tokens of lower ids are counted on the way).  Then
 // a wave adds up the tokens of a table row in 2048 columns and writes the row, zeros where it has none.  Rows with more tokens than a
 // stretch of the sorted ones holds are summed by stretches first, in parallel, and then over these.
+#include <type_traits>
+
 #include "row_io.h"
 
 namespace {
@@ -42,50 +44,119 @@ __global__ __launch_bounds__(256) void embed_kernel(LookupArgs a)
 }
 
 // ------------------------------------------------------------------------------------------------ order
-constexpr int kWaves = 16, kMostBins = 512;
+constexpr int kWaves = 16, kBins = 512;
+constexpr int kLoads = 8;        // of 64 tokens each, on their way at a time
+constexpr int kPlaces = 16;      // 64 entries each of a wave's list
 
 struct SortArgs {
     const int32_t *ids;
-    int32_t *start;      // V + 1: where each id's tokens begin in `order`
-    int32_t *order;      // tokens by id, those of an id in their order
-    int T, V, bins;      // ids of a slice: a power of two
+    intx2 *rows;         // V: where each id's tokens begin in `order`, and how many they are
+    int32_t *order;      // tokens of an id next to one another, in their order
+    int32_t *total;      // of all ids
+    int T, V, slices;    // a power of two
     int *status;
 };
 
+// A token's place among those of its bin: adds the wave's tokens of each bin to that bin's counter, in the order of the lanes.
+__device__ inline int place_in(int *counters, bool mine, int bin, int bins)
+{
+    const int lane = threadIdx.x & 63;
+    const unsigned long long all = __ballot(mine);
+    unsigned lo = (unsigned)all, hi = (unsigned)(all >> 32);      // the lanes with this one's bin
+    for (int bit = 0; bins - 1 >> bit; ++bit) {
+        const int has = (int)((unsigned)bin << (31 - bit)) >> 31;
+        const unsigned long long set = __ballot(has < 0);
+        lo &= ~((unsigned)set ^ has);
+        hi &= ~((unsigned)(set >> 32) ^ has);
+    }
+    const int first = lo ? __ffs(lo) - 1 : 31 + __ffs(hi), before = __builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0u));
+    int place = 0;
+    if (mine && lane == first) place = atomicAdd(&counters[bin], __popc(lo) + __popc(hi));
+    return __shfl(place, first & 63, 64) + before;
+}
+
+// Workgroup s takes the ids s, s + slices, ... (so that frequent ids, which lie together, fall to different ones).  A wave takes a
+// section of the tokens and lists its own ones first, since few are; mostly the list holds them all, and they are looked for once.
 __global__ __launch_bounds__(64 * kWaves) void embed_sort_kernel(SortArgs a)
 {
-    extern __shared__ int count[];                    // [kWaves][bins]
+    __shared__ int count[kWaves][kBins];
+    __shared__ unsigned listed[kWaves][64 * kPlaces];      // place in the section * kBins + bin
     __shared__ int below[kWaves], scan[kWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int lo = blockIdx.x * a.bins, hi = min(a.V, lo + a.bins) - lo;      // own ids: 0 <= id - lo < hi
+    const int slice = blockIdx.x, low = a.slices - 1, shift = __popc(low), bins = (a.V + low) >> shift;
     const int each = ((a.T + kWaves - 1) / kWaves + 63) / 64 * 64;
     const int64_t from = (int64_t)wave * each;
-    const int to = (int)(from + each < a.T ? from + each : a.T);
-    int *const own = count + wave * a.bins;
-    for (int i = tid; i < kWaves * a.bins; i += 64 * kWaves) count[i] = 0;
-    __syncthreads();
-    int less = 0;
+    const int64_t to = from + each < a.T ? from + each : a.T;
+    int *const own = count[wave];
+    unsigned *const list = listed[wave];
+    int less = 0, n = 0;
     bool bad = false;
-    for (int64_t t0 = from; t0 < to; t0 += 256) {
-        int id[4];
+    int id[kLoads];
+    auto load = [&](int64_t t0) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) id[i] = t0 + i * 64 + lane < to ? a.ids[t0 + i * 64 + lane] : -1;
+        for (int i = 0; i < kLoads; ++i) id[i] = t0 + i * 64 + lane < to ? a.ids[t0 + i * 64 + lane] : -1;
+    };
+    // the wave's own tokens of those loaded, behind the list; the next ones' loads
+    auto find = [&](int64_t t0) {
+        int now[kLoads];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            less += id[i] >= 0 && id[i] < lo;
-            bad |= id[i] >= a.V;
-            if ((unsigned)(id[i] - lo) < (unsigned)hi && id[i] >= 0) atomicAdd(&own[id[i] - lo], 1);
+        for (int i = 0; i < kLoads; ++i) now[i] = id[i];
+        load(t0 + 64 * kLoads);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            bad |= now[i] >= a.V;
+            const bool real = (unsigned)now[i] < (unsigned)a.V;
+            const int part = now[i] & low;
+            less += real && part < slice;
+            const unsigned long long mine = __ballot(real && part == slice);
+            if (mine == 0) continue;
+            const int at = n + __builtin_amdgcn_mbcnt_hi((unsigned)(mine >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mine, 0u));
+            if (real && part == slice) list[at] = (unsigned)(t0 - from + i * 64 + lane) * kBins + (unsigned)(now[i] >> shift);
+            n += __popcll(mine);
         }
+    };
+    int place[kPlaces];
+    // places of the list's tokens among the wave's of their ids
+    auto match = [&]() {
+#pragma unroll
+        for (int i = 0; i < kPlaces; ++i)
+            if (i * 64 < n) {
+                const bool mine = i * 64 + lane < n;
+                place[i] = place_in(own, mine, mine ? (int)(list[i * 64 + lane] % kBins) : 0, bins);
+            }
+    };
+    auto store = [&](bool kept) {
+#pragma unroll
+        for (int i = 0; i < kPlaces; ++i)
+            if (i * 64 < n && i * 64 + lane < n) {
+                const unsigned entry = list[i * 64 + lane];
+                a.order[place[i] + (kept ? own[entry % kBins] : 0)] = (int)(from + entry / kBins);
+            }
+    };
+    for (int i = lane; i < kBins; i += 64) own[i] = 0;
+    bool kept = true;      // the list and the places in it are all of the wave's
+    load(from);
+    for (int64_t t0 = from; t0 < to; t0 += 64 * kLoads) {
+        if (n > 64 * (kPlaces - kLoads)) {
+            match();
+            n = 0;
+            kept = false;
+        }
+        find(t0);
     }
-    if (blockIdx.x == 0 && bad) obc_latch(a.status, OBC_ERR_BAD_ARG);
+    match();
+    if (slice == 0 && bad) obc_latch(a.status, OBC_ERR_BAD_ARG);
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) less += __shfl_xor(less, off, 64);
     if (lane == 0) below[wave] = less;
     __syncthreads();
-    // thread b: id lo + b.  Its tokens in all waves, the ids' running sum, then where each wave's begin
-    int sum = 0;
-    if (tid < a.bins)
-        for (int w = 0; w < kWaves; ++w) sum += count[w * a.bins + tid];
+    // thread b: bin b.  Its tokens in all waves, the bins' running sum, then where each wave's begin
+    int sum = 0, tokens[kWaves];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        tokens[w] = tid < kBins ? count[w][tid] : 0;
+        sum += tokens[w];
+    }
     int run = sum;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
@@ -95,39 +166,37 @@ __global__ __launch_bounds__(64 * kWaves) void embed_sort_kernel(SortArgs a)
     if (lane == 63) scan[wave] = run;
     __syncthreads();
     int at = run - sum;
+#pragma unroll
     for (int w = 0; w < kWaves; ++w) at += below[w] + (w < wave ? scan[w] : 0);
-    if (tid < hi) a.start[lo + tid] = at;
-    if (tid == hi - 1 && lo + hi == a.V) a.start[a.V] = at + sum;
-    if (tid < a.bins)
+    const int64_t row = ((int64_t)tid << shift) + slice;
+    if (tid < bins && row < a.V) a.rows[row] = intx2{at, sum};
+    if (slice == low && tid == kBins - 1) *a.total = at + sum;
+    if (tid < kBins)
+#pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-            const int n = count[w * a.bins + tid];
-            count[w * a.bins + tid] = at;
-            at += n;
+            count[w][tid] = at;
+            at += tokens[w];
         }
     __syncthreads();
-    for (int64_t t0 = from; t0 < to; t0 += 64) {
-        const int id = t0 + lane < to ? a.ids[t0 + lane] : -1;
-        const bool mine = id >= 0 && (unsigned)(id - lo) < (unsigned)hi;
-        unsigned long long same = __ballot(mine);
-        if (same == 0) continue;
-        // the lanes with this one's id
-        const int b = id - lo;
-        for (int bit = 1; bit < a.bins; bit <<= 1) {
-            const unsigned long long has = __ballot(mine && (b & bit));
-            same &= b & bit ? has : ~has;
+    if (kept) return store(true);
+    n = 0;
+    load(from);
+    for (int64_t t0 = from; t0 < to; t0 += 64 * kLoads) {
+        if (n > 64 * (kPlaces - kLoads)) {
+            match();
+            store(false);
+            n = 0;
         }
-        if (!mine) same = 1ull << lane;
-        const int first = __ffsll(same) - 1;
-        int place = 0;
-        if (mine && lane == first) place = atomicAdd(&own[b], __popcll(same));
-        place = __shfl(place, first, 64) + __popcll(same & ((1ull << lane) - 1));
-        if (mine) a.order[place] = (int)(t0 + lane);
+        find(t0);
     }
+    match();
+    store(false);
 }
 
 // ------------------------------------------------------------------------------------------------ sums
 struct GradArgs {
-    const int32_t *ids, *start, *order;
+    const int32_t *ids, *order, *total;
+    const intx2 *rows;
     const void *dy;
     void *dtable;
     float *part;         // per stretch: the sum of a row's tokens that go on from before it, and of one's that go on behind it
@@ -137,116 +206,169 @@ struct GradArgs {
     bool accumulate;
 };
 
-constexpr int kChunk = 512, kChunks = 4;      // columns of a wave's load, loads of a row
+// Columns of a lane, 16 bytes of the wider of the two types: stores and loads of a wave's columns are whole lines
+template <int TYPE, int OT>
+constexpr int kCols = TYPE == OBC_F32 || OT == OBC_F32 ? 4 : 8;
 
-// The sum of the tokens order[from .. to) in the columns c0 + 512 i + 8 lane
-template <int TYPE>
-__device__ inline void add_tokens(const GradArgs &a, int from, int to, int c0, float (&acc)[kChunks][8])
+// `N` columns as fp32; only the first `left` are touched
+template <int TYPE, int N>
+__device__ inline void load_cols(const void *p, int64_t at, int left, float (&v)[N])
 {
-    const int lane = threadIdx.x & 63;
+    if (N == 8) {
+        float w[8];
+        load8<TYPE>(p, at, left, w);
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = w[j];
+    } else if (left >= N && TYPE == OBC_F32) {
+        const floatx4 w = *(const floatx4_at4 *)((const float *)p + at);
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = w[j & 3];
+    } else if (left >= N) {
+        const uintx2 w = *(const uintx2_at2 *)((const unsigned short *)p + at);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const unsigned e = j & 2 ? w.y : w.x;
+            v[j] = TYPE == OBC_F16 ? (j & 1 ? half_hi(e) : half_lo(e)) : (j & 1 ? bf16_hi(e) : bf16_lo(e));
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = j < left ? load_as<TYPE>(p, at + j) : 0.f;
+    }
+}
+
+// (Past the caches: the table's gradient is not read again soon, dy is.)
+template <int TYPE, int N>
+__device__ inline void store_cols(void *p, int64_t at, int left, const float (&v)[N])
+{
+    if (left < N) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (j < left) store_as<TYPE>(p, at + j, v[j]);
+    } else if (TYPE == OBC_F32) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) __builtin_nontemporal_store(floatx4{v[i], v[i + 1], v[i + 2], v[i + 3]}, (floatx4_at4 *)((float *)p + at + i));
+    } else {
+        unsigned w[N / 2];
+#pragma unroll
+        for (int j = 0; j < N / 2; ++j) w[j] = TYPE == OBC_F16 ? pair_f16(v[2 * j], v[2 * j + 1]) : pair_bf16(v[2 * j], v[2 * j + 1]);
+        if (N == 8) __builtin_nontemporal_store(uintx4{w[0], w[1], w[2 % (N / 2)], w[3 % (N / 2)]}, (uintx4_at2 *)((unsigned short *)p + at));
+        else __builtin_nontemporal_store(uintx2{w[0], w[1]}, (uintx2_at2 *)((unsigned short *)p + at));
+    }
+}
+
+// The sum of the tokens order[from .. to) in the columns from c on, MANY tokens on their way at a time
+template <int TYPE, int N, int MANY>
+__device__ inline void add_tokens(const GradArgs &a, int from, int to, int c, float (&acc)[N])
+{
+    const int lane = threadIdx.x & 63, left = a.d - c;
     for (int n0 = from; n0 < to; n0 += 64) {
         const int mine = n0 + lane < to ? a.order[n0 + lane] : 0, n = min(64, to - n0);
-#pragma unroll 2
-        for (int i = 0; i < n; ++i) {
-            const int64_t base = (int64_t)__builtin_amdgcn_readlane(mine, i) * a.lddy;
+        auto add = [&](int i0, auto many) {
+            float v[many][N];
 #pragma unroll
-            for (int k = 0; k < kChunks; ++k) {
-                const int c = c0 + k * kChunk + lane * 8, left = a.d - c;
-                if (left <= 0) continue;
-                float v[8];
-                load8<TYPE>(a.dy, base + c, left, v);
+            for (int i = 0; i < many; ++i)
+                if (left > 0) load_cols<TYPE, N>(a.dy, (int64_t)__builtin_amdgcn_readlane(mine, i0 + i) * a.lddy + c, left, v[i]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) acc[k][j] += v[j];
-            }
-        }
+            for (int i = 0; i < many; ++i)
+#pragma unroll
+                for (int j = 0; j < N; ++j) acc[j] += v[i][j];
+        };
+        int i = 0;
+        for (; i + MANY <= n; i += MANY) add(i, std::integral_constant<int, MANY>());
+        if (MANY > 8 && n & 8) { add(i, std::integral_constant<int, 8>()); i += 8; }
+        if (n & 4) { add(i, std::integral_constant<int, 4>()); i += 4; }
+        if (n & 2) { add(i, std::integral_constant<int, 2>()); i += 2; }
+        if (n & 1) add(i, std::integral_constant<int, 1>());
     }
 }
 
-// The stretches' shares of rows with more than `stretch` tokens
+// The stretches' shares of rows with more than `stretch` tokens: 64 N columns of one to a wave
 template <int TYPE>
-__global__ __launch_bounds__(64) void embed_stretch_kernel(GradArgs a)
+__global__ __launch_bounds__(256) void embed_stretch_kernel(GradArgs a)
 {
-    const int total = a.start[a.V], c0 = blockIdx.y * kChunk * kChunks;
-    const int64_t from64 = (int64_t)blockIdx.x * a.stretch;
+    constexpr int N = kCols<TYPE, OBC_F32>;
+    const int c = (blockIdx.y * 256 + threadIdx.x) * N, left = a.d - c;
+    const int total = *a.total;
+    const int64_t from64 = (int64_t)(blockIdx.x >> 1) * a.stretch;
+    const int half = blockIdx.x & 1;
     if (from64 >= total) return;
     const int from = (int)from64, to = (int)min((int64_t)total, from64 + a.stretch);
-    for (int half = 0; half < 2; ++half) {
-        const int id = a.ids[a.order[half ? to - 1 : from]];
-        const int s = a.start[id], e = a.start[id + 1];
-        if (e - s <= a.stretch || (half && s <= from)) continue;
-        float acc[kChunks][8] = {};
-        add_tokens<TYPE>(a, max(s, from), min(e, to), c0, acc);
-#pragma unroll
-        for (int k = 0; k < kChunks; ++k) {
-            const int c = c0 + k * kChunk + (threadIdx.x & 63) * 8, left = a.d - c;
-            if (left > 0) store8<OBC_F32>(a.part, ((int64_t)blockIdx.x * 2 + half) * a.d + c, left, acc[k]);
-        }
-    }
+    const int id = a.ids[a.order[half ? to - 1 : from]];
+    const intx2 own = a.rows[id];
+    const int s = own.x, e = s + own.y;
+    if (own.y <= a.stretch || (half && s <= from)) return;
+    float acc[N] = {};
+    add_tokens<TYPE, N, 8>(a, max(s, from), min(e, to), c, acc);
+    if (left >= N) *(floatx4_at4 *)(a.part + (int64_t)blockIdx.x * a.d + c) = floatx4{acc[0], acc[1], acc[2], acc[3]};
+    else
+        for (int j = 0; j < N; ++j)
+            if (j < left) a.part[(int64_t)blockIdx.x * a.d + c + j] = acc[j];
 }
 
-// A table row in 2048 columns to a wave, four rows to a workgroup
+// 64 N columns of a table row to a wave, four rows to a workgroup
 template <int TYPE, int OT>
 __global__ __launch_bounds__(256) void embed_grad_kernel(GradArgs a)
 {
-    const int lane = threadIdx.x & 63, c0 = blockIdx.y * kChunk * kChunks;
+    constexpr int N = kCols<TYPE, OT>;
+    const int c = (blockIdx.y * 64 + (threadIdx.x & 63)) * N, left = a.d - c;
     const int64_t v = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (v >= a.V) return;
-    const int s = a.start[v], e = a.start[v + 1];
+    const intx2 own = a.rows[v];
+    const int s = own.x, e = s + own.y;
     if (a.accumulate && s == e) return;
-    float acc[kChunks][8] = {};
+    float acc[N] = {};
     if (e - s <= a.stretch) {
-        add_tokens<TYPE>(a, s, e, c0, acc);
-    } else {
+        add_tokens<TYPE, N, 8>(a, s, e, c, acc);
+    } else if (left > 0) {
         const int first = s / a.stretch, last = (e - 1) / a.stretch;
-        for (int p = first; p <= last; ++p) {
-            const int64_t base = ((int64_t)p * 2 + (p == first && s > p * a.stretch)) * a.d;
+        const float *p = a.part + ((int64_t)first * 2 + (s > first * a.stretch)) * a.d + c;
+        load_cols<OBC_F32, N>(p, 0, left, acc);
+        p = a.part + c;
+        for (int q = first + 1; q <= last; q += 8) {
+            float x[8][N];
 #pragma unroll
-            for (int k = 0; k < kChunks; ++k) {
-                const int c = c0 + k * kChunk + lane * 8, left = a.d - c;
-                if (left <= 0) continue;
-                float x[8];
-                load8<OBC_F32>(a.part, base + c, left, x);
+            for (int i = 0; i < 8; ++i)
+                if (q + i <= last) load_cols<OBC_F32, N>(p, (int64_t)(q + i) * 2 * a.d, left, x[i]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) acc[k][j] += x[j];
-            }
+            for (int i = 0; i < 8; ++i)
+                if (q + i <= last)
+#pragma unroll
+                    for (int j = 0; j < N; ++j) acc[j] += x[i][j];
         }
     }
+    if (left <= 0) return;
+    float old[N] = {};
+    if (a.accumulate) load_cols<OT, N>(a.dtable, v * a.lddt + c, left, old);
 #pragma unroll
-    for (int k = 0; k < kChunks; ++k) {
-        const int c = c0 + k * kChunk + lane * 8, left = a.d - c;
-        if (left <= 0) continue;
-        float old[8];
-        if (a.accumulate) load8<OT>(a.dtable, v * a.lddt + c, left, old);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) acc[k][j] = a.accumulate ? fmaf(acc[k][j], a.scale, old[j]) : s < e ? acc[k][j] * a.scale : 0.f;
-        store8<OT>(a.dtable, v * a.lddt + c, left, acc[k]);
-    }
+    for (int j = 0; j < N; ++j) acc[j] = a.accumulate ? fmaf(acc[j], a.scale, old[j]) : s < e ? acc[j] * a.scale : 0.f;
+    store_cols<OT, N>(a.dtable, v * a.lddt + c, left, acc);
 }
 
-inline int bins_of(int V)
+// Workgroups that sort: one to a compute unit, or more where each would have more ids than it has counters for
+inline int slices_of(int V)
 {
-    int bins = 64;
-    while (bins < kMostBins && (int64_t)bins * 256 < V) bins *= 2;
-    return bins;
+    int n = 256;
+    while ((int64_t)n * kBins < V) n *= 2;
+    return n;
 }
 
-// Tokens of a stretch: rows with more are summed in two steps
+// Tokens of a stretch: rows with more are summed in two steps, in another launch, which a hundred tokens are not worth
 inline int stretch_of(int T)
 {
-    int n = 32;
+    int n = T <= 128 ? 128 : 32;
     while ((int64_t)n * 512 < T) n *= 2;
     return n;
 }
 
 struct Plan {
-    size_t start, order, part, bytes;
+    size_t rows, order, part, bytes;      // (the total lies before the rows)
 };
 
 inline Plan plan_of(int T, int V, int d)
 {
     Plan p;
-    p.start = 0;
-    p.order = obc_align_up(((size_t)V + 1) * 4, 256);
+    p.rows = 256;
+    p.order = p.rows + obc_align_up((size_t)V * 8, 256);
     p.part = p.order + obc_align_up((size_t)T * 4, 256);
     const int n = stretch_of(T);
     p.bytes = p.part + (T > n ? ((size_t)T + n - 1) / n * 2 * (size_t)d * 4 : 0);
@@ -267,19 +389,24 @@ void launch_lookup(obc_ctx *ctx, const LookupArgs &a, int y_type)
     else launch_lookup<TYPE, OBC_BF16>(ctx, a);
 }
 
+inline int type_cols(int type, int out_type) { return type == OBC_F32 || out_type == OBC_F32 ? 4 : 8; }
+
 template <int TYPE>
 void launch_grad(obc_ctx *ctx, const GradArgs &a, int out_type)
 {
-    const unsigned chunks = (a.d + kChunk * kChunks - 1) / (kChunk * kChunks);
-    if (a.T > a.stretch)
-        embed_stretch_kernel<TYPE><<<dim3(((int64_t)a.T + a.stretch - 1) / a.stretch, chunks), 64, 0, ctx->stream>>>(a);
-    const dim3 grid((unsigned)(((int64_t)a.V + 3) / 4), chunks);
+    if (a.T > a.stretch) {
+        constexpr int N = kCols<TYPE, OBC_F32>;
+        const dim3 grid((unsigned)(((int64_t)a.T + a.stretch - 1) / a.stretch * 2), (a.d + 256 * N - 1) / (256 * N));
+        embed_stretch_kernel<TYPE><<<grid, 256, 0, ctx->stream>>>(a);
+    }
+    const int n = type_cols(TYPE, out_type);
+    const dim3 grid((unsigned)(((int64_t)a.V + 3) / 4), (a.d + 64 * n - 1) / (64 * n));
     if (out_type == OBC_F32) embed_grad_kernel<TYPE, OBC_F32><<<grid, 256, 0, ctx->stream>>>(a);
     else if (out_type == OBC_F16) embed_grad_kernel<TYPE, OBC_F16><<<grid, 256, 0, ctx->stream>>>(a);
     else embed_grad_kernel<TYPE, OBC_BF16><<<grid, 256, 0, ctx->stream>>>(a);
 }
 
-constexpr int kMostCols = 1 << 20, kMostTokens = 1 << 30;
+constexpr int kMostCols = 1 << 20, kMostTokens = 1 << 26;
 
 }  // namespace
 
@@ -329,17 +456,18 @@ int obc_embed_grad(obc_ctx *ctx, const int32_t *ids, int T, const void *dy, int 
     if (!dtable || (T > 0 && (!ids || !dy))) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_embed_grad: null argument");
     if ((T > 0 && (((uintptr_t)dy & (size_of_type(type) - 1)) != 0 || ((uintptr_t)ids & 3) != 0)) || ((uintptr_t)dtable & (size_of_type(dtable_type) - 1)) != 0)
         return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_embed_grad: an array is not aligned to its elements");
-    const int64_t chunks = (d + kChunk * kChunks - 1) / (kChunk * kChunks);
+    const int n = 64 * type_cols(type, dtable_type);
+    const int64_t chunks = (d + n - 1) / n;
     if (!obc_grid_fits(((int64_t)V + 3) / 4 * chunks, 256)) return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_embed_grad: too many table rows");
     const Plan p = plan_of(T, V, d);
     if (!ws || ((uintptr_t)ws & 15) != 0 || ws_bytes < p.bytes)
         return obc_fail(ctx, OBC_ERR_WORKSPACE, "obc_embed_grad: workspace of %zu bytes needed", p.bytes);
-    int32_t *const start = (int32_t *)ws, *const order = (int32_t *)((char *)ws + p.order);
-    const int bins = bins_of(V);
-    const SortArgs sort = {ids, start, order, T, V, bins, ctx->d_status};
-    embed_sort_kernel<<<(unsigned)(((int64_t)V + bins - 1) / bins), 64 * kWaves, (size_t)kWaves * bins * 4, ctx->stream>>>(sort);
+    int32_t *const total = (int32_t *)ws, *const order = (int32_t *)((char *)ws + p.order);
+    intx2 *const rows = (intx2 *)((char *)ws + p.rows);
+    const int slices = slices_of(V);
+    embed_sort_kernel<<<slices, 64 * kWaves, 0, ctx->stream>>>(SortArgs{ids, rows, order, total, T, V, slices, ctx->d_status});
     OBC_LAUNCH_CHECK(ctx, "embed_sort_kernel");
-    const GradArgs a = {ids, start, order, dy, dtable, (float *)((char *)ws + p.part), T, V, d, stretch_of(T), lddy, lddt, scale, accumulate != 0};
+    const GradArgs a = {ids, order, total, rows, dy, dtable, (float *)((char *)ws + p.part), T, V, d, stretch_of(T), lddy, lddt, scale, accumulate != 0};
     if (type == OBC_F32) launch_grad<OBC_F32>(ctx, a, dtable_type);
     else if (type == OBC_F16) launch_grad<OBC_F16>(ctx, a, dtable_type);
     else launch_grad<OBC_BF16>(ctx, a, dtable_type);

@@ -15,6 +15,7 @@ typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
 typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
 // the same, at any element's address
 typedef unsigned uintx4_at2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef unsigned uintx2_at2 __attribute__((ext_vector_type(2), aligned(2)));
 typedef unsigned uintx2_at1 __attribute__((ext_vector_type(2), aligned(1)));
 typedef float floatx4_at4 __attribute__((ext_vector_type(4), aligned(4)));
 
