@@ -431,7 +431,7 @@ int obc_embed_grad_workspace_bytes(int T, int V, int d, size_t *bytes);
 int obc_embed_grad(obc_ctx *ctx, const int32_t *ids, int T, const void *dy, int type, int64_t lddy, float scale, int V, int d,
                    int accumulate, void *dtable, int dtable_type, int64_t lddt, void *ws, size_t ws_bytes);
 
-/* A tensor of obc_adamw: n elements each, contiguous.  Inputs and outputs may be the same arrays (the usual case) or others that
+/* A tensor of obc_adamw_plan: n elements each, contiguous.  Inputs and outputs may be the same arrays (the usual case) or others that
  * do not overlap. */
 typedef struct obc_adamw_tensor {
     const void *p;                  /* parameters, of `type` */
@@ -449,20 +449,28 @@ typedef struct obc_adamw_tensor {
     float decay;
 } obc_adamw_tensor;
 
-/* One step of AdamW over `count` tensors:
+/* Lay out `count` tensors for obc_adamw, which takes them in one launch.
+ *   tensors     HOST array; it may go when the call returns
+ *   bits        of the moments: 32 or 8
+ *   plan        obc_adamw_plan_bytes on the device, aligned to 16 bytes, opaque; written on the context's stream
+ *   workgroups  HOST out, for obc_adamw.  (2^24 - 1 at most, of 2048 elements of a tensor each.) */
+int obc_adamw_plan_bytes(int count, size_t *bytes);
+int obc_adamw_plan(obc_ctx *ctx, const obc_adamw_tensor *tensors, int count, int type, int bits, void *plan, int64_t *workgroups);
+
+/* One step of AdamW over a plan's tensors:
  *   g' = g grad_scale,  m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2
  *   p = p (1 - lr decay) - lr m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps)
  * in fp32, on master where there is one; p is rounded to nearest from that.
- *   tensors   HOST array; it may go when the call returns
- *   bits      of the moments: 32 or 8.  8: m and sqrt(v) are divided by their block's scale, its largest magnitude / 448, and rounded
- *             up or down with the chances that keep them on average, by a hash of seed, step, the tensor's place in the list and the
- *             element's in the tensor; sqrt(v) > 0 is never rounded to 0.  A block whose largest is below 1e-30 becomes zeros.
- *             A block with a NaN or an infinity gets scale NaN.
- *   step      1 for the first; step_at (device, nullable) is read in its place.  lr_at (device, nullable) in lr's place.
- *             Neither is changed.  A step_at below 1 latches OBC_ERR_BAD_ARG and leaves all values as they are.
+ *   count, workgroups, type, bits   the plan's
+ *   step        1 for the first; step_at (device, nullable) is read in its place.  lr_at (device, nullable) in lr's place.
+ *               Neither is changed.  A step_at below 1 latches OBC_ERR_BAD_ARG and leaves all values as they are.
  *   grad_scale  device, nullable (1): a loss scale's reciprocal or a clipping factor.  Infinite or NaN: all values stay as they are.
- * 0 <= beta < 1, eps > 0.  Results do not depend on how tensors are listed, but for the hash. */
-int obc_adamw(obc_ctx *ctx, const obc_adamw_tensor *tensors, int count, int type, int bits, int64_t step, const int64_t *step_at,
+ * Moments of 8 bits: m and sqrt(v) are divided by their block's scale, its largest magnitude / 448, and rounded up or down with the
+ * chances that keep them on average, by a hash of seed, step, the tensor's place in the list and the element's in the tensor (in 64
+ * bits where fp32 would not decide surely); sqrt(v) > 0 is never rounded to 0.  A block whose largest is below 1e-30 becomes zeros.  A
+ * block with a NaN or an infinity gets scale NaN.
+ * 0 <= beta < 1, eps >= 2^-120.  A v below fp32's smallest normal number may count as zero in p's step.  Results do not depend on how tensors are listed, but for the hash. */
+int obc_adamw(obc_ctx *ctx, const void *plan, int count, int64_t workgroups, int type, int bits, int64_t step, const int64_t *step_at,
               float lr, const float *lr_at, double beta1, double beta2, float eps, const float *grad_scale, uint32_t seed);
 
 #ifdef __cplusplus

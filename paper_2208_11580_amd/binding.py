@@ -41,7 +41,8 @@ EXPORTS = [
     "obc_rmsnorm", "obc_rmsnorm_grad_workspace_bytes", "obc_rmsnorm_grad", "obc_distill",
     "obc_score_workspace_bytes", "obc_score",
     "obc_layernorm", "obc_layernorm_grad_workspace_bytes", "obc_layernorm_grad",
-    "obc_embed", "obc_embed_grad_workspace_bytes", "obc_embed_grad", "obc_adamw",
+    "obc_embed", "obc_embed_grad_workspace_bytes", "obc_embed_grad",
+    "obc_adamw_plan_bytes", "obc_adamw_plan", "obc_adamw",
 ]
 
 _TYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16, torch.int8: I8}
@@ -152,7 +153,9 @@ def load_library():
     lib.obc_embed.argtypes = [vp, vp, c_int, c_int, c_int, i64, vp, c_int, c_float, vp, c_int, i64]
     lib.obc_embed_grad_workspace_bytes.argtypes = [c_int, c_int, c_int, sp]
     lib.obc_embed_grad.argtypes = [vp, vp, c_int, vp, c_int, i64, c_float, c_int, c_int, c_int, vp, c_int, i64, vp, c_size_t]
-    lib.obc_adamw.argtypes = [vp, vp, c_int, c_int, c_int, i64, vp, c_float, vp, ctypes.c_double, ctypes.c_double, c_float, vp,
+    lib.obc_adamw_plan_bytes.argtypes = [c_int, sp]
+    lib.obc_adamw_plan.argtypes = [vp, vp, c_int, c_int, c_int, vp, POINTER(i64)]
+    lib.obc_adamw.argtypes = [vp, vp, c_int, i64, c_int, c_int, i64, vp, c_float, vp, ctypes.c_double, ctypes.c_double, c_float, vp,
                               ctypes.c_uint32]
     for name in EXPORTS:
         fn = getattr(lib, name)
@@ -225,11 +228,11 @@ def _no_grad(*tensors):
 
 
 class AdamPlan:
-    """The tensors of obc_adamw, which it keeps, and their addresses as the C entry point takes them."""
+    """The tensors of obc_adamw, which it keeps, laid out by obc_adamw_plan."""
 
-    def __init__(self, params, grads, states, decay=0.01, out=None):
+    def __init__(self, ctx, params, grads, states, decay=0.01, out=None):
         params, states = list(params), list(states)
-        self.params, self.states = params, states
+        self.ctx, self.params, self.states = ctx, params, states
         self.new = (params, states) if out is None else (list(out[0]), list(out[1]))
         self.count = count = len(params)
         if not len(states) == len(self.new[0]) == len(self.new[1]) == count:
@@ -254,6 +257,10 @@ class AdamPlan:
                                       ("master", torch.float32, n)):
                 setattr(d, name, self._at(i, getattr(st, name), dtype, size))
                 setattr(d, name + "_out", self._at(i, getattr(new, name), dtype, size))
+        need = c_size_t()
+        ctx.lib.obc_adamw_plan_bytes(count, byref(need))
+        self.data = ctx._empty((max(need.value, 16),), torch.uint8, ctx.stream.device)
+        self.address = self.data.data_ptr()
         self.use(grads)
 
     @staticmethod
@@ -263,14 +270,17 @@ class AdamPlan:
         return _ptr(t, dtype)
 
     def use(self, grads):
-        """Other gradients from the next step on."""
+        """Other gradients from the next step on (on the context's stream: steps before this call keep theirs)."""
         grads = list(grads)
         if len(grads) != self.count:
             raise ValueError("there must be as many gradients as parameters")
-        for i, g in enumerate(grads):
-            _no_grad(g)
-            self.tensors[i].g = self._at(i, g, self.params[0].dtype, self.params[i].numel())
-        self.grads = grads
+        addresses = [self._at(i, g, self.params[0].dtype, self.params[i].numel()) for i, g in enumerate(grads)]
+        _no_grad(*grads)
+        for t, g in zip(self.tensors, addresses):
+            t.g = g
+        n = c_int64()
+        self.ctx._ck(self.ctx.lib.obc_adamw_plan(self.ctx.h, self.tensors, self.count, self.type, self.bits, self.address, byref(n)))
+        self.workgroups, self.grads = n.value, grads
 
 
 class Context:
@@ -864,7 +874,7 @@ class Context:
         """The lists of parameters, gradients of their type, and AdamStates (all of 32 or all of 8 bits) that obc_adamw goes over, as it
         takes them; kept from step to step.  decay: a float or one for each tensor.  Steps are in place, unless out holds other
         parameters and states."""
-        return AdamPlan(params, grads, states, decay, out)
+        return AdamPlan(self, params, grads, states, decay, out)
 
     def obc_adamw(self, plan, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=None, seed=0):
         """A step of AdamW over an AdamPlan's tensors.  step: an int, 1 for the first, or an int64 tensor on the device; lr: a float or
@@ -876,8 +886,8 @@ class Context:
             step_at, step = _ptr(step, torch.int64), 0
         if torch.is_tensor(lr):
             lr_at, lr = _vector(lr, 1, "lr"), 0.0
-        rc = self.lib.obc_adamw(self.h, plan.tensors, plan.count, plan.type, plan.bits, int(step), step_at, float(lr), lr_at,
-                                float(beta1), float(beta2), float(eps), _vector(grad_scale, 1, "grad_scale"), int(seed) & 0xffffffff)
+        rc = self.lib.obc_adamw(self.h, plan.address, plan.count, plan.workgroups, plan.type, plan.bits, int(step), step_at, float(lr),
+                                lr_at, float(beta1), float(beta2), float(eps), _vector(grad_scale, 1, "grad_scale"), int(seed) & 0xffffffff)
         if rc != OBC_OK:
             self._ck(rc)
         return plan.new

@@ -1,4 +1,4 @@
-// obc_adamw: a step of AdamW over many tensors in one launch for every kTensors of them.
+// obc_adamw: a step of AdamW over many tensors in one launch; obc_adamw_plan writes their descriptors to device memory once.
 //
 //   g' = g grad_scale;  m = b1 m + (1 - b1) g';  v = b2 v + (1 - b2) g'^2
 //   p = p (1 - lr decay) - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps)
@@ -10,18 +10,45 @@
 
 namespace {
 
-constexpr int kTensors = 32;      // of a launch: their descriptors go with its arguments
+constexpr int kWritten = 24;      // descriptors that a launch of the plan's kernel takes with its arguments
 constexpr int NT = 256, E = 8, kChunk = NT * E;
+constexpr int64_t kMostBlocks = (1 << 24) - 1;      // a launch holds fewer than 2^32 threads
 constexpr int kScaled = 256;      // 8-bit moments that share a scale: 32 lanes' elements
 constexpr float kTop8 = 448.f;    // the largest of the 8-bit numbers (4 bits of exponent, 3 of mantissa)
 
+// A plan: the tensors' descriptors, and from which workgroup on each is
+struct Layout {
+    size_t first, bytes;
+};
+inline Layout layout_of(int count)
+{
+    const size_t t = obc_align_up((size_t)count * sizeof(obc_adamw_tensor), 256);
+    return Layout{t, t + obc_align_up((size_t)count * 4, 256)};
+}
+
+struct PlanArgs {
+    obc_adamw_tensor t[kWritten];
+    unsigned first[kWritten];
+    int tensors;
+    obc_adamw_tensor *to;
+    unsigned *first_to;
+};
+
+__global__ __launch_bounds__(64) void adamw_plan_kernel(PlanArgs a)
+{
+    const int i = threadIdx.x;
+    if (i >= a.tensors) return;
+    a.to[i] = a.t[i];
+    a.first_to[i] = a.first[i];
+}
+
 struct Args {
-    obc_adamw_tensor t[kTensors];
-    unsigned first[kTensors];      // the first workgroup of each tensor
-    int tensors, ordinal;
+    const obc_adamw_tensor *t;
+    const unsigned *first;
+    int tensors;
     const int64_t *step;
     const float *lr_at, *grad_scale;
-    double beta1, beta2;
+    double beta1, beta2, root_b2, root_n2;      // and the roots of beta2 and 1 - beta2
     float lr, c1, c2, eps;
     unsigned key;                  // the seed's part of the hash
     int *status;
@@ -38,6 +65,8 @@ __device__ inline double one_minus_power(double b, int64_t t)
     return 1.0 - r;
 }
 
+constexpr unsigned kClose = 6;
+
 // 32 bits from an element's place: odd multipliers (of the fractions of the golden ratio, the root of 2, and pi) and shifts
 __device__ inline unsigned mix(unsigned h)
 {
@@ -49,18 +78,55 @@ __device__ inline unsigned mix(unsigned h)
     return h ^ h >> 16;
 }
 
-// a (0 .. 448) on the 8-bit numbers' grid: eight steps to an octave, down to 2^-9; up with a chance of the distance
-__device__ inline float on_grid(float a, unsigned u16)
+// a (0 .. 448) on the 8-bit numbers' grid: eight steps to an octave, down to 2^-9; up with a chance of the distance.  From 2^-6 on that
+// is to add u, 20 bits of chance, to the 20 bits that go, and what is smaller is moved there first.  edge: how near to where the sum
+// turns it fell, at least, in units of a float's last place.
+__device__ inline float on_grid(float a, unsigned u, unsigned &edge)
 {
-    const int e = max((int)(__builtin_bit_cast(unsigned, a) >> 23), 127 - 6) - 3;      // exponent of the grid's step
-    const float q = __builtin_bit_cast(float, (unsigned)e << 23), per = __builtin_bit_cast(float, (unsigned)(254 - e) << 23);
-    return floorf(a * per + (float)u16 * 0x1p-16f) * q;
+    const float off = a < 0x1p-6f ? 0x1p-6f : 0.f;
+    const unsigned sum = __builtin_bit_cast(unsigned, a + off) + u;
+    edge = min(edge, (sum + kClose) & 0xfffffu);
+    return __builtin_bit_cast(float, sum & 0xfff00000u) - off;
 }
 
-__device__ inline float over_block(float v)
+__device__ inline double on_grid(double a, unsigned u16)
+{
+    const int e = max((int)(__builtin_bit_cast(unsigned long long, a) >> 52), 1023 - 6) - 3;
+    const double q = __builtin_bit_cast(double, (unsigned long long)e << 52), per = __builtin_bit_cast(double, (unsigned long long)(2046 - e) << 52);
+    return floor(a * per + (double)u16 * 0x1p-16) * q;
+}
+
+// The first element to the end
+template <typename V>
+__device__ inline void turn(V (&v)[8])
+{
+    const V first = v[0];
+#pragma unroll
+    for (int j = 0; j < 7; ++j) v[j] = v[j + 1];
+    v[7] = first;
+}
+
+__device__ inline void turn_bytes(unsigned (&w)[2])
+{
+    const unsigned lo = __builtin_amdgcn_alignbyte(w[1], w[0], 1), hi = __builtin_amdgcn_alignbyte(w[0], w[1], 1);
+    w[0] = lo;
+    w[1] = hi;
+}
+
+__device__ inline double over_block(double v)
 {
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) v = larger(v, __shfl_xor(v, off, 64));
+    for (int off = 16; off > 0; off >>= 1) {
+        const double o = __shfl_xor(v, off, 64);
+        v = o > v ? o : v;
+    }
+    return v;
+}
+
+__device__ inline unsigned over_block(unsigned v)
+{
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) v = max(v, (unsigned)__shfl_xor((int)v, off, 64));
     return v;
 }
 
@@ -91,13 +157,30 @@ __device__ inline void store_bytes(void *p, int64_t at, int left, const unsigned
         if (j < left) q[j] = (uint8_t)(w[j >> 2] >> (8 * (j & 3)));
 }
 
-__device__ inline void decode(const unsigned (&w)[2], float scale, float (&v)[8])
+// As store8, past the caches: the next step finds nothing of this one there anyway.
+template <int TYPE>
+__device__ inline void put8(void *p, int64_t at, int left, const float (&v)[8])
+{
+    if (left < 8) return store8<TYPE>(p, at, left, v);
+    if (TYPE == OBC_F32) {
+        floatx4_at4 *const q = (floatx4_at4 *)((float *)p + at);
+        __builtin_nontemporal_store(floatx4{v[0], v[1], v[2], v[3]}, q);
+        __builtin_nontemporal_store(floatx4{v[4], v[5], v[6], v[7]}, (floatx4_at4 *)((float *)p + at + 4));
+    } else {
+        uintx4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = TYPE == OBC_F16 ? pair_f16(v[2 * j], v[2 * j + 1]) : pair_bf16(v[2 * j], v[2 * j + 1]);
+        __builtin_nontemporal_store(w, (uintx4_at2 *)((unsigned short *)p + at));
+    }
+}
+
+__device__ inline void decode(const unsigned (&w)[2], float (&v)[8])
 {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const auto pair = j & 1 ? __builtin_amdgcn_cvt_pk_f32_fp8(w[j >> 1], true) : __builtin_amdgcn_cvt_pk_f32_fp8(w[j >> 1], false);
-        v[2 * j] = pair[0] * scale;
-        v[2 * j + 1] = pair[1] * scale;
+        v[2 * j] = pair[0];
+        v[2 * j + 1] = pair[1];
     }
 }
 
@@ -112,15 +195,21 @@ __device__ inline void encode(const float (&v)[8], unsigned (&w)[2])
 }
 
 template <int TYPE, bool BITS8>
-__global__ __launch_bounds__(NT) void adamw_kernel(Args a)
+__global__ __launch_bounds__(NT, BITS8 ? 5 : 4) void adamw_kernel(Args a)
 {
     __shared__ float shared[2];
     const int tid = threadIdx.x;
-    // the tensor: the last that begins at or before this workgroup
+    // the tensor: the last that begins at or before this workgroup, 64 of them looked at in a step
     const int lane = tid & 63;
-    const unsigned begins = a.first[lane < kTensors ? lane : 0];
-    const int n_before = __popcll(__ballot(lane < a.tensors && lane < kTensors && begins <= blockIdx.x));
-    const int ti = __builtin_amdgcn_readfirstlane(n_before - 1);
+    int ti = 0;
+    for (int span = a.tensors; span > 1;) {
+        const int each = (span + 63) >> 6;
+        const int i = lane * each;
+        const int n = __popcll(__ballot(i < span && a.first[ti + (i < span ? i : 0)] <= blockIdx.x)) - 1;
+        ti += n * each;
+        span = min(each, span - n * each);
+    }
+    ti = __builtin_amdgcn_readfirstlane(ti);
     const obc_adamw_tensor t = a.t[ti];
     const int64_t at = (int64_t)(blockIdx.x - a.first[ti]) * kChunk + tid * E, left64 = t.n - at;
     const int left = left64 < 0 ? 0 : left64 > E ? E : (int)left64;
@@ -155,68 +244,115 @@ __global__ __launch_bounds__(NT) void adamw_kernel(Args a)
         key += (unsigned)step * 0xBB67AE85u;
     }
     const float lr = a.lr_at ? *a.lr_at : a.lr, gs = a.grad_scale ? *a.grad_scale : 1.f;
-    const float b1 = (float)a.beta1, b2 = (float)a.beta2, n1 = (float)(1.0 - a.beta1), n2 = (float)(1.0 - a.beta2);
     const bool skip = !(fabsf(gs) < __builtin_inff()) || (a.step && step < 1);
     if (a.step && step < 1 && blockIdx.x == 0 && tid == 0) obc_latch(a.status, OBC_ERR_BAD_ARG);
     const float keep = (float)(1.0 - (double)lr * (double)t.decay), rate = lr * c1;
+    const float gm = (float)(gs * (1.0 - a.beta1)), gv = (float)(gs * a.root_n2), b1 = (float)a.beta1, b2 = (float)a.beta2;
     float root[8];
     if (BITS8) {
-        decode(m8, m_scale, m);
-        decode(v8, v_scale, root);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = root[j] * root[j];
+        decode(m8, m);
+        decode(v8, root);
     }
     if (!skip) {
+        const float sm = m_scale * b1, sv = v_scale * (float)a.root_b2;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float x = g[j] * gs;
-            m[j] = fmaf(m[j], b1, x * n1);
-            v[j] = fmaf(v[j], b2, x * x * n2);
-            root[j] = sqrtf(v[j]);
-            p[j] = p[j] * keep - rate * m[j] / fmaf(root[j], c2, a.eps);
+            const float x = g[j] * gv;
+            m[j] = fmaf(g[j], gm, m[j] * (BITS8 ? sm : b1));
+            if (BITS8) {
+                root[j] *= sv;
+                v[j] = fmaf(root[j], root[j], x * x);
+            } else {
+                v[j] = fmaf(v[j], b2, x * x);
+            }
+            root[j] = __builtin_amdgcn_sqrtf(v[j]);      // (to a unit in the last place)
+            p[j] = fmaf(p[j], keep, -rate * m[j] * __builtin_amdgcn_rcpf(fmaf(root[j], c2, a.eps)));
         }
     }
     if (left > 0) {
-        if (master) store8<OBC_F32>(t.master_out, at, left, p);
-        if (!(skip && master)) store8<TYPE>(t.p_out, at, left, p);
+        if (master) put8<OBC_F32>(t.master_out, at, left, p);
+        if (!(skip && master)) put8<TYPE>(t.p_out, at, left, p);
     }
     if (skip && master && left > 0) {      // the parameters as they were, which need not be the copies rounded
         float old[8];
         load8<TYPE>(t.p, at, left, old);
-        store8<TYPE>(t.p_out, at, left, old);
+        put8<TYPE>(t.p_out, at, left, old);
     }
     if (!BITS8) {
         if (left > 0) {
-            store8<OBC_F32>(t.m_out, at, left, m);
-            store8<OBC_F32>(t.v_out, at, left, v);
+            put8<OBC_F32>(t.m_out, at, left, m);
+            put8<OBC_F32>(t.v_out, at, left, v);
         }
         return;
     }
     if (!skip) {
-        float top_m = 0.f, top_v = 0.f;
+        // the largest magnitudes, by their bits: a NaN is larger than an infinity, that than any number.  (Beyond the end all are zero.)
+        unsigned bits_m = 0u, bits_v = 0u;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            top_m = larger(top_m, j < left ? m[j] : 0.f);
-            top_v = larger(top_v, j < left ? root[j] : 0.f);
+            bits_m = max(bits_m, __builtin_bit_cast(unsigned, m[j]) & 0x7fffffffu);
+            bits_v = max(bits_v, __builtin_bit_cast(unsigned, root[j]) & 0x7fffffffu);
         }
-        top_m = over_block(top_m);
-        top_v = over_block(top_v);
+        const float top_m = __builtin_bit_cast(float, over_block(bits_m)), top_v = __builtin_bit_cast(float, over_block(bits_v));
         // (a block whose largest number is next to nothing, below 1e-30, is taken for zeros: its reciprocal would not be finite)
         const bool lost_m = !(top_m < __builtin_inff()), lost_v = !(top_v < __builtin_inff());
-        const float up_m = !lost_m && top_m > 1e-30f ? kTop8 / top_m : 0.f, up_v = !lost_v && top_v > 1e-30f ? kTop8 / top_v : 0.f;
-        m_scale = lost_m ? __builtin_nanf("") : top_m > 1e-30f ? top_m / kTop8 : 0.f;
-        v_scale = lost_v ? __builtin_nanf("") : top_v > 1e-30f ? top_v / kTop8 : 0.f;
-        const unsigned base = key + (unsigned)(a.ordinal + ti) * 0x3C6EF373u + (unsigned)((uint64_t)at >> 32) * 0x243F6A89u;
+        const bool any_m = !lost_m && top_m > 1e-30f, any_v = !lost_v && top_v > 1e-30f;
+        const float up_m = any_m ? kTop8 / top_m : 0.f, up_v = any_v ? kTop8 / top_v : 0.f;
+        const float old_m = m_scale, old_v = v_scale;
+        m_scale = lost_m ? __builtin_nanf("") : any_m ? top_m / kTop8 : 0.f;
+        v_scale = lost_v ? __builtin_nanf("") : any_v ? top_v / kTop8 : 0.f;
+        const unsigned base = key + (unsigned)ti * 0x3C6EF373u + (unsigned)((uint64_t)at >> 32) * 0x243F6A89u;
+        unsigned edge = ~0u;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const unsigned u = mix(((unsigned)at + j) ^ base);
-            const float am = lost_m ? 0.f : fminf(fabsf(m[j]) * up_m, kTop8), av = lost_v ? 0.f : fminf(root[j] * up_v, kTop8);
-            m[j] = copysignf(on_grid(am, u & 0xffffu), m[j]);
-            root[j] = on_grid(av, u >> 16);
-            if (av > 0.f) root[j] = fmaxf(root[j], 0x1p-9f);
+            const float am = fminf(fabsf(m[j]) * up_m, kTop8), av = fminf(root[j] * up_v, kTop8);
+            m[j] = copysignf(on_grid(am, u << 16 >> 12, edge), m[j]);
+            root[j] = fmaxf(on_grid(av, u >> 16 << 4, edge), av > 0.f ? 0x1p-9f : 0.f);
+        }
+        // Where a number lies so near to where the dither turns that fp32's roundings would decide (moments are off by a few halves
+        // of their last place, mostly), the wave, one in eighty, does it all again in 64 bits: results are those of the
+        // formula, not of an order of roundings.
+        if (__any(edge < 2 * kClose)) {
+            // (one element after the other, the first of arrays that turn: in a loop that is not unrolled, so that the usual way needs no
+            // registers for this one -- 119 with eight at once, at which a step of 64 million took 210 us instead of 165)
+            auto again = [&](double &xm, double &xv) {
+                const double x = (double)g[0] * gs, old = (double)__builtin_amdgcn_cvt_f32_fp8(v8[0], 0) * old_v;
+                xm = (double)__builtin_amdgcn_cvt_f32_fp8(m8[0], 0) * old_m * a.beta1 + x * (1.0 - a.beta1);
+                xv = old * old * a.beta2 + x * x * (1.0 - a.beta2);
+                turn(g);
+                turn_bytes(m8);
+                turn_bytes(v8);
+            };
+            double tm = 0.0, tv = 0.0, xm, xv;
+#pragma unroll 1
+            for (int j = 0; j < 8; ++j) {
+                again(xm, xv);
+                if (j < left) {
+                    tm = fmax(tm, fabs(xm));
+                    tv = fmax(tv, xv);
+                }
+            }
+            tm = over_block(tm) / (double)kTop8;
+            tv = sqrt(over_block(tv)) / (double)kTop8;
+            // (a block of zeros, or of what is not finite, stays as it is)
+#pragma unroll 1
+            for (int j = 0; j < 8; ++j) {
+                again(xm, xv);
+                const unsigned u = mix(((unsigned)at + j) ^ base);
+                if (any_m) m[0] = copysignf((float)on_grid(fmin(fabs(xm) / tm, (double)kTop8), u & 0xffffu), (float)xm);
+                if (any_v) {
+                    root[0] = (float)on_grid(fmin(sqrt(xv) / tv, (double)kTop8), u >> 16);
+                    if (xv > 0.0) root[0] = fmaxf(root[0], 0x1p-9f);
+                }
+                turn(m);
+                turn(root);
+            }
         }
         encode(m, m8);
         encode(root, v8);
+        if (!any_m) m8[0] = m8[1] = 0u;
+        if (!any_v) v8[0] = v8[1] = 0u;
     }
     if (left > 0) {
         store_bytes(t.m_out, at, left, m8);
@@ -237,40 +373,85 @@ void launch(obc_ctx *ctx, const Args &a, unsigned blocks, bool bits8)
 
 }  // namespace
 
-extern "C" int obc_adamw(obc_ctx *ctx, const obc_adamw_tensor *tensors, int count, int type, int bits, int64_t step, const int64_t *step_at,
-                         float lr, const float *lr_at, double beta1, double beta2, float eps, const float *grad_scale, uint32_t seed)
+extern "C" {
+
+int obc_adamw_plan_bytes(int count, size_t *bytes)
+{
+    if (!bytes || count < 0) return OBC_ERR_BAD_ARG;
+    *bytes = layout_of(count).bytes;
+    return OBC_OK;
+}
+
+int obc_adamw_plan(obc_ctx *ctx, const obc_adamw_tensor *tensors, int count, int type, int bits, void *plan, int64_t *workgroups)
 {
     if (!ctx) return OBC_ERR_BAD_ARG;
-    if (count < 0 || (count > 0 && !tensors)) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw: no tensors");
-    if (!float_type(type) || (bits != 8 && bits != 32)) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw: type %d, moments of %d bits", type, bits);
-    if (!(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0)) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw: betas are in [0, 1)");
-    if (!(eps > 0.f && eps < __builtin_inff())) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw: eps is not positive and finite");
-    if (!step_at && step < 1) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw: steps count from 1");
-    if (!lr_at && !(fabsf(lr) < __builtin_inff())) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw: lr is not finite");
-    if ((((uintptr_t)step_at) & 7) != 0 || (((uintptr_t)lr_at | (uintptr_t)grad_scale) & 3) != 0)
-        return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw: step_at, lr_at or grad_scale is not aligned");
+    if (count < 0 || !workgroups || (count > 0 && (!tensors || !plan))) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw_plan: null argument");
+    if (!float_type(type) || (bits != 8 && bits != 32)) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw_plan: type %d, moments of %d bits", type, bits);
+    if (((uintptr_t)plan & 15) != 0) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw_plan: the plan is not aligned to 16 bytes");
     const size_t e = size_of_type(type) - 1;
+    int64_t blocks = 0;
     for (int i = 0; i < count; ++i) {
         const obc_adamw_tensor &t = tensors[i];
-        if (t.n < 0 || t.n > (int64_t)1 << 40) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw: tensor %d: bad size", i);
-        if (!(fabsf(t.decay) < __builtin_inff())) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw: tensor %d: decay is not finite", i);
+        if (t.n < 0) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw_plan: tensor %d: bad size", i);
+        if (!(fabsf(t.decay) < __builtin_inff())) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw_plan: tensor %d: decay is not finite", i);
         if (t.n == 0) continue;
         if (!t.p || !t.p_out || !t.g || !t.m || !t.m_out || !t.v || !t.v_out || (t.master == nullptr) != (t.master_out == nullptr))
-            return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw: tensor %d: null argument", i);
+            return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw_plan: tensor %d: null argument", i);
         if (bits == 8 && (!t.m_scale || !t.m_scale_out || !t.v_scale || !t.v_scale_out))
-            return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw: tensor %d: moments of 8 bits have scales", i);
+            return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw_plan: tensor %d: moments of 8 bits have scales", i);
         const uintptr_t words = (uintptr_t)t.master | (uintptr_t)t.master_out |
                                 (bits == 8 ? (uintptr_t)t.m_scale | (uintptr_t)t.m_scale_out | (uintptr_t)t.v_scale | (uintptr_t)t.v_scale_out
                                            : (uintptr_t)t.m | (uintptr_t)t.m_out | (uintptr_t)t.v | (uintptr_t)t.v_out);
         if (((((uintptr_t)t.p | (uintptr_t)t.p_out | (uintptr_t)t.g) & e) | (words & 3)) != 0)
-            return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw: tensor %d: an array is not aligned to its elements", i);
+            return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw_plan: tensor %d: an array is not aligned to its elements", i);
+        const int64_t more = t.n / kChunk + (t.n % kChunk != 0);
+        if (more > kMostBlocks - blocks) return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_adamw_plan: more elements than a launch takes");
+        blocks += more;
     }
+    *workgroups = blocks;
+    unsigned first = 0;
+    for (int i = 0; i < count; i += kWritten) {
+        PlanArgs a;
+        a.tensors = count - i < kWritten ? count - i : kWritten;
+        a.to = (obc_adamw_tensor *)plan + i;
+        a.first_to = (unsigned *)((char *)plan + layout_of(count).first) + i;
+        for (int j = 0; j < a.tensors; ++j) {
+            a.t[j] = tensors[i + j];
+            a.first[j] = first;
+            first += (unsigned)(a.t[j].n / kChunk + (a.t[j].n % kChunk != 0));
+        }
+        adamw_plan_kernel<<<1, 64, 0, ctx->stream>>>(a);
+        OBC_LAUNCH_CHECK(ctx, "adamw_plan_kernel");
+    }
+    return OBC_OK;
+}
+
+int obc_adamw(obc_ctx *ctx, const void *plan, int count, int64_t workgroups, int type, int bits, int64_t step, const int64_t *step_at, float lr,
+              const float *lr_at, double beta1, double beta2, float eps, const float *grad_scale, uint32_t seed)
+{
+    if (!ctx) return OBC_ERR_BAD_ARG;
+    if (count < 0 || workgroups < 0 || workgroups > kMostBlocks || (workgroups > 0 && count == 0))
+        return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw: not a plan's numbers");
+    if (!float_type(type) || (bits != 8 && bits != 32)) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw: type %d, moments of %d bits", type, bits);
+    if (!(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0)) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw: betas are in [0, 1)");
+    if (!(eps >= 0x1p-120f && eps < __builtin_inff())) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw: eps is not in [2^-120, inf)");
+    if (!step_at && step < 1) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw: steps count from 1");
+    if (!lr_at && !(fabsf(lr) < __builtin_inff())) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw: lr is not finite");
+    if ((((uintptr_t)step_at) & 7) != 0 || (((uintptr_t)lr_at | (uintptr_t)grad_scale) & 3) != 0)
+        return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw: step_at, lr_at or grad_scale is not aligned");
+    if (workgroups == 0) return OBC_OK;
+    if (!plan || ((uintptr_t)plan & 15) != 0) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw: no plan");
     Args a;
+    a.t = (const obc_adamw_tensor *)plan;
+    a.first = (const unsigned *)((const char *)plan + layout_of(count).first);
+    a.tensors = count;
     a.step = step_at;
     a.lr_at = lr_at;
     a.grad_scale = grad_scale;
     a.beta1 = beta1;
     a.beta2 = beta2;
+    a.root_b2 = sqrt(beta2);
+    a.root_n2 = sqrt(1.0 - beta2);
     a.lr = lr;
     a.eps = eps;
     a.c1 = a.c2 = 1.f;
@@ -281,25 +462,11 @@ extern "C" int obc_adamw(obc_ctx *ctx, const obc_adamw_tensor *tensors, int coun
         a.c2 = (float)(1.0 / sqrt(-expm1((double)step * log(beta2))));
         a.key += (unsigned)step * 0xBB67AE85u;
     }
-    constexpr int64_t kMostBlocks = 1 << 23;      // of a launch: below 2^32 threads
-    int i = 0;
-    while (i < count) {
-        a.tensors = 0;
-        a.ordinal = i;
-        int64_t blocks = 0;
-        for (; i < count && a.tensors < kTensors; ++i) {
-            const int64_t more = (tensors[i].n + kChunk - 1) / kChunk;
-            if (a.tensors > 0 && blocks + more > kMostBlocks) break;
-            if (more > kMostBlocks) return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_adamw: tensor %d: more than 2^34 - 1 elements", i);
-            a.first[a.tensors] = (unsigned)blocks;
-            a.t[a.tensors++] = tensors[i];
-            blocks += more;
-        }
-        if (blocks == 0) continue;
-        if (type == OBC_F32) launch<OBC_F32>(ctx, a, (unsigned)blocks, bits == 8);
-        else if (type == OBC_F16) launch<OBC_F16>(ctx, a, (unsigned)blocks, bits == 8);
-        else launch<OBC_BF16>(ctx, a, (unsigned)blocks, bits == 8);
-        OBC_LAUNCH_CHECK(ctx, "adamw_kernel");
-    }
+    if (type == OBC_F32) launch<OBC_F32>(ctx, a, (unsigned)workgroups, bits == 8);
+    else if (type == OBC_F16) launch<OBC_F16>(ctx, a, (unsigned)workgroups, bits == 8);
+    else launch<OBC_BF16>(ctx, a, (unsigned)workgroups, bits == 8);
+    OBC_LAUNCH_CHECK(ctx, "adamw_kernel");
     return OBC_OK;
 }
+
+}  // extern "C"
