@@ -7,6 +7,8 @@
 // logits reach and few more do; those that do go to LDS as whole numbers (logit, then index) and are sorted there.  Where too many
 // reach it (equal logits, mostly), the k-th largest is found exactly, by bisection, and equal ones are taken in their order.  Rows
 // of several parts are joined by a second kernel.
+#include <type_traits>
+
 #include "row_io.h"
 
 namespace {
@@ -14,7 +16,6 @@ namespace {
 typedef unsigned long long Key;      // a logit's order above its index's opposite; 0: none
 
 constexpr int kMaxTop = 1024, kMaxCols = 1 << 30;
-constexpr int kCap = 2048;      // candidates in LDS
 constexpr int NT = 256, WAVES = NT / 64;
 constexpr float kLn2 = 0.693147180559945f;
 
@@ -52,6 +53,14 @@ struct Order {
     static __device__ float bound(unsigned o) { return unordered(o << SHIFT); }
 };
 
+// A piece's element.  (Not Piece's own access: with that the half-precision pieces would live in memory.)
+template <int TYPE>
+__device__ inline float element(const Piece<TYPE> &p, int j)
+{
+    if (TYPE == OBC_F16) return (float)half_pair(p.v[j >> 1])[j & 1];
+    return p[j];
+}
+
 template <int N>
 __device__ inline void block_sums(float (&v)[N], float (*buf)[N])
 {
@@ -86,7 +95,7 @@ __device__ inline int block_count(int n, int *buf)
 
 __device__ inline Key key_of(float z, int index) { return (Key)ordered(z + 0.f) << 32 | ~(unsigned)index; }
 
-// keys[0 .. n) in LDS, n <= kCap, largest first; all threads of the workgroup.  `out` gets the first k.
+// keys[0 .. n) in LDS, with room for the next power of two, largest first; all threads of the workgroup.  `out` gets the first k.
 template <typename OUT>
 __device__ inline void sort_keys(Key *keys, int n, int k, OUT out)
 {
@@ -94,11 +103,13 @@ __device__ inline void sort_keys(Key *keys, int n, int k, OUT out)
     if (n <= NT) {
         const Key own = tid < n ? keys[tid] : 0;
         int rank = 0;
-        for (int j = 0; j < n; ++j) rank += keys[j] > own;
+        if (tid - (tid & 63) < n)
+#pragma unroll 8
+            for (int j = 0; j < n; ++j) rank += keys[j] > own;
         if (tid < n && rank < k) out(rank, own);
         return;
     }
-    int size = 512;
+    int size = 2 * NT;
     while (size < n) size *= 2;
     for (int i = n + tid; i < size; i += NT) keys[i] = 0;
     __syncthreads();
@@ -138,14 +149,26 @@ __device__ inline int target_of(const Args &a, int64_t row)
     return t;
 }
 
-template <int TYPE, int CH>
-__global__ __launch_bounds__(NT, 4) void score_kernel(Args a)
+// The larger halves of two dwords.  bf16 numbers lie in the order of the half-precision ones of the same bits, up to 2^121; beyond
+// (infinities too) those are NaNs, which this drops.
+__device__ inline unsigned larger_halves(unsigned a, unsigned b)
+{
+    unsigned r;
+    asm("v_pk_max_f16 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+
+// PIECES: room for 16-byte pieces that hold a candidate, KEYS: for candidates (0 both: none are asked for)
+template <int TYPE, int CH, int PIECES, int KEYS>
+__global__ __launch_bounds__(NT, PIECES > 512 ? 3 : 4) void score_kernel(Args a)
 {
     constexpr int E = Piece<TYPE>::E;
     typedef Order<TYPE> O;
-    __shared__ float buf1[WAVES], buf2[WAVES][2], buf3[WAVES];
-    __shared__ int buf4[WAVES], found;
-    __shared__ Key keys[kCap];
+    __shared__ float buf1[WAVES], buf2[2][WAVES][2], buf3[WAVES];
+    __shared__ int buf4[WAVES], found, queued;
+    __shared__ __align__(16) uintx4 queue[PIECES + 1];
+    __shared__ int queue_at[PIECES + 1];
+    __shared__ Key keys[KEYS + 1];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t row = blockIdx.x / a.parts;
     const int part = (int)(blockIdx.x - row * a.parts), from = part * a.len, n = max(0, min(a.len, a.V - from));
@@ -153,26 +176,33 @@ __global__ __launch_bounds__(NT, 4) void score_kernel(Args a)
     const float c2 = 1.44269504088896f / a.tau;
     // pieces 0 .. whole - 1 are whole in every thread; the part ends inside the next one, x[CH] wherever that is
     const int whole = n / (NT * E);
+    const bool tail = n > whole * NT * E;
     Piece<TYPE> x[CH + 1];
 #pragma unroll
     for (int i = 0; i < CH; ++i)
         if (i < whole) x[i].load(z, (i * NT + tid) * E);
-    x[CH].load_end(z, (whole * NT + tid) * E, n);
+    if (tail) x[CH].load_end(z, (whole * NT + tid) * E, n);
     int target = -1;
     float zt = 0.f;
     if (a.parts == 1 && tid == 0) {
         target = target_of(a, row);
         if (target >= 0) zt = load_as<TYPE>(a.z, row * a.ldz + target);
     }
-    if (tid == 0) found = 0;
-    // the largest of each piece and of them all
-    float most[CH + 1], own = -__builtin_inff();
+    if (tid == 0) found = queued = 0;
+    float most[CH + 1], s[2], top, bound;      // the largest of each piece
+    float own = -__builtin_inff();
 #pragma unroll
     for (int i = 0; i <= CH; ++i) {
         most[i] = -__builtin_inff();
-        if (i < whole || i == CH) {
+        if (i < CH ? i < whole : tail) {
+            if (TYPE != OBC_F32) {
+                const uintx4 w = x[i].v;
+                const unsigned m = larger_halves(larger_halves(w[0], w[1]), larger_halves(w[2], w[3]));
+                most[i] = TYPE == OBC_F16 ? fmaxf(half_lo(m), half_hi(m)) : fmaxf(bf16_lo(m), bf16_hi(m));
+            } else {
 #pragma unroll
-            for (int j = 0; j < E; ++j) most[i] = fmaxf(most[i], x[i][j]);
+                for (int j = 0; j < E; ++j) most[i] = fmaxf(most[i], element(x[i], j));
+            }
             own = fmaxf(own, most[i]);
         }
     }
@@ -180,20 +210,20 @@ __global__ __launch_bounds__(NT, 4) void score_kernel(Args a)
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) wave_top = fmaxf(wave_top, __shfl_xor(wave_top, off, 64));
     // what at least r of this wave's lanes (or of their pieces) reach, and not many more
-    float bound = -__builtin_inff();
-    if (a.k > 0) {
-        const int r = (a.k + WAVES - 1) / WAVES;
+    bound = -__builtin_inff();
+    if (KEYS > 0) {
+        // waves with something in every lane; the others' candidates come on top
+        const int live = min(WAVES, n / (64 * E)), r = live > 0 ? (a.k + live - 1) / live : 1 << 20;
         auto count = [&](float b) {
             if (r <= 32) return (int)__popcll(__ballot(own >= b));
             int c = 0;
 #pragma unroll
             for (int i = 0; i <= CH; ++i)
-                if (i < whole || i == CH) c += __popcll(__ballot(most[i] >= b));
+                if (i < CH ? i < whole : tail) c += __popcll(__ballot(most[i] >= b));
             return c;
         };
-        unsigned lo = O::of(-__builtin_inff()), hi = __builtin_amdgcn_readfirstlane(O::of(wave_top));
-        if (wave_top < __builtin_inff() && count(O::bound(lo + 1)) >= r) {
-            ++lo;
+        unsigned lo = O::of(-__builtin_inff()) + 1, hi = __builtin_amdgcn_readfirstlane(O::of(wave_top));
+        if (wave_top < __builtin_inff() && count(O::bound(lo)) >= r) {
             while (lo < hi) {
                 const unsigned mid = lo + (hi - lo + 1) / 2;
                 const int c = count(O::bound(mid));
@@ -203,141 +233,203 @@ __global__ __launch_bounds__(NT, 4) void score_kernel(Args a)
             }
             bound = O::bound(lo);
         }
+        if (live > 0 && wave >= live) bound = __builtin_inff();
     }
     if (lane == 0) {
         buf1[wave] = wave_top;
         buf3[wave] = bound;
     }
     __syncthreads();
-    float top = buf1[0];
+    top = buf1[0];
     bound = buf3[0];
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) {
         top = fmaxf(top, buf1[w]);
         bound = fminf(bound, buf3[w]);
     }
-    const float base = top == -__builtin_inff() ? 0.f : top;
-    float s[2] = {0.f, 0.f};
+    float base = top == -__builtin_inff() ? 0.f : top;
+    const float off = base * c2;
+    s[0] = s[1] = 0.f;
 #pragma unroll
     for (int i = 0; i <= CH; ++i)
-        if (i < whole || i == CH) {
+        if (i < CH ? i < whole : tail) {
             x[i].forget();
 #pragma unroll
             for (int j = 0; j < E; ++j) {
-                const float d = (x[i][j] - base) * c2, e = __builtin_amdgcn_exp2f(d);
+                const float d = fmaf(element(x[i], j), c2, -off), e = __builtin_amdgcn_exp2f(d);
                 s[0] += e;
                 s[1] = fmaf(e, fmaxf(d, -1e30f), s[1]);      // (a logit of -inf adds nothing)
             }
         }
-    block_sums<2>(s, buf2);
+    block_sums<2>(s, buf2[0]);
+    {
+        // the product base c2 was rounded: all exponents are off by this, and the sums are brought back
+        const float r = fmaf(base, c2, -off), f = __builtin_amdgcn_exp2f(-r);
+        s[1] = fmaf(-r, s[0], s[1]) * f;
+        s[0] *= f;
+    }
+    // Numbers that these short ways do not know (NaN, infinities, and beyond 2^100; bf16: nothing but -inf and what is near the type's
+    // lowest to reach the bound): once more, from the caches, for here and below.  Loops over the registers would take some from the
+    // usual way.
+    const int pieces = (n + NT * E - 1) / (NT * E);
+    auto all = [&](auto f) {
+#pragma unroll 4
+        for (int i = 0; i < pieces; ++i) {
+            Piece<TYPE> p;
+            p.load_end(z, (i * NT + tid) * E, n);
+            f(p, from + (i * NT + tid) * E);
+        }
+    };
+    const bool known = s[0] < __builtin_inff() && fabsf(off) < 0x1p100f && (TYPE != OBC_BF16 || (fabsf(base) < 0x1p120f && (KEYS == 0 || bound > -0x1p120f)));
+    if (!known) {
+        own = -__builtin_inff();
+        all([&](const Piece<TYPE> &p, int) {
+#pragma unroll
+            for (int j = 0; j < E; ++j) own = fmaxf(own, element(p, j));
+        });
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) own = fmaxf(own, __shfl_xor(own, off, 64));
+        if (lane == 0) buf1[wave] = own;
+        __syncthreads();
+        top = buf1[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) top = fmaxf(top, buf1[w]);
+        base = top == -__builtin_inff() ? 0.f : top;
+        s[0] = s[1] = 0.f;
+        all([&](const Piece<TYPE> &p, int) {
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                const float d = (element(p, j) - base) * c2, e = __builtin_amdgcn_exp2f(d);
+                s[0] += e;
+                s[1] = fmaf(e, fmaxf(d, -1e30f), s[1]);
+            }
+        });
+        block_sums<2>(s, buf2[1]);
+    }
     if (tid == 0) {
         if (a.parts == 1) finish(a, row, base, s[0], s[1], zt, target);
         else a.stats[blockIdx.x] = Stats{base, s[0], s[1], 0.f};
     }
-    if (a.k == 0) return;
+    if (KEYS == 0) return;
 
-    // the logits that reach `b` go to LDS, as far as there is room; the bound's are above -inf
-    auto each = [&](int i, float b, auto f) {
-        if (most[i] >= b) {
-            const int c = from + ((i == CH ? whole : i) * NT + tid) * E;
-#pragma unroll
-            for (int j = 0; j < E; ++j)
-                if (x[i][j] >= b) f(x[i][j], c + j);
-        }
-    };
+    // The logits that reach `b`, which is above -inf, go to LDS, as far as there is room: first the pieces that hold one, of which a
+    // thread has few, then, piece by piece, they themselves.  Returns whether there was room.
     auto collect = [&](float b) {
-        int mine = 0;
+        auto slots = [&](int *counter, int many) {      // the first of `many`, for the wave
+            int first = 0;
+            if (lane == 0) first = atomicAdd(counter, many);
+            return __builtin_amdgcn_readfirstlane(first);
+        };
+        auto rank = [](unsigned long long m) { return (int)__builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0u)); };
+        int many = 0;
 #pragma unroll
         for (int i = 0; i <= CH; ++i)
-            if (i < whole || i == CH) {
-                x[i].forget();
-                each(i, b, [&](float, int) { ++mine; });
-            }
-        int at = mine;
+            if (i < CH ? i < whole : tail) many += __popcll(__ballot(most[i] >= b));
+        int at = slots(&queued, many);
 #pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const int o = __shfl_up(at, off, 64);
-            if (lane >= off) at += o;
-        }
-        int first = 0;
-        if (lane == 63) first = atomicAdd(&found, at);
-        at += __shfl(first, 63, 64) - mine;
-        if (mine > 0)
-#pragma unroll
-            for (int i = 0; i <= CH; ++i)
-                if (i < whole || i == CH) {
-                    x[i].forget();
-                    each(i, b, [&](float v, int c) {
-                        if (at < kCap) keys[at] = key_of(v, c);
-                        ++at;
-                    });
+        for (int i = 0; i <= CH; ++i)
+            if (i < CH ? i < whole : tail) {
+                const unsigned long long m = __ballot(most[i] >= b);
+                if (m == 0) continue;
+                const int to = at + rank(m);
+                if (most[i] >= b && to < PIECES) {
+                    queue[to] = x[i].v;
+                    queue_at[to] = from + ((i == CH ? whole : i) * NT + tid) * E;
                 }
+                at += __popcll(m);
+            }
+        __syncthreads();
+        const int pieces = min(queued, PIECES);
+        for (int q0 = wave * 64; q0 < pieces; q0 += NT) {
+            const int q = min(q0 + lane, pieces - 1);
+            Piece<TYPE> p;
+            p.v = queue[q];
+            const int c = queue_at[q];
+            const float least = q0 + lane < pieces ? b : __builtin_inff();      // (+inf is no candidate either: its row is lost)
+            many = 0;
+#pragma unroll
+            for (int j = 0; j < E; ++j) many += __popcll(__ballot(element(p, j) >= least));
+            at = slots(&found, many);
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                const unsigned long long m = __ballot(element(p, j) >= least);
+                const int to = at + rank(m);
+                if (element(p, j) >= least && to < KEYS) keys[to] = key_of(element(p, j), c + j);
+                at += __popcll(m);
+            }
+        }
+        __syncthreads();
+        return queued <= PIECES && found <= KEYS;
     };
     const float least = O::bound(O::of(-__builtin_inff()) + 1);      // above -inf
-    collect(fmaxf(bound, least));
-    __syncthreads();
+    const bool room = known && collect(fmaxf(bound, least));
     int have = found;
     __syncthreads();      // (found is set again below)
-    if (have > kCap) {
+    if (!room) {
         // Exactly: the largest bound that k logits reach, those above it, and of those on it the first
         auto count = [&](float b) {
             int c = 0;
+            all([&](const Piece<TYPE> &p, int) {
 #pragma unroll
-            for (int i = 0; i <= CH; ++i)
-                if (i < whole || i == CH) {
-                    x[i].forget();
-#pragma unroll
-                    for (int j = 0; j < E; ++j) c += x[i][j] >= b;
-                }
+                for (int j = 0; j < E; ++j) c += element(p, j) >= b;
+            });
             return block_count(c, buf4);
         };
-        unsigned lo = __builtin_amdgcn_readfirstlane(O::of(fmaxf(bound, least))), hi = __builtin_amdgcn_readfirstlane(O::of(top));
-        while (lo < hi) {
+        unsigned lo = __builtin_amdgcn_readfirstlane(O::of(known ? fmaxf(bound, least) : least)), hi = __builtin_amdgcn_readfirstlane(O::of(top));
+        const unsigned highest = hi;
+        const int finite = count(least);
+        int need = min(a.k, finite);
+        while (lo < hi && finite > need) {
             const unsigned mid = lo + (hi - lo + 1) / 2;
-            if (count(O::bound(mid)) >= a.k) lo = mid;
+            if (count(O::bound(mid)) >= need) lo = mid;
             else hi = mid - 1;
         }
-        const float at_least = O::bound(lo), above = O::bound(lo + 1);
-        int need = a.k;
-        if (lo < O::of(top)) need -= count(above);
+        const float at_least = O::bound(lo), above = lo < highest ? O::bound(lo + 1) : __builtin_inff();
         if (tid == 0) found = 0;
         __syncthreads();
-        if (lo < O::of(top)) collect(above);
+        all([&](const Piece<TYPE> &p, int c) {
+#pragma unroll
+            for (int j = 0; j < E; ++j)
+                if (element(p, j) >= above && element(p, j) < __builtin_inff()) {      // (fewer than k)
+                    const int to = atomicAdd(&found, 1);
+                    if (to < KEYS) keys[to] = key_of(element(p, j), c + j);
+                }
+        });
         __syncthreads();
-        int filled = found;
+        int filled = min(found, need);
+        need -= filled;
+        for (int i = 0; i < pieces && need > 0; ++i) {
+            Piece<TYPE> p;
+            p.load_end(z, (i * NT + tid) * E, n);
+            auto on = [&](float v) { return v >= at_least && !(v >= above); };
+            int mine = 0;
 #pragma unroll
-        for (int i = 0; i <= CH; ++i)
-            if ((i < whole || i == CH) && need > 0) {
-                auto on = [&](float v) { return v >= at_least && !(lo < O::of(top) && v >= above); };
-                int mine = 0;
+            for (int j = 0; j < E; ++j) mine += on(element(p, j));
+            int at = mine;
 #pragma unroll
-                for (int j = 0; j < E; ++j) mine += on(x[i][j]);
-                int at = mine;
-#pragma unroll
-                for (int off = 1; off < 64; off <<= 1) {
-                    const int o = __shfl_up(at, off, 64);
-                    if (lane >= off) at += o;
-                }
-                __syncthreads();
-                if (lane == 63) buf4[wave] = at;
-                __syncthreads();
-                at -= mine;
-                int all = 0;
-#pragma unroll
-                for (int w = 0; w < WAVES; ++w) {
-                    at += w < wave ? buf4[w] : 0;
-                    all += buf4[w];
-                }
-                const int c = from + ((i == CH ? whole : i) * NT + tid) * E;
-#pragma unroll
-                for (int j = 0; j < E; ++j)
-                    if (on(x[i][j])) {
-                        if (at < need) keys[filled + at] = key_of(x[i][j], c + j);
-                        ++at;
-                    }
-                filled += min(all, need);
-                need -= min(all, need);
+            for (int off = 1; off < 64; off <<= 1) {
+                const int o = __shfl_up(at, off, 64);
+                if (lane >= off) at += o;
             }
+            __syncthreads();
+            if (lane == 63) buf4[wave] = at;
+            __syncthreads();
+            at -= mine;
+            int these = 0;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                at += w < wave ? buf4[w] : 0;
+                these += buf4[w];
+            }
+#pragma unroll
+            for (int j = 0; j < E; ++j)
+                if (on(element(p, j))) {
+                    if (at < need) keys[filled + at] = key_of(element(p, j), from + (i * NT + tid) * E + j);
+                    ++at;
+                }
+            filled += min(these, need);
+            need -= min(these, need);
+        }
         __syncthreads();
         have = filled;
     }
@@ -358,74 +450,106 @@ __global__ __launch_bounds__(NT, 4) void score_kernel(Args a)
     }
 }
 
-// Rows of several parts: sums brought to the largest maximum; an entry's place is its own in its list and the number of larger ones
-// in each of the others.
-template <int TYPE, bool LDS>
+// Rows of several parts: sums brought to the largest maximum, lists joined.  At least k entries of all lists reach the least of the
+// lists' entries k / parts (counted from 1, rounded up), and also the largest of their k-th ones: what reaches both is sorted.
+template <int TYPE>
 __global__ __launch_bounds__(NT) void score_join_kernel(Args a)
 {
-    extern __shared__ Key held[];
-    const int tid = threadIdx.x;
+    constexpr int KEYS = 2048;
+    __shared__ Key keys[KEYS];
+    __shared__ Key limits[WAVES][2];
+    __shared__ int found;
+    const int tid = threadIdx.x, lane = tid & 63;
     const int64_t row = blockIdx.x;
     const Stats *const st = a.stats + row * a.parts;
     const Key *const lists = a.lists + row * a.parts * a.k;
     const int n = a.parts * a.k;
-    if (LDS)
-        for (int i = tid; i < n; i += NT) held[i] = lists[i];
-    const Key *const from = LDS ? held : lists;
     int target = -1;
     float zt = 0.f;
     if (tid == 0) {
+        found = 0;
         target = target_of(a, row);
         if (target >= 0) zt = load_as<TYPE>(a.z, row * a.ldz + target);
     }
     const float c2 = 1.44269504088896f / a.tau;
+    // every wave for itself, a part to a lane
+    Key low = ~(Key)0, high = 0;
     float top = -__builtin_inff(), sum = 0.f, dot = 0.f;
-    for (int p = 0; p < a.parts; ++p) top = st[p].sum == 0.f ? top : fmaxf(top, st[p].top);
+    const int share = a.k > 0 ? (a.k + a.parts - 1) / a.parts : 0;
+    for (int p = lane; p < a.parts; p += 64) {
+        top = st[p].sum == 0.f ? top : fmaxf(top, st[p].top);
+        if (a.k > 0) {
+            const Key l = lists[p * a.k + share - 1], h = lists[p * a.k + a.k - 1];
+            low = l < low ? l : low;
+            high = h > high ? h : high;
+        }
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) {
+        top = fmaxf(top, __shfl_xor(top, off, 64));
+        const Key l = __shfl_xor(low, off, 64), h = __shfl_xor(high, off, 64);
+        low = l < low ? l : low;
+        high = h > high ? h : high;
+    }
     if (top == -__builtin_inff()) top = 0.f;
-    for (int p = 0; p < a.parts; ++p) {
+    for (int p = lane; p < a.parts; p += 64) {
         const Stats s = st[p];
         if (s.sum == 0.f) continue;
         const float d = (s.top - top) * c2, w = __builtin_amdgcn_exp2f(d);
         sum = fmaf(s.sum, w, sum);
         dot = fmaf(fmaf(s.sum, fmaxf(d, -1e30f), s.dot), w, dot);
     }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) {
+        sum += __shfl_xor(sum, off, 64);
+        dot += __shfl_xor(dot, off, 64);
+    }
     if (tid == 0) finish(a, row, top, sum, dot, zt, target);
     if (a.k == 0) return;
     const bool lost = !(sum == sum);
+    auto put = [&](int i, Key key) {
+        a.top_index[row * a.k + i] = lost ? -1 : (int)~(unsigned)key;
+        a.top_logit[row * a.k + i] = lost ? __builtin_nanf("") : unordered((unsigned)(key >> 32));
+    };
+    Key bound = low > high ? low : high;
+    if (bound == 0) bound = 1;      // (0: no entry)
     __syncthreads();
-    int entries = 0;
-    for (int p = 0; p < a.parts; ++p) {
-        // the entries of a list end where the first 0 is
-        const Key *const l = from + p * a.k;
-        int lo = 0, hi = a.k;
-        while (lo < hi) {
-            const int mid = (lo + hi) / 2;
-            if (l[mid] != 0) lo = mid + 1;
-            else hi = mid;
-        }
-        entries = min(entries + lo, a.k);
+    for (int e0 = 0; e0 < n; e0 += NT) {
+        const Key key = e0 + tid < n ? lists[e0 + tid] : 0;
+        const unsigned long long m = __ballot(key >= bound);
+        if (m == 0) continue;
+        int at = 0;
+        if (lane == 0) at = atomicAdd(&found, __popcll(m));
+        at = __builtin_amdgcn_readfirstlane(at) + __builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0u));
+        if (key >= bound && at < KEYS) keys[at] = key;
     }
-    for (int e = tid; e < n; e += NT) {
-        const Key key = from[e];
-        if (key == 0) continue;
-        const int own = e / a.k;
-        int rank = e - own * a.k;
-        for (int p = 0; p < a.parts && rank < a.k; ++p) {
-            if (p == own) continue;
-            const Key *const l = from + p * a.k;
-            int lo = 0, hi = a.k;
-            while (lo < hi) {
-                const int mid = (lo + hi) / 2;
-                if (l[mid] > key) lo = mid + 1;
-                else hi = mid;
+    __syncthreads();
+    int have = found;
+    if (have <= KEYS) {
+        sort_keys(keys, have, a.k, put);
+    } else {
+        // too many: an entry's place is its own in its list and the number of larger ones in each of the others
+        have = a.k;
+        for (int e = tid; e < n; e += NT) {
+            const Key key = lists[e];
+            if (key == 0) continue;
+            const int own = e / a.k;
+            int rank = e - own * a.k;
+            for (int p = 0; p < a.parts && rank < a.k; ++p) {
+                if (p == own) continue;
+                const Key *const l = lists + p * a.k;
+                int lo = 0, hi = a.k;
+                while (lo < hi) {
+                    const int mid = (lo + hi) / 2;
+                    if (l[mid] > key) lo = mid + 1;
+                    else hi = mid;
+                }
+                rank += lo;
             }
-            rank += lo;
+            if (rank < a.k) put(rank, key);
         }
-        if (rank >= a.k) continue;
-        a.top_index[row * a.k + rank] = lost ? -1 : (int)~(unsigned)key;
-        a.top_logit[row * a.k + rank] = lost ? __builtin_nanf("") : unordered((unsigned)(key >> 32));
     }
-    for (int i = entries + tid; i < a.k; i += NT) {
+    for (int i = have + tid; i < a.k; i += NT) {
         a.top_index[row * a.k + i] = -1;
         a.top_logit[row * a.k + i] = lost ? __builtin_nanf("") : -__builtin_inff();
     }
@@ -458,12 +582,15 @@ template <int TYPE>
 void launch(obc_ctx *ctx, const Args &a, int pieces)
 {
     const unsigned blocks = (unsigned)((int64_t)a.T * a.parts);
-    if (pieces == 16) score_kernel<TYPE, 16><<<blocks, NT, 0, ctx->stream>>>(a);
-    else score_kernel<TYPE, 4><<<blocks, NT, 0, ctx->stream>>>(a);
+    auto go = [&](auto ch) {
+        if (a.k == 0) score_kernel<TYPE, ch, 0, 0><<<blocks, NT, 0, ctx->stream>>>(a);
+        else if (a.k <= 256) score_kernel<TYPE, ch, 512, 1024><<<blocks, NT, 0, ctx->stream>>>(a);
+        else score_kernel<TYPE, ch, 1536, 2048><<<blocks, NT, 0, ctx->stream>>>(a);
+    };
+    if (pieces == 16) go(std::integral_constant<int, 16>());
+    else go(std::integral_constant<int, 4>());
     if (a.parts == 1) return;
-    const size_t held = (size_t)a.parts * a.k * sizeof(Key);
-    if (held <= 32768) score_join_kernel<TYPE, true><<<a.T, NT, held, ctx->stream>>>(a);
-    else score_join_kernel<TYPE, false><<<a.T, NT, 0, ctx->stream>>>(a);
+    score_join_kernel<TYPE><<<a.T, NT, 0, ctx->stream>>>(a);
 }
 
 }  // namespace
