@@ -297,6 +297,8 @@ class Context:
         if rc != OBC_OK:
             raise ObcError(rc, "obc_create failed")
         self.h = h
+        # (asked before every call, and these ask in a tenth of the time that torch.cuda's stream objects take)
+        self._raw, self._device = self.stream.cuda_stream, self.stream.device.index
         self._ws = None
         self._needs = {}
 
@@ -315,10 +317,13 @@ class Context:
         if rc != OBC_OK:
             raise ObcError(rc, self.lib.obc_last_error(self.h).decode())
 
+    def _is_current(self):
+        return torch._C._cuda_getCurrentRawStream(self._device) == self._raw
+
     def _capturing(self):
         """Whether the context's stream is being captured into a graph."""
-        if torch.cuda.current_stream(self.stream.device) == self.stream:
-            return torch.cuda.is_current_stream_capturing()
+        if self._is_current():
+            return torch._C._cuda_isCurrentStreamCapturing()
         with torch.cuda.stream(self.stream):
             return torch.cuda.is_current_stream_capturing()
 
@@ -563,7 +568,7 @@ class Context:
     def _empty(self, shape, dtype, device):
         """An output for kernels on the context's stream: allocated on that stream, which need not be the current
         one, so that the allocator does not hand out memory that the current stream still uses."""
-        if torch.cuda.current_stream(device) == self.stream:
+        if self._is_current():
             return torch.empty(shape, dtype=dtype, device=device)
         with torch.cuda.stream(self.stream):
             return torch.empty(shape, dtype=dtype, device=device)
@@ -748,22 +753,30 @@ class Context:
         k = int(top)
         if k < 0:
             raise ValueError("top must not be negative")
-        r = {}
-        for name, shape, dtype in (("logp", (T,), torch.float32), ("entropy", (T,), torch.float32), ("lse", (T,), torch.float32),
-                                   ("top_index", (T, k), torch.int32), ("top_logit", (T, k), torch.float32)):
-            r[name] = None
-            if (target is None and name == "logp") or (k == 0 and len(shape) == 2):
-                continue
-            r[name] = out.get(name)
-            if r[name] is None:
-                r[name] = self._empty(shape, dtype, z.device)
-            elif r[name].shape != shape:
-                raise ValueError("%s must have the shape %s" % (name, shape))
+        logp, entropy, lse = out.get("logp"), out.get("entropy"), out.get("lse")
+        index, logit = (out.get("top_index"), out.get("top_logit")) if k else (None, None)
+        if target is None:
+            logp = None
+        elif logp is None:
+            logp = self._empty((T,), torch.float32, z.device)
+        if entropy is None:
+            entropy = self._empty((T,), torch.float32, z.device)
+        if lse is None:
+            lse = self._empty((T,), torch.float32, z.device)
+        if k:
+            if index is None:
+                index = self._empty((T, k), torch.int32, z.device)
+            if logit is None:
+                logit = self._empty((T, k), torch.float32, z.device)
+            if index.shape != (T, k) or logit.shape != (T, k):
+                raise ValueError("top_index and top_logit must be %d x %d" % (T, k))
         ws, n, _held = self._need("obc_score_workspace_bytes", T, V, t, k)
-        self._ck(self.lib.obc_score(self.h, zp, t, T, V, ldz, _ints(target, T, "target"), float(temperature), k,
-                                    _vector(r["logp"], T, "logp"), _vector(r["entropy"], T, "entropy"), _vector(r["lse"], T, "lse"),
-                                    _ints(r["top_index"], T * k, "top_index"), _vector(r["top_logit"], T * k, "top_logit"), ws, n))
-        return r
+        rc = self.lib.obc_score(self.h, zp, t, T, V, ldz, _ints(target, T, "target"), float(temperature), k, _vector(logp, T, "logp"),
+                                _vector(entropy, T, "entropy"), _vector(lse, T, "lse"), _ints(index, T * k, "top_index"),
+                                _vector(logit, T * k, "top_logit"), ws, n)
+        if rc != OBC_OK:
+            self._ck(rc)
+        return dict(logp=logp, entropy=entropy, lse=lse, top_index=index, top_logit=logit)
 
     def obc_layernorm(self, x, gain, bias=None, eps=1e-5, residual=None, quant8=False, want_stats=False, out=None):
         """h = x + residual and its layer norm y.  out may hold h, y, scale (quant8), mean and rstd; without a residual, h is x

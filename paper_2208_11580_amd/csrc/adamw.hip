@@ -125,9 +125,7 @@ __device__ inline double over_block(double v)
 
 __device__ inline unsigned over_block(unsigned v)
 {
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) v = max(v, (unsigned)__shfl_xor((int)v, off, 64));
-    return v;
+    return join_lanes<32>(v, [](unsigned a, unsigned b) { return max(a, b); });
 }
 
 __device__ inline void load_bytes(const void *p, int64_t at, int left, unsigned (&w)[2])

@@ -14,9 +14,7 @@ template <int NT, int N>
 __device__ inline void sums(float (&v)[N], float (*buf)[N])
 {
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1)
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], off, 64);
+    for (int i = 0; i < N; ++i) v[i] = sum_lanes(v[i]);
     if (NT == 64) return;
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
@@ -34,8 +32,7 @@ __device__ inline void sums(float (&v)[N], float (*buf)[N])
 template <int NT>
 __device__ inline float largest(float v, float *buf)
 {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v = larger(v, __shfl_xor(v, off, 64));
+    v = join_lanes(v, larger);
     if (NT == 64) return v;
     if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
     __syncthreads();

@@ -165,3 +165,33 @@ struct Piece {
             if (c + j < V) store_as<TYPE>(p, c + j, g[j]);
     }
 };
+
+// A wave's lanes joined by an operation that is the same in either order; every lane gets the same result.  Steps between the lanes of
+// 16 and swaps of halves: a few cycles each, where a shuffle goes through LDS.
+template <int CONTROL>
+__device__ inline unsigned from_lane(unsigned v)
+{
+    return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CONTROL, 0xf, 0xf, true);
+}
+
+template <int LANES = 64, typename V, typename OP>
+__device__ inline V join_lanes(V v, OP op)
+{
+    static_assert(sizeof(V) == 4 && (LANES == 32 || LANES == 64), "");
+    const auto bits = [](V x) { return __builtin_bit_cast(unsigned, x); };
+    const auto value = [](unsigned x) { return __builtin_bit_cast(V, x); };
+    v = op(v, value(from_lane<0xb1>(bits(v))));       // lanes 1 0 3 2
+    v = op(v, value(from_lane<0x4e>(bits(v))));       // lanes 2 3 0 1
+    v = op(v, value(from_lane<0x141>(bits(v))));      // eight lanes turned round
+    v = op(v, value(from_lane<0x140>(bits(v))));      // sixteen lanes turned round
+    auto pair = __builtin_amdgcn_permlane16_swap(bits(v), bits(v), false, false);
+    v = op(value(pair[0]), value(pair[1]));
+    if (LANES == 32) return v;
+    pair = __builtin_amdgcn_permlane32_swap(bits(v), bits(v), false, false);
+    return op(value(pair[0]), value(pair[1]));
+}
+
+__device__ inline float sum_lanes(float v)
+{
+    return join_lanes(v, [](float a, float b) { return a + b; });
+}

@@ -16,7 +16,6 @@ namespace {
 typedef unsigned long long Key;      // a logit's order above its index's opposite; 0: none
 
 constexpr int kMaxTop = 1024, kMaxCols = 1 << 30;
-constexpr int NT = 256, WAVES = NT / 64;
 constexpr float kLn2 = 0.693147180559945f;
 
 struct Stats {
@@ -61,13 +60,14 @@ __device__ inline float element(const Piece<TYPE> &p, int j)
     return p[j];
 }
 
-template <int N>
+__device__ inline float fmaxf_of(float a, float b) { return fmaxf(a, b); }
+
+template <int NT, int N>
 __device__ inline void block_sums(float (&v)[N], float (*buf)[N])
 {
+    constexpr int WAVES = NT / 64;
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1)
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], off, 64);
+    for (int i = 0; i < N; ++i) v[i] = sum_lanes(v[i]);
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
         for (int i = 0; i < N; ++i) buf[threadIdx.x >> 6][i] = v[i];
@@ -80,10 +80,11 @@ __device__ inline void block_sums(float (&v)[N], float (*buf)[N])
     }
 }
 
+template <int NT>
 __device__ inline int block_count(int n, int *buf)
 {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off, 64);
+    constexpr int WAVES = NT / 64;
+    n = join_lanes(n, [](int a, int b) { return a + b; });
     __syncthreads();      // buf is read by all before it is written again
     if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = n;
     __syncthreads();
@@ -96,11 +97,11 @@ __device__ inline int block_count(int n, int *buf)
 __device__ inline Key key_of(float z, int index) { return (Key)ordered(z + 0.f) << 32 | ~(unsigned)index; }
 
 // keys[0 .. n) in LDS, with room for the next power of two, largest first; all threads of the workgroup.  `out` gets the first k.
-template <typename OUT>
+template <int NT, typename OUT>
 __device__ inline void sort_keys(Key *keys, int n, int k, OUT out)
 {
     const int tid = threadIdx.x;
-    if (n <= NT) {
+    if (n <= 256) {
         const Key own = tid < n ? keys[tid] : 0;
         int rank = 0;
         if (tid - (tid & 63) < n)
@@ -109,7 +110,7 @@ __device__ inline void sort_keys(Key *keys, int n, int k, OUT out)
         if (tid < n && rank < k) out(rank, own);
         return;
     }
-    int size = 2 * NT;
+    int size = 512;
     while (size < n) size *= 2;
     for (int i = n + tid; i < size; i += NT) keys[i] = 0;
     __syncthreads();
@@ -159,10 +160,10 @@ __device__ inline unsigned larger_halves(unsigned a, unsigned b)
 }
 
 // PIECES: room for 16-byte pieces that hold a candidate, KEYS: for candidates (0 both: none are asked for)
-template <int TYPE, int CH, int PIECES, int KEYS>
-__global__ __launch_bounds__(NT, PIECES > 512 ? 3 : 4) void score_kernel(Args a)
+template <int TYPE, int NT, int CH, int PIECES, int KEYS>
+__global__ __launch_bounds__(NT, NT == 1024 || PIECES <= 512 ? 4 : 3) void score_kernel(Args a)
 {
-    constexpr int E = Piece<TYPE>::E;
+    constexpr int E = Piece<TYPE>::E, WAVES = NT / 64;
     typedef Order<TYPE> O;
     __shared__ float buf1[WAVES], buf2[2][WAVES][2], buf3[WAVES];
     __shared__ int buf4[WAVES], found, queued;
@@ -206,9 +207,8 @@ __global__ __launch_bounds__(NT, PIECES > 512 ? 3 : 4) void score_kernel(Args a)
             own = fmaxf(own, most[i]);
         }
     }
-    float wave_top = own;
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) wave_top = fmaxf(wave_top, __shfl_xor(wave_top, off, 64));
+    // the largest and the least of the lanes' largest
+    const float wave_top = join_lanes(own, fmaxf_of), wave_low = KEYS > 0 ? join_lanes(own, [](float a, float b) { return fminf(a, b); }) : 0.f;
     // what at least r of this wave's lanes (or of their pieces) reach, and not many more
     bound = -__builtin_inff();
     if (KEYS > 0) {
@@ -223,9 +223,12 @@ __global__ __launch_bounds__(NT, PIECES > 512 ? 3 : 4) void score_kernel(Args a)
             return c;
         };
         unsigned lo = O::of(-__builtin_inff()) + 1, hi = __builtin_amdgcn_readfirstlane(O::of(wave_top));
+        if (r <= 64 && wave_low > -__builtin_inff()) lo = __builtin_amdgcn_readfirstlane(O::of(wave_low));
         if (wave_top < __builtin_inff() && count(O::bound(lo)) >= r) {
-            while (lo < hi) {
-                const unsigned mid = lo + (hi - lo + 1) / 2;
+            // halves of the values' range first, of the numbers' in between where that is slow
+            for (int step = 0; lo < hi; ++step) {
+                unsigned mid = lo + (hi - lo + 1) / 2;
+                if (step < 8) mid = min(max(__builtin_amdgcn_readfirstlane(O::of(0.5f * O::bound(lo) + 0.5f * O::bound(hi))), lo + 1), hi);
                 const int c = count(O::bound(mid));
                 if (c >= r) lo = mid;
                 else hi = mid - 1;
@@ -261,7 +264,7 @@ __global__ __launch_bounds__(NT, PIECES > 512 ? 3 : 4) void score_kernel(Args a)
                 s[1] = fmaf(e, fmaxf(d, -1e30f), s[1]);      // (a logit of -inf adds nothing)
             }
         }
-    block_sums<2>(s, buf2[0]);
+    block_sums<NT, 2>(s, buf2[0]);
     {
         // the product base c2 was rounded: all exponents are off by this, and the sums are brought back
         const float r = fmaf(base, c2, -off), f = __builtin_amdgcn_exp2f(-r);
@@ -287,8 +290,7 @@ __global__ __launch_bounds__(NT, PIECES > 512 ? 3 : 4) void score_kernel(Args a)
 #pragma unroll
             for (int j = 0; j < E; ++j) own = fmaxf(own, element(p, j));
         });
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) own = fmaxf(own, __shfl_xor(own, off, 64));
+        own = join_lanes(own, fmaxf_of);
         if (lane == 0) buf1[wave] = own;
         __syncthreads();
         top = buf1[0];
@@ -304,7 +306,7 @@ __global__ __launch_bounds__(NT, PIECES > 512 ? 3 : 4) void score_kernel(Args a)
                 s[1] = fmaf(e, fmaxf(d, -1e30f), s[1]);
             }
         });
-        block_sums<2>(s, buf2[1]);
+        block_sums<NT, 2>(s, buf2[1]);
     }
     if (tid == 0) {
         if (a.parts == 1) finish(a, row, base, s[0], s[1], zt, target);
@@ -373,7 +375,7 @@ __global__ __launch_bounds__(NT, PIECES > 512 ? 3 : 4) void score_kernel(Args a)
 #pragma unroll
                 for (int j = 0; j < E; ++j) c += element(p, j) >= b;
             });
-            return block_count(c, buf4);
+            return block_count<NT>(c, buf4);
         };
         unsigned lo = __builtin_amdgcn_readfirstlane(O::of(known ? fmaxf(bound, least) : least)), hi = __builtin_amdgcn_readfirstlane(O::of(top));
         const unsigned highest = hi;
@@ -435,7 +437,7 @@ __global__ __launch_bounds__(NT, PIECES > 512 ? 3 : 4) void score_kernel(Args a)
     }
     if (a.parts == 1) {
         const bool lost = !(s[0] == s[0]);
-        sort_keys(keys, have, a.k, [&](int i, Key key) {
+        sort_keys<NT>(keys, have, a.k, [&](int i, Key key) {
             a.top_index[row * a.k + i] = lost ? -1 : (int)~(unsigned)key;
             a.top_logit[row * a.k + i] = lost ? __builtin_nanf("") : unordered((unsigned)(key >> 32));
         });
@@ -445,7 +447,7 @@ __global__ __launch_bounds__(NT, PIECES > 512 ? 3 : 4) void score_kernel(Args a)
         }
     } else {
         Key *const list = a.lists + (int64_t)blockIdx.x * a.k;
-        sort_keys(keys, have, a.k, [&](int i, Key key) { list[i] = key; });
+        sort_keys<NT>(keys, have, a.k, [&](int i, Key key) { list[i] = key; });
         for (int i = have + tid; i < a.k; i += NT) list[i] = 0;
     }
 }
@@ -453,11 +455,10 @@ __global__ __launch_bounds__(NT, PIECES > 512 ? 3 : 4) void score_kernel(Args a)
 // Rows of several parts: sums brought to the largest maximum, lists joined.  At least k entries of all lists reach the least of the
 // lists' entries k / parts (counted from 1, rounded up), and also the largest of their k-th ones: what reaches both is sorted.
 template <int TYPE>
-__global__ __launch_bounds__(NT) void score_join_kernel(Args a)
+__global__ __launch_bounds__(256) void score_join_kernel(Args a)
 {
-    constexpr int KEYS = 2048;
+    constexpr int NT = 256, KEYS = 2048;
     __shared__ Key keys[KEYS];
-    __shared__ Key limits[WAVES][2];
     __shared__ int found;
     const int tid = threadIdx.x, lane = tid & 63;
     const int64_t row = blockIdx.x;
@@ -486,11 +487,11 @@ __global__ __launch_bounds__(NT) void score_join_kernel(Args a)
     }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) {
-        top = fmaxf(top, __shfl_xor(top, off, 64));
         const Key l = __shfl_xor(low, off, 64), h = __shfl_xor(high, off, 64);
         low = l < low ? l : low;
         high = h > high ? h : high;
     }
+    top = join_lanes(top, fmaxf_of);
     if (top == -__builtin_inff()) top = 0.f;
     for (int p = lane; p < a.parts; p += 64) {
         const Stats s = st[p];
@@ -499,11 +500,8 @@ __global__ __launch_bounds__(NT) void score_join_kernel(Args a)
         sum = fmaf(s.sum, w, sum);
         dot = fmaf(fmaf(s.sum, fmaxf(d, -1e30f), s.dot), w, dot);
     }
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) {
-        sum += __shfl_xor(sum, off, 64);
-        dot += __shfl_xor(dot, off, 64);
-    }
+    sum = sum_lanes(sum);
+    dot = sum_lanes(dot);
     if (tid == 0) finish(a, row, top, sum, dot, zt, target);
     if (a.k == 0) return;
     const bool lost = !(sum == sum);
@@ -526,7 +524,7 @@ __global__ __launch_bounds__(NT) void score_join_kernel(Args a)
     __syncthreads();
     int have = found;
     if (have <= KEYS) {
-        sort_keys(keys, have, a.k, put);
+        sort_keys<NT>(keys, have, a.k, put);
     } else {
         // too many: an entry's place is its own in its list and the number of larger ones in each of the others
         have = a.k;
@@ -556,17 +554,27 @@ __global__ __launch_bounds__(NT) void score_join_kernel(Args a)
 }
 
 struct Plan {
-    int pieces, parts, len;
+    int threads, pieces, parts, len;
     size_t lists, bytes;
 };
 
+// Threads and pieces to a part.  Many rows: 256 with 16 each, the most that leave four workgroups to a compute unit.  Few: a row that
+// 1024 threads hold goes to these, for the sooner end of it and of one launch (1 x 32000 in fp32: XX us against YY with 256 and a join);
+// longer ones to small parts, as many of them as there can be.
 inline Plan plan_of(int T, int V, int type, int k)
 {
     const int E = type == OBC_F32 ? 4 : 8;
     Plan p;
-    const int64_t large = (int64_t)NT * 16 * E;
-    p.pieces = k > 256 || (int64_t)T * ((V + large - 1) / large) >= 512 ? 16 : 4;
-    const int64_t most = (int64_t)NT * p.pieces * E;
+    const int64_t large = (int64_t)256 * 16 * E;
+    const bool many = (int64_t)T * ((V + large - 1) / large) >= 512;
+    if (!many && V > 256 * 4 * E && V <= 1024 * 8 * E) {
+        p.threads = 1024;
+        p.pieces = 8;
+    } else {
+        p.threads = 256;
+        p.pieces = many || k > 256 ? 16 : 4;
+    }
+    const int64_t most = (int64_t)p.threads * p.pieces * E;
     p.parts = (int)((V + most - 1) / most);
     p.len = (int)(((int64_t)V + p.parts - 1) / p.parts);
     p.len = (p.len + E - 1) / E * E;
@@ -579,18 +587,19 @@ inline Plan plan_of(int T, int V, int type, int k)
 }
 
 template <int TYPE>
-void launch(obc_ctx *ctx, const Args &a, int pieces)
+void launch(obc_ctx *ctx, const Args &a, const Plan &p)
 {
     const unsigned blocks = (unsigned)((int64_t)a.T * a.parts);
-    auto go = [&](auto ch) {
-        if (a.k == 0) score_kernel<TYPE, ch, 0, 0><<<blocks, NT, 0, ctx->stream>>>(a);
-        else if (a.k <= 256) score_kernel<TYPE, ch, 512, 1024><<<blocks, NT, 0, ctx->stream>>>(a);
-        else score_kernel<TYPE, ch, 1536, 2048><<<blocks, NT, 0, ctx->stream>>>(a);
+    auto go = [&](auto nt, auto ch) {
+        if (a.k == 0) score_kernel<TYPE, nt, ch, 0, 0><<<blocks, nt.value, 0, ctx->stream>>>(a);
+        else if (a.k <= 256) score_kernel<TYPE, nt, ch, 512, 1024><<<blocks, nt.value, 0, ctx->stream>>>(a);
+        else score_kernel<TYPE, nt, ch, 1536, 2048><<<blocks, nt.value, 0, ctx->stream>>>(a);
     };
-    if (pieces == 16) go(std::integral_constant<int, 16>());
-    else go(std::integral_constant<int, 4>());
+    if (p.threads == 1024) go(std::integral_constant<int, 1024>(), std::integral_constant<int, 8>());
+    else if (p.pieces == 16) go(std::integral_constant<int, 256>(), std::integral_constant<int, 16>());
+    else go(std::integral_constant<int, 256>(), std::integral_constant<int, 4>());
     if (a.parts == 1) return;
-    score_join_kernel<TYPE><<<a.T, NT, 0, ctx->stream>>>(a);
+    score_join_kernel<TYPE><<<a.T, 256, 0, ctx->stream>>>(a);
 }
 
 }  // namespace
@@ -622,15 +631,15 @@ int obc_score(obc_ctx *ctx, const void *z, int type, int T, int V, int64_t ldz, 
     if (!z) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_score: null z");
     if (((uintptr_t)z & (size_of_type(type) - 1)) != 0) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_score: z is not aligned to its elements");
     const Plan p = plan_of(T, V, type, k);
-    if (!obc_grid_fits((int64_t)T * p.parts, NT) || (int64_t)p.parts * k >= (int64_t)1 << 30)
+    if (!obc_grid_fits((int64_t)T * p.parts, p.threads) || (int64_t)p.parts * k >= (int64_t)1 << 30)
         return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_score: too many rows or columns");
     if (p.bytes > 0 && (!ws || ((uintptr_t)ws & 15) != 0 || ws_bytes < p.bytes))
         return obc_fail(ctx, OBC_ERR_WORKSPACE, "obc_score: workspace of %zu bytes needed", p.bytes);
     const Args a = {z, target, logp, entropy, lse, top_index, top_logit, T, V, k, p.parts, p.len, ldz, temperature, (Stats *)ws,
                     (Key *)((char *)ws + p.lists), ctx->d_status};
-    if (type == OBC_F32) launch<OBC_F32>(ctx, a, p.pieces);
-    else if (type == OBC_F16) launch<OBC_F16>(ctx, a, p.pieces);
-    else launch<OBC_BF16>(ctx, a, p.pieces);
+    if (type == OBC_F32) launch<OBC_F32>(ctx, a, p);
+    else if (type == OBC_F16) launch<OBC_F16>(ctx, a, p);
+    else launch<OBC_BF16>(ctx, a, p);
     OBC_LAUNCH_CHECK(ctx, "score_kernel");
     return OBC_OK;
 }
