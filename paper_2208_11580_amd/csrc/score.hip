@@ -101,7 +101,7 @@ template <int NT, typename OUT>
 __device__ inline void sort_keys(Key *keys, int n, int k, OUT out)
 {
     const int tid = threadIdx.x;
-    if (n <= 256) {
+    if (n <= (NT < 512 ? NT : 512)) {
         const Key own = tid < n ? keys[tid] : 0;
         int rank = 0;
         if (tid - (tid & 63) < n)
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(NT, NT == 1024 || PIECES <= 512 ? 4 : 3) void score
     if (tail) x[CH].load_end(z, (whole * NT + tid) * E, n);
     int target = -1;
     float zt = 0.f;
-    if (a.parts == 1 && tid == 0) {
+    if (a.parts == 1 && tid == NT - 64) {
         target = target_of(a, row);
         if (target >= 0) zt = load_as<TYPE>(a.z, row * a.ldz + target);
     }
@@ -222,9 +222,18 @@ __global__ __launch_bounds__(NT, NT == 1024 || PIECES <= 512 ? 4 : 3) void score
                 if (i < CH ? i < whole : tail) c += __popcll(__ballot(most[i] >= b));
             return c;
         };
+        if (r <= 4) {
+            // the largest taken away a few times
+            float rest = own;
+            bound = wave_top;
+            for (int i = 1; i < r; ++i) {
+                rest = lane == __ffsll(__ballot(rest == bound)) - 1 ? -__builtin_inff() : rest;
+                bound = join_lanes(rest, fmaxf_of);
+            }
+        }
         unsigned lo = O::of(-__builtin_inff()) + 1, hi = __builtin_amdgcn_readfirstlane(O::of(wave_top));
-        if (r <= 64 && wave_low > -__builtin_inff()) lo = __builtin_amdgcn_readfirstlane(O::of(wave_low));
-        if (wave_top < __builtin_inff() && count(O::bound(lo)) >= r) {
+        if (r > 4 && r <= 64 && wave_low > -__builtin_inff()) lo = __builtin_amdgcn_readfirstlane(O::of(wave_low));
+        if (r > 4 && wave_top < __builtin_inff() && count(O::bound(lo)) >= r) {
             // halves of the values' range first, of the numbers' in between where that is slow
             for (int step = 0; lo < hi; ++step) {
                 unsigned mid = lo + (hi - lo + 1) / 2;
@@ -308,7 +317,7 @@ __global__ __launch_bounds__(NT, NT == 1024 || PIECES <= 512 ? 4 : 3) void score
         });
         block_sums<NT, 2>(s, buf2[1]);
     }
-    if (tid == 0) {
+    if (tid == NT - 64) {      // (the last wave, which has the least to do with the largest)
         if (a.parts == 1) finish(a, row, base, s[0], s[1], zt, target);
         else a.stats[blockIdx.x] = Stats{base, s[0], s[1], 0.f};
     }
@@ -559,7 +568,7 @@ struct Plan {
 };
 
 // Threads and pieces to a part.  Many rows: 256 with 16 each, the most that leave four workgroups to a compute unit.  Few: a row that
-// 1024 threads hold goes to these, for the sooner end of it and of one launch (1 x 32000 in fp32: XX us against YY with 256 and a join);
+// 1024 threads hold goes to these, for the sooner end of it and of one launch (1 x 32000 in fp32: 8.2 us against 10.9 with 256 and a join);
 // longer ones to small parts, as many of them as there can be.
 inline Plan plan_of(int T, int V, int type, int k)
 {
