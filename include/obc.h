@@ -419,20 +419,22 @@ int obc_layernorm_grad(obc_ctx *ctx, const void *h, const float *gain, const flo
 /* y[t] = scale table[ids[t]] for T tokens, T x d.
  *   table   V x d of `type`, leading dimension ldt >= d;  y  of y_type, leading dimension ldy >= d (OBC_F32, OBC_F16, OBC_BF16 each)
  *   ids     T int32; negative: no token, a row of zeros
- * The product is fp32, rounded once.  An id >= V latches OBC_ERR_BAD_ARG and counts as no token.  1 <= d <= 2^20. */
+ * The product is fp32, rounded once.  An id >= V latches OBC_ERR_BAD_ARG and counts as no token.  y may not overlap
+ * the table.  1 <= d <= 2^20. */
 int obc_embed(obc_ctx *ctx, const void *table, int type, int V, int d, int64_t ldt, const int32_t *ids, int T, float scale, void *y,
               int y_type, int64_t ldy);
 
 /* The table's gradient: dtable[v] = scale sum over the tokens t with ids[t] = v of dy[t]; every row is written, with zeros where it
  * has no token.  accumulate != 0: dtable[v] += that, rows without a token are not touched.
  *   dy      T x d of `type`, leading dimension lddy >= d;  dtable  V x d of dtable_type, leading dimension lddt >= d
- * Sums are fp32, over an id's tokens in a fixed order; one rounding.  Ids as in obc_embed.  T <= 2^26. */
+ * Sums are fp32, over an id's tokens in a fixed order; one rounding.  Ids as in obc_embed.  dtable may not
+ * overlap dy.  T <= 2^26. */
 int obc_embed_grad_workspace_bytes(int T, int V, int d, size_t *bytes);
 int obc_embed_grad(obc_ctx *ctx, const int32_t *ids, int T, const void *dy, int type, int64_t lddy, float scale, int V, int d,
                    int accumulate, void *dtable, int dtable_type, int64_t lddt, void *ws, size_t ws_bytes);
 
 /* A tensor of obc_adamw_plan: n elements each, contiguous.  Inputs and outputs may be the same arrays (the usual case) or others that
- * do not overlap. */
+ * overlap nothing. */
 typedef struct obc_adamw_tensor {
     const void *p;                  /* parameters, of `type` */
     void *p_out;
@@ -453,7 +455,8 @@ typedef struct obc_adamw_tensor {
  *   tensors     HOST array; it may go when the call returns
  *   bits        of the moments: 32 or 8
  *   plan        obc_adamw_plan_bytes on the device, aligned to 16 bytes, opaque; written on the context's stream
- *   workgroups  HOST out, for obc_adamw.  (2^24 - 1 at most, of 2048 elements of a tensor each.) */
+ *   workgroups  HOST out, for obc_adamw.  (2^24 - 1 at most, of 2048 elements of a tensor each.)
+ * Arrays that a step writes may not overlap each other, so that a tensor is listed once. */
 int obc_adamw_plan_bytes(int count, size_t *bytes);
 int obc_adamw_plan(obc_ctx *ctx, const obc_adamw_tensor *tensors, int count, int type, int bits, void *plan, int64_t *workgroups);
 

@@ -228,7 +228,8 @@ def _no_grad(*tensors):
 
 
 class AdamPlan:
-    """The tensors of obc_adamw, which it keeps, laid out by obc_adamw_plan."""
+    """The tensors of obc_adamw, which it keeps, laid out by obc_adamw_plan for the context's stream.  (Their addresses: a tensor that is
+    given other memory needs another plan.  A captured graph needs its plans as long as it is replayed.)"""
 
     def __init__(self, ctx, params, grads, states, decay=0.01, out=None):
         params, states = list(params), list(states)
@@ -246,7 +247,7 @@ class AdamPlan:
         self.tensors = (AdamTensor * max(count, 1))()
         for i in range(count):
             d, p, st, new = self.tensors[i], params[i], states[i], self.new[1][i]
-            _no_grad(p, self.new[0][i], *st, *new)
+            ctx._take(p, self.new[0][i], *st, *new)
             n = d.n = p.numel()
             d.decay = float(decays[i])
             d.p, d.p_out = self._at(i, p, params[0].dtype, n), self._at(i, self.new[0][i], params[0].dtype, n)
@@ -271,11 +272,14 @@ class AdamPlan:
 
     def use(self, grads):
         """Other gradients from the next step on (on the context's stream: steps before this call keep theirs)."""
+        if self.ctx._capturing():
+            # the descriptors would be written by the graph's replays alone, and read by steps before them
+            raise ValueError("a plan is laid out before a capture, not in it")
         grads = list(grads)
         if len(grads) != self.count:
             raise ValueError("there must be as many gradients as parameters")
         addresses = [self._at(i, g, self.params[0].dtype, self.params[i].numel()) for i, g in enumerate(grads)]
-        _no_grad(*grads)
+        self.ctx._take(*grads)
         for t, g in zip(self.tensors, addresses):
             t.g = g
         n = c_int64()
@@ -573,6 +577,21 @@ class Context:
         with torch.cuda.stream(self.stream):
             return torch.empty(shape, dtype=dtype, device=device)
 
+    def _take(self, *tensors):
+        """Refuses what the calls below cannot take: tensors that autograd follows, or of another device than the context's, or
+        calls while another device is the current one."""
+        device = self._device
+        if torch._C._cuda_getDevice() != device:
+            raise ValueError("the context's device is cuda:%d, the current one is not" % device)
+        follows = torch.is_grad_enabled()
+        for t in tensors:
+            if t is None:
+                continue
+            if t.get_device() != device:
+                raise ValueError("the context's device is cuda:%d, a tensor's is %s" % (device, t.device))
+            if follows and t.requires_grad:
+                _no_grad(t)
+
     def _need(self, query, *sizes):
         """Workspace of one of the queries (asked once for each set of sizes): address, bytes, and what keeps it."""
         key = (query,) + sizes
@@ -749,7 +768,7 @@ class Context:
         t = _type_of(z, "z")
         zp, ldz, T, V = _rows_of(z, "z")
         out = {} if out is None else out
-        _no_grad(z, *out.values())
+        self._take(z, target, *out.values())
         k = int(top)
         if k < 0:
             raise ValueError("top must not be negative")
@@ -784,7 +803,7 @@ class Context:
         T, d = x.shape
         t = _type_of(x, "x")
         out = {} if out is None else out
-        _no_grad(x, gain, bias, residual, *out.values())
+        self._take(x, gain, bias, residual, *out.values())
         h = out.get("h")
         if h is None and residual is not None:
             h = self._empty((T, d), x.dtype, x.device)
@@ -813,7 +832,7 @@ class Context:
         T, d = h.shape
         t = _type_of(h, "h")
         out = {} if out is None else out
-        _no_grad(h, gain, mean, rstd, dy, dh, *out.values())
+        self._take(h, gain, mean, rstd, dy, dh, *out.values())
         dx = out.get("dx")
         if dx is None:
             dx = self._empty((T, d), h.dtype, h.device)
@@ -835,7 +854,7 @@ class Context:
     def obc_embed(self, table, ids, scale=1.0, out=None, out_dtype=None):
         """y[t] = scale table[ids[t]] (T x d); ids: T int32, negative: a row of zeros.  y has out's type, else out_dtype, else the
         table's."""
-        _no_grad(table, out)
+        self._take(table, ids, out)
         t = _type_of(table, "table")
         tp, ldt, V, d = _rows_of(table, "table")
         T = ids.numel()
@@ -852,7 +871,7 @@ class Context:
     def obc_embed_grad(self, ids, dy, rows, scale=1.0, out=None, out_dtype=None, accumulate=False):
         """The gradient (rows x d) of a table of so many rows that obc_embed read, from dy (T x d).  out's type, else out_dtype, else
         dy's; accumulate: added to out."""
-        _no_grad(dy, out)
+        self._take(ids, dy, out)
         t = _type_of(dy, "dy")
         dp, lddy, T, d = _rows_of(dy, "dy")
         if out is None:
@@ -892,10 +911,13 @@ class Context:
     def obc_adamw(self, plan, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=None, seed=0):
         """A step of AdamW over an AdamPlan's tensors.  step: an int, 1 for the first, or an int64 tensor on the device; lr: a float or
         an fp32 tensor on the device; grad_scale: an fp32 tensor on the device.  Returns the new parameters and states."""
+        if plan.ctx is not self:
+            raise ValueError("the plan is another context's, whose stream it was laid out on")
         step_at = lr_at = None
         if torch.is_tensor(step):
             if step.numel() != 1:
                 raise ValueError("step must be one value")
+            self._take(step)
             step_at, step = _ptr(step, torch.int64), 0
         if torch.is_tensor(lr):
             lr_at, lr = _vector(lr, 1, "lr"), 0.0

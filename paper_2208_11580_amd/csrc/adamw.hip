@@ -6,6 +6,8 @@
 // half of v's).  Those are rounded up or down by chance, from a hash of seed, step, tensor and element: rounded to nearest, v would
 // stay where it is, since a step changes it by a thousandth and the nearest 8-bit numbers are an eighth away.  A root that is not
 // zero does not become zero, or the next step would be divided by next to nothing.
+#include <algorithm>
+
 #include "row_io.h"
 
 namespace {
@@ -369,6 +371,21 @@ void launch(obc_ctx *ctx, const Args &a, unsigned blocks, bool bits8)
     else adamw_kernel<TYPE, false><<<blocks, NT, 0, ctx->stream>>>(a);
 }
 
+// Memory that a step writes, for the check that no two arrays share any
+struct Span {
+    uintptr_t from, to;
+};
+inline void put_span(Span *spans, int64_t &n, const void *p, int64_t bytes)
+{
+    if (p && bytes > 0) spans[n++] = Span{(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes};
+}
+// An output is its input, or apart from it.
+inline bool apart(const void *in, const void *out, int64_t bytes)
+{
+    const uintptr_t a = (uintptr_t)in, b = (uintptr_t)out;
+    return a == b || a + (uintptr_t)bytes <= b || b + (uintptr_t)bytes <= a;
+}
+
 }  // namespace
 
 extern "C" {
@@ -406,6 +423,30 @@ int obc_adamw_plan(obc_ctx *ctx, const obc_adamw_tensor *tensors, int count, int
         if (more > kMostBlocks - blocks) return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_adamw_plan: more elements than a launch takes");
         blocks += more;
     }
+    Span *const spans = new (std::nothrow) Span[(size_t)count * 6 + 1];
+    if (!spans) return obc_fail(ctx, OBC_ERR_HIP, "obc_adamw_plan: no host memory");
+    int64_t written = 0;
+    int whole = -1;
+    for (int i = 0; i < count; ++i) {
+        const obc_adamw_tensor &t = tensors[i];
+        if (t.n == 0) continue;
+        const int64_t p = t.n * (int64_t)size_of_type(type), m = t.n * (bits / 8), s = bits == 8 ? (t.n + kScaled - 1) / kScaled * 4 : 0;
+        if (!apart(t.p, t.p_out, p) || !apart(t.m, t.m_out, m) || !apart(t.v, t.v_out, m) || !apart(t.master, t.master_out, 4 * t.n) ||
+            !apart(t.m_scale, t.m_scale_out, s) || !apart(t.v_scale, t.v_scale_out, s))
+            whole = i;
+        put_span(spans, written, t.p_out, p);
+        put_span(spans, written, t.m_out, m);
+        put_span(spans, written, t.v_out, m);
+        put_span(spans, written, t.master_out, 4 * t.n);
+        put_span(spans, written, t.m_scale_out, s);
+        put_span(spans, written, t.v_scale_out, s);
+    }
+    std::sort(spans, spans + written, [](const Span &a, const Span &b) { return a.from < b.from; });
+    bool shared = false;
+    for (int64_t i = 1; i < written; ++i) shared |= spans[i].from < spans[i - 1].to;
+    delete[] spans;
+    if (whole >= 0) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw_plan: tensor %d: an output overlaps its input", whole);
+    if (shared) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw_plan: two outputs overlap (is a tensor listed twice?)");
     *workgroups = blocks;
     unsigned first = 0;
     for (int i = 0; i < count; i += kWritten) {

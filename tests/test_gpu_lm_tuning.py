@@ -802,3 +802,134 @@ def test_refusals(ctx):
         with torch.no_grad():
             call(lambda t: t.clone().requires_grad_())
     ctx.obc_check()
+
+
+@pytest.mark.parametrize("kind,factor", [("f32", 1e35), ("bf16", 1e35), ("f16", 2e3), ("f32", 1e-30), ("bf16", 1e-38)])
+def test_score_of_huge_and_tiny_logits(ctx, kind, factor):
+    """Differences that no exponential survives, maxima that a product with 1 / temperature brings near fp32's end, and logits that
+    are all but equal."""
+    g = _gen(1)
+    for V in (300, 9000, 40000):
+        z = (torch.randn(3, V, generator=g, device="cuda") * factor).to(TYPES[kind])
+        z[1, ::7] = -INF
+        z[2, ::3] = torch.finfo(TYPES[kind]).min
+        target = torch.randint(0, V, (3,), generator=g, device="cuda", dtype=torch.int32)
+        r = ctx.obc_score(z, target, top=12, temperature=0.5)
+        _check_score(r, z, target, 12, 0.5)
+    ctx.obc_check()
+
+
+@pytest.mark.parametrize("allowed", [1, 5, 63, 64, 65, 2000])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_score_of_constrained_answers(ctx, kind, allowed):
+    """Few tokens are allowed, fewer than are asked for and more: the rest is masked with -inf or with the type's lowest value."""
+    g = _gen(allowed)
+    V = 50000
+    z = torch.full((4, V), -INF, device="cuda")
+    for row in range(4):
+        at = torch.randperm(V, generator=g, device="cuda")[:allowed]
+        z[row, at] = torch.randn(allowed, generator=g, device="cuda")
+    z[2:] = z[2:].clamp_min(torch.finfo(TYPES[kind]).min)
+    z = z.to(TYPES[kind])
+    r = ctx.obc_score(z, None, top=64)
+    _check_score(r, z, None, 64, 1.0)
+    ctx.obc_check()
+
+
+def test_offsets_beyond_32_bits(ctx):
+    """Rows that begin beyond 2^31 and 2^32 elements."""
+    g = _gen(1)
+    big = torch.empty(3 * 1600000000 + 6000, dtype=torch.bfloat16, device="cuda")
+    z = big.as_strided((4, 5000), (1600000000, 1))
+    z.copy_(torch.randn(4, 5000, generator=g, device="cuda"))
+    target = torch.randint(0, 5000, (4,), generator=g, device="cuda", dtype=torch.int32)
+    want = ctx.obc_score(z.contiguous(), target, top=20)
+    got = ctx.obc_score(z, target, top=20)
+    assert all(torch.equal(want[n], got[n]) for n in want)
+    ids = torch.tensor([3, 1, -1, 2, 0, 3], dtype=torch.int32, device="cuda")
+    y = ctx.obc_embed(z, ids, scale=2.0)
+    assert torch.equal(y, ctx.obc_embed(z.contiguous(), ids, scale=2.0))
+    dt = ctx.obc_embed_grad(ids, y, 4)
+    z.zero_()
+    ctx.obc_embed_grad(ids, y, 4, out=z)
+    assert torch.equal(z, dt)
+    del big, z
+    T, d = 33000, 65536
+    x = torch.empty(T, d, dtype=torch.bfloat16, device="cuda")
+    x.normal_(generator=g)
+    gain, bias = torch.rand(d, generator=g, device="cuda"), torch.rand(d, generator=g, device="cuda")
+    n = ctx.obc_layernorm(x, gain, bias, want_stats=True)
+    last = ctx.obc_layernorm(x[-5:].contiguous(), gain, bias, want_stats=True)
+    assert all(torch.equal(n[k][-5:], last[k]) for k in ("y", "mean", "rstd"))
+    dy = n["y"]
+    r = ctx.obc_layernorm_grad(x, gain, n["mean"], n["rstd"], dy)
+    tail = ctx.obc_layernorm_grad(x[-5:].contiguous(), gain, n["mean"][-5:].contiguous(), n["rstd"][-5:].contiguous(), dy[-5:].contiguous())
+    assert torch.equal(r["dx"][-5:], tail["dx"])
+    ctx.obc_check()
+
+
+def test_adamw_beyond_32_bits(ctx):
+    """A tensor of more than 2^32 elements: its last ones as a short tensor's, but for the dither, which their places give."""
+    import paper_2208_11580_amd as pkg
+
+    n, m = 2 ** 32 + 5000, 5000 - 5000 % 256
+    p = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    grad = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g = _gen(2)
+    tail = slice(2 ** 32, 2 ** 32 + m)
+    grad[tail] = torch.randn(m, generator=g, device="cuda").to(torch.bfloat16)
+    st = ctx.obc_adamw_state(p, bits=8)
+    ctx.obc_adamw(ctx.obc_adamw_plan([p], [grad], [st], decay=0.0), 1, LR, B1, B2, EPS)
+    want = _adam_reference(p[tail] * 0, grad[tail], torch.zeros(m, device="cuda"), torch.zeros(m, device="cuda"), 1, decay=0.0)
+    _within(p[tail], want[0], want[3] + ROUND["bf16"] * 1.01 * want[0].abs() + TINY["bf16"])
+    assert (p[:2 ** 32].view(torch.int64) == 0).all()
+    scale = st.m_scale[2 ** 32 // 256:][:m // 256].double()
+    _within(scale, _blocks(want[1].abs()).amax(1) / 448, 8 * U32 * scale + 1e-30)
+    got = _values(st.m[tail], scale)
+    # up or down: within a step of an eighth, and of 2^-9 of the scale
+    assert ((got - want[1]).abs() <= want[1].abs() / 8 + 2.0 ** -9 * scale.repeat_interleave(256)).all()
+    assert isinstance(st, pkg.AdamState)
+
+
+def test_refusals_of_plans_and_devices(ctx):
+    import paper_2208_11580_amd as pkg
+
+    p, q = torch.zeros(600, device="cuda"), torch.zeros(600, device="cuda")
+    st, su = ctx.obc_adamw_state(p), ctx.obc_adamw_state(q)
+    both = pkg.AdamState(st.m, st.v)
+    big = torch.zeros(1000, device="cuda")
+    for args, out in ((([p, p], [p, p], [st, su]), None), (([p, q], [p, p], [st, both]), None), (([p], [q], [st]), ([st.m], [su])),
+                      (([big[:600]], [q], [st]), ([big[8:608]], [su])), (([p], [q], [pkg.AdamState(big[:600], big[400:])]), None),
+                      (([p, q], [p, p], [st, su]), ([big[:600], big[400:]], [ctx.obc_adamw_state(p), ctx.obc_adamw_state(p)]))):
+        if out is not None and out[0][0] is st.m:
+            out = ([su.m], [su])
+        with pytest.raises(pkg.ObcError):
+            ctx.obc_adamw_plan(*args, out=out)
+    ctx.obc_adamw_plan([big[:600], big[600:]], [p, p[:400]], [st, ctx.obc_adamw_state(big[600:])])      # neighbours are apart
+    plan = ctx.obc_adamw_plan([p], [q], [st])
+    other = pkg.Context()
+    with pytest.raises(ValueError):
+        other.obc_adamw(plan, 1, LR)
+    other._device = 1      # as if it were another device's
+    i3 = torch.zeros(3, dtype=torch.int32, device="cuda")
+    z = torch.zeros(3, 600, device="cuda")
+    for call in (lambda c: c.obc_score(z), lambda c: c.obc_layernorm(z, p), lambda c: c.obc_layernorm_grad(z, p, p[:3], p[:3], z),
+                 lambda c: c.obc_embed(z, i3), lambda c: c.obc_embed_grad(i3, z, 4), lambda c: c.obc_adamw_plan([p], [q], [st])):
+        with pytest.raises(ValueError):
+            call(other)
+    other._device = 0
+    other.close()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        c = pkg.Context(side)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            y = c.obc_embed(z, i3)
+            with pytest.raises(ValueError):
+                c.obc_adamw_plan([p], [q], [st])
+        graph.replay()
+        side.synchronize()
+        assert (y == 0).all()
+        del graph
+        c.close()
+    ctx.obc_check()
