@@ -37,7 +37,7 @@ __global__ __launch_bounds__(256) void embed_kernel(LookupArgs a)
     float v[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = 0.f;
-    if (id >= 0) load8<TYPE>(a.table, id * a.ldt + c, left, v);
+    if (id >= 0) load8_of<TYPE>(a.table, id * a.ldt, c, a.d, v);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = id >= 0 ? v[j] * a.scale : 0.f;
     store8<YT>(a.y, t * a.ldy + c, left, v);
@@ -204,35 +204,46 @@ struct GradArgs {
     int64_t lddy, lddt;
     float scale;
     bool accumulate;
+    int wide;            // waves next to one another in a row: 1 << wide
+    unsigned across;     // workgroups to a row
 };
 
 // Columns of a lane, 16 bytes of the wider of the two types: stores and loads of a wave's columns are whole lines
 template <int TYPE, int OT>
 constexpr int kCols = TYPE == OBC_F32 || OT == OBC_F32 ? 4 : 8;
 
-// `N` columns as fp32; only the first `left` are touched
+// `N` columns of a row of d at column c as fp32, zeros beyond its end
 template <int TYPE, int N>
-__device__ inline void load_cols(const void *p, int64_t at, int left, float (&v)[N])
+__device__ inline void load_cols(const void *p, int64_t base, int c, int d, float (&v)[N])
 {
     if (N == 8) {
         float w[8];
-        load8<TYPE>(p, at, left, w);
+        load8_of<TYPE>(p, base, c, d, w);
 #pragma unroll
         for (int j = 0; j < N; ++j) v[j] = w[j];
-    } else if (left >= N && TYPE == OBC_F32) {
-        const floatx4 w = *(const floatx4_at4 *)((const float *)p + at);
+    } else if (TYPE == OBC_F32) {
+        unsigned w[4];
+        load_words<OBC_F32>(p, base, c, d, 0u, w);
 #pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = w[j & 3];
-    } else if (left >= N) {
-        const uintx2 w = *(const uintx2_at2 *)((const unsigned short *)p + at);
+        for (int j = 0; j < N; ++j) v[j] = __builtin_bit_cast(float, w[j & 3]);
+    } else {
+        const unsigned short *const row = (const unsigned short *)p + base;
+        unsigned w[2] = {0u, 0u};
+        if (d >= 4) {
+            if (c < d) {
+                const uintx2 x = *(const uintx2_at2 *)(row + (c + 4 <= d ? c : d - 4));
+                w[0] = x.x;
+                w[1] = x.y;
+                if (c + 4 > d) move_words<true>(w, c + 4 - d, 0u);
+            }
+        } else {
+            for (int j = 0; c + j < d; ++j) w[j >> 1] |= (unsigned)row[c + j] << (16 * (j & 1));
+        }
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            const unsigned e = j & 2 ? w.y : w.x;
+            const unsigned e = w[j >> 1 & 1];
             v[j] = TYPE == OBC_F16 ? (j & 1 ? half_hi(e) : half_lo(e)) : (j & 1 ? bf16_hi(e) : bf16_lo(e));
         }
-    } else {
-#pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = j < left ? load_as<TYPE>(p, at + j) : 0.f;
     }
 }
 
@@ -267,7 +278,7 @@ __device__ inline void add_tokens(const GradArgs &a, int from, int to, int c, fl
             float v[many][N];
 #pragma unroll
             for (int i = 0; i < many; ++i)
-                if (left > 0) load_cols<TYPE, N>(a.dy, (int64_t)__builtin_amdgcn_readlane(mine, i0 + i) * a.lddy + c, left, v[i]);
+                if (left > 0) load_cols<TYPE, N>(a.dy, (int64_t)__builtin_amdgcn_readlane(mine, i0 + i) * a.lddy, c, a.d, v[i]);
 #pragma unroll
             for (int i = 0; i < many; ++i)
 #pragma unroll
@@ -305,14 +316,17 @@ __global__ __launch_bounds__(256) void embed_stretch_kernel(GradArgs a)
             if (j < left) a.part[(int64_t)blockIdx.x * a.d + c + j] = acc[j];
 }
 
-// 64 N columns of a table row to a wave, four rows to a workgroup
+// 64 N columns of a table row to a wave; a workgroup's four waves lie next to one another in a row (or in two, or four, where rows are
+// as short), and the workgroups of a row too: what is written at a time lies together.
 template <int TYPE, int OT>
 __global__ __launch_bounds__(256) void embed_grad_kernel(GradArgs a)
 {
     constexpr int N = kCols<TYPE, OT>;
-    const int c = (blockIdx.y * 64 + (threadIdx.x & 63)) * N, left = a.d - c;
-    const int64_t v = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (v >= a.V) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned group = blockIdx.x / a.across;      // of 4 >> a.wide rows
+    const int c = (((blockIdx.x - group * a.across) << a.wide | (wave & ((1 << a.wide) - 1))) * 64 + (threadIdx.x & 63)) * N, left = a.d - c;
+    const int64_t v = (int64_t)group * (4 >> a.wide) + (wave >> a.wide);
+    if (v >= a.V || left + (int)(threadIdx.x & 63) * N <= 0) return;
     const intx2 own = a.rows[v];
     const int s = own.x, e = s + own.y;
     if (a.accumulate && s == e) return;
@@ -321,14 +335,12 @@ __global__ __launch_bounds__(256) void embed_grad_kernel(GradArgs a)
         add_tokens<TYPE, N, 8>(a, s, e, c, acc);
     } else if (left > 0) {
         const int first = s / a.stretch, last = (e - 1) / a.stretch;
-        const float *p = a.part + ((int64_t)first * 2 + (s > first * a.stretch)) * a.d + c;
-        load_cols<OBC_F32, N>(p, 0, left, acc);
-        p = a.part + c;
+        load_cols<OBC_F32, N>(a.part, ((int64_t)first * 2 + (s > first * a.stretch)) * a.d, c, a.d, acc);
         for (int q = first + 1; q <= last; q += 8) {
             float x[8][N];
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (q + i <= last) load_cols<OBC_F32, N>(p, (int64_t)(q + i) * 2 * a.d, left, x[i]);
+                if (q + i <= last) load_cols<OBC_F32, N>(a.part, (int64_t)(q + i) * 2 * a.d, c, a.d, x[i]);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if (q + i <= last)
@@ -338,7 +350,7 @@ __global__ __launch_bounds__(256) void embed_grad_kernel(GradArgs a)
     }
     if (left <= 0) return;
     float old[N] = {};
-    if (a.accumulate) load_cols<OT, N>(a.dtable, v * a.lddt + c, left, old);
+    if (a.accumulate) load_cols<OT, N>(a.dtable, v * a.lddt, c, a.d, old);
 #pragma unroll
     for (int j = 0; j < N; ++j) acc[j] = a.accumulate ? fmaf(acc[j], a.scale, old[j]) : s < e ? acc[j] * a.scale : 0.f;
     store_cols<OT, N>(a.dtable, v * a.lddt + c, left, acc);
@@ -389,18 +401,35 @@ void launch_lookup(obc_ctx *ctx, const LookupArgs &a, int y_type)
     else launch_lookup<TYPE, OBC_BF16>(ctx, a);
 }
 
-inline int type_cols(int type, int out_type) { return type == OBC_F32 || out_type == OBC_F32 ? 4 : 8; }
+struct RowGrid {
+    int wide;
+    unsigned across;
+    int64_t blocks;
+};
+
+inline RowGrid row_grid(int V, int d, int type, int out_type)
+{
+    const int n = 64 * (type == OBC_F32 || out_type == OBC_F32 ? 4 : 8), waves = (d + n - 1) / n;
+    RowGrid g;
+    g.wide = waves > 2 ? 2 : waves > 1 ? 1 : 0;
+    g.across = (unsigned)(waves + (1 << g.wide) - 1) >> g.wide;
+    const int rows = 4 >> g.wide;
+    g.blocks = ((int64_t)V + rows - 1) / rows * g.across;
+    return g;
+}
 
 template <int TYPE>
-void launch_grad(obc_ctx *ctx, const GradArgs &a, int out_type)
+void launch_grad(obc_ctx *ctx, GradArgs a, int out_type)
 {
     if (a.T > a.stretch) {
         constexpr int N = kCols<TYPE, OBC_F32>;
         const dim3 grid((unsigned)(((int64_t)a.T + a.stretch - 1) / a.stretch * 2), (a.d + 256 * N - 1) / (256 * N));
         embed_stretch_kernel<TYPE><<<grid, 256, 0, ctx->stream>>>(a);
     }
-    const int n = type_cols(TYPE, out_type);
-    const dim3 grid((unsigned)(((int64_t)a.V + 3) / 4), (a.d + 64 * n - 1) / (64 * n));
+    const RowGrid g = row_grid(a.V, a.d, TYPE, out_type);
+    a.wide = g.wide;
+    a.across = g.across;
+    const unsigned grid = (unsigned)g.blocks;
     if (out_type == OBC_F32) embed_grad_kernel<TYPE, OBC_F32><<<grid, 256, 0, ctx->stream>>>(a);
     else if (out_type == OBC_F16) embed_grad_kernel<TYPE, OBC_F16><<<grid, 256, 0, ctx->stream>>>(a);
     else embed_grad_kernel<TYPE, OBC_BF16><<<grid, 256, 0, ctx->stream>>>(a);
@@ -456,9 +485,7 @@ int obc_embed_grad(obc_ctx *ctx, const int32_t *ids, int T, const void *dy, int 
     if (!dtable || (T > 0 && (!ids || !dy))) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_embed_grad: null argument");
     if ((T > 0 && (((uintptr_t)dy & (size_of_type(type) - 1)) != 0 || ((uintptr_t)ids & 3) != 0)) || ((uintptr_t)dtable & (size_of_type(dtable_type) - 1)) != 0)
         return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_embed_grad: an array is not aligned to its elements");
-    const int n = 64 * type_cols(type, dtable_type);
-    const int64_t chunks = (d + n - 1) / n;
-    if (!obc_grid_fits(((int64_t)V + 3) / 4 * chunks, 256)) return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_embed_grad: too many table rows");
+    if (!obc_grid_fits(row_grid(V, d, type, dtable_type).blocks, 256)) return obc_fail(ctx, OBC_ERR_BAD_SHAPE, "obc_embed_grad: too many table rows");
     const Plan p = plan_of(T, V, d);
     if (!ws || ((uintptr_t)ws & 15) != 0 || ws_bytes < p.bytes)
         return obc_fail(ctx, OBC_ERR_WORKSPACE, "obc_embed_grad: workspace of %zu bytes needed", p.bytes);
@@ -467,7 +494,7 @@ int obc_embed_grad(obc_ctx *ctx, const int32_t *ids, int T, const void *dy, int 
     const int slices = slices_of(V);
     embed_sort_kernel<<<slices, 64 * kWaves, 0, ctx->stream>>>(SortArgs{ids, rows, order, total, T, V, slices, ctx->d_status});
     OBC_LAUNCH_CHECK(ctx, "embed_sort_kernel");
-    const GradArgs a = {ids, order, total, rows, dy, dtable, (float *)((char *)ws + p.part), T, V, d, stretch_of(T), lddy, lddt, scale, accumulate != 0};
+    const GradArgs a = {ids, order, total, rows, dy, dtable, (float *)((char *)ws + p.part), T, V, d, stretch_of(T), lddy, lddt, scale, accumulate != 0, 0, 1};
     if (type == OBC_F32) launch_grad<OBC_F32>(ctx, a, dtable_type);
     else if (type == OBC_F16) launch_grad<OBC_F16>(ctx, a, dtable_type);
     else launch_grad<OBC_BF16>(ctx, a, dtable_type);

@@ -57,6 +57,64 @@ __device__ inline void store8(void *p, int64_t at, int left, const float (&v)[8]
     }
 }
 
+// N words moved to the front by `by` half-words (HALF) or words, `fill` behind them; by a power of two at a time
+template <bool HALF, int N>
+__device__ inline void move_words(unsigned (&w)[N], int by, unsigned fill)
+{
+#pragma unroll
+    for (int step = N / 2; step > 0; step >>= 1) {
+        const bool on = by & (HALF ? 2 * step : step);
+#pragma unroll
+        for (int j = 0; j < N; ++j) w[j] = on ? (j + step < N ? w[j + step < N ? j + step : j] : fill) : w[j];
+    }
+    if (HALF) {
+        const bool on = by & 1;
+#pragma unroll
+        for (int j = 0; j < N; ++j) w[j] = on ? w[j] >> 16 | (j + 1 < N ? w[j + 1 < N ? j + 1 : j] : fill) << 16 : w[j];
+    }
+}
+
+// 16 bytes of a row at column c of d, `fill` beyond its end (in both halves of a word).  At the row's end the last 16 bytes are read and
+// moved, for one load instead of several that wait for each other; only a row shorter than that goes element by element.
+template <int TYPE>
+__device__ inline void load_words(const void *p, int64_t base, int c, int d, unsigned fill, unsigned (&w)[4])
+{
+    constexpr int E = TYPE == OBC_F32 ? 4 : 8;
+    const char *const row = (const char *)p + base * (16 / E);
+    if (c + E <= d || (d >= E && c < d)) {
+        const char *const at = row + (unsigned)(c + E <= d ? c : d - E) * (16u / E);
+        const uintx4 v = TYPE == OBC_F32 ? __builtin_bit_cast(uintx4, (floatx4) * (const floatx4_at4 *)at) : (uintx4) * (const uintx4_at2 *)at;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = v[j];
+        if (c + E > d) move_words<TYPE != OBC_F32>(w, c + E - d, fill);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = fill;
+    if (c >= d) return;
+#pragma unroll
+    for (int j = 0; j < E; ++j)
+        if (c + j < d) {
+            if (TYPE == OBC_F32) w[j & 3] = ((const unsigned *)row)[c + j];
+            else w[j >> 1] = j & 1 ? (w[j >> 1] & 0xffffu) | (unsigned)((const unsigned short *)row)[c + j] << 16
+                                   : (w[j >> 1] & 0xffff0000u) | ((const unsigned short *)row)[c + j];
+        }
+}
+
+// Eight elements of a row of d at column c as fp32, zeros beyond its end
+template <int TYPE>
+__device__ inline void load8_of(const void *p, int64_t base, int c, int d, float (&v)[8])
+{
+    unsigned w[2][4];
+    load_words<TYPE>(p, base, c, d, 0u, w[0]);
+    if (TYPE == OBC_F32) load_words<TYPE>(p, base, c + 4, d, 0u, w[1]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const unsigned e = TYPE == OBC_F32 ? w[j >> 2][j & 3] : w[0][j >> 1];
+        v[j] = TYPE == OBC_F32 ? __builtin_bit_cast(float, e) : TYPE == OBC_F16 ? (j & 1 ? half_hi(e) : half_lo(e)) : (j & 1 ? bf16_hi(e) : bf16_lo(e));
+    }
+}
+
 // Eight elements on their way, in their own type
 template <int TYPE>
 struct Eight {
