@@ -3,6 +3,11 @@
 //   mean = sum h / d, var = sum (h - mean)^2 / d, y = (h - mean) rstd gain + bias
 // A row is read once and kept in registers: the mean first, then the squares of what is left, so that a large mean costs the
 // variance no digits; 8 bits take a third reduction, the largest |y|.
+//
+// Memory-bound: 4096 x 8192 in bf16 with residual and sum, 268 MB, takes 54 us with fresh inputs (5.0 TB/s; a large copy reaches 5.2), one row of
+// 768 2.6 us, of which an empty launch is 2.  The backward pass keeps each workgroup's shares of the gain's and the bias's gradient in registers
+// over its rows: 4096 x 4096 in bf16 with the residual's gradient, 134 MB, takes 29 to 37 us (fresh inputs), 24 to 31 of them the
+// rows and 5 the sum of 512 shares.
 #include "row_io.h"
 
 namespace {
@@ -49,6 +54,7 @@ struct NormArgs {
     float *y_scale, *mean, *rstd;
     float eps;
     int T, d;
+    bool past;
 };
 
 template <int TYPE, bool Q8, int NT, int CH>
@@ -69,7 +75,7 @@ __global__ __launch_bounds__(NT) void layernorm_kernel(NormArgs a)
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[k][j] += r[j];
         }
-        if (a.h) store8<TYPE>(a.h, base + c, left, v[k]);
+        if (a.h) put8<TYPE>(a.h, base + c, left, v[k], a.past);
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[0] += v[k][j];      // (zeros beyond the row's end)
     }
@@ -105,7 +111,7 @@ __global__ __launch_bounds__(NT) void layernorm_kernel(NormArgs a)
             v[k][j] = fmaf(v[k][j] * rstd, g[j], a.bias ? b[j] : 0.f);
             if (Q8) top = larger(top, v[k][j]);
         }
-        if (!Q8) store8<TYPE>(a.y, base + c, left, v[k]);
+        if (!Q8) put8<TYPE>(a.y, base + c, left, v[k], a.past);
     }
     if (!Q8) return;
     top = largest<NT>(top, &buf[2][0][0]);
@@ -138,6 +144,7 @@ struct GradArgs {
     void *dx;
     float *part;      // per workgroup: its rows' share of dgain, then of dbias
     int T, d;
+    bool past;
 };
 
 // Workgroup b takes the rows b, b + gridDim.x, ... and keeps its columns' shares of dgain and dbias in registers; the next
@@ -197,7 +204,7 @@ __global__ __launch_bounds__(NT) void layernorm_grad_kernel(GradArgs a)
             if (a.dh) dh[k].get(r);
 #pragma unroll
             for (int j = 0; j < 8; ++j) r[j] = fmaf(rstd, fmaf(-x[k][j], m1, g[k][j] - m0), r[j]);
-            store8<TYPE>(a.dx, base + c, left, r);
+            put8<TYPE>(a.dx, base + c, left, r, a.past);
         }
     }
 #pragma unroll
@@ -259,7 +266,7 @@ __global__ __launch_bounds__(1024) void layernorm_grad_wide_kernel(GradArgs a)
             if (a.dh) load8<TYPE>(a.dh, base + c, left, r);
 #pragma unroll
             for (int j = 0; j < 8; ++j) r[j] = fmaf(rstd, fmaf(-(x[j] - mean) * rstd, m1, g[j] * w[j] - m0), r[j]);
-            store8<TYPE>(a.dx, base + c, left, r);
+            put8<TYPE>(a.dx, base + c, left, r, a.past);
         }
     }
     if (!SHARES) return;
@@ -328,12 +335,15 @@ inline int grad_parts(int T) { return T < 512 ? T : 512; }
 template <int TYPE, bool Q8>
 void launch_norm(obc_ctx *ctx, const NormArgs &a)
 {
+    // Few rows: as many threads to a row as it has pieces, for the sooner end of each.  Many: the fewest that leave a row's values in
+    // registers without giving up waves (fresh inputs: 4096 x 8192 in bf16 with 512 threads 54 us, 256 59, 1024 55 to 57; 2000 x 8000 in fp32
+    // with 1024 54 us, 512 60, 256 63; 4096 x 4096 in bf16 22.3 us with 256 or 512)
     const bool few = a.T <= 512;
     if (a.d <= 2048) layernorm_kernel<TYPE, Q8, 256, 1><<<a.T, 256, 0, ctx->stream>>>(a);
     else if (a.d <= 4096 && few) layernorm_kernel<TYPE, Q8, 512, 1><<<a.T, 512, 0, ctx->stream>>>(a);
     else if (a.d <= 4096) layernorm_kernel<TYPE, Q8, 256, 2><<<a.T, 256, 0, ctx->stream>>>(a);
-    else if (a.d <= 8192 && few) layernorm_kernel<TYPE, Q8, 1024, 1><<<a.T, 1024, 0, ctx->stream>>>(a);
-    else if (a.d <= 8192) layernorm_kernel<TYPE, Q8, 256, 4><<<a.T, 256, 0, ctx->stream>>>(a);
+    else if (a.d <= 8192 && (few || TYPE == OBC_F32)) layernorm_kernel<TYPE, Q8, 1024, 1><<<a.T, 1024, 0, ctx->stream>>>(a);
+    else if (a.d <= 8192) layernorm_kernel<TYPE, Q8, 512, 2><<<a.T, 512, 0, ctx->stream>>>(a);
     else if (a.d <= 16384) layernorm_kernel<TYPE, Q8, 512, 4><<<a.T, 512, 0, ctx->stream>>>(a);
     else layernorm_kernel<TYPE, Q8, 1024, 8><<<a.T, 1024, 0, ctx->stream>>>(a);
 }
@@ -380,7 +390,7 @@ int obc_layernorm(obc_ctx *ctx, const void *x, const void *residual, int x_type,
         const size_t at = (size_t)t0 * d;
         const NormArgs a = {(const char *)x + at * in, residual ? (const char *)residual + at * in : nullptr, gain, bias,
                             h ? (char *)h + at * in : nullptr, (char *)y + at * out, y_scale ? y_scale + t0 : nullptr,
-                            mean ? mean + t0 : nullptr, rstd ? rstd + t0 : nullptr, eps, T - t0 < kMost ? (int)(T - t0) : kMost, d};
+                            mean ? mean + t0 : nullptr, rstd ? rstd + t0 : nullptr, eps, T - t0 < kMost ? (int)(T - t0) : kMost, d, (int64_t)T * d * (int64_t)(out + (h ? in : 0)) > kCaches};
         if (x_type == OBC_F32) q8 ? launch_norm<OBC_F32, true>(ctx, a) : launch_norm<OBC_F32, false>(ctx, a);
         else if (x_type == OBC_F16) q8 ? launch_norm<OBC_F16, true>(ctx, a) : launch_norm<OBC_F16, false>(ctx, a);
         else q8 ? launch_norm<OBC_BF16, true>(ctx, a) : launch_norm<OBC_BF16, false>(ctx, a);
@@ -412,7 +422,7 @@ int obc_layernorm_grad(obc_ctx *ctx, const void *h, const float *gain, const flo
     if (need > 0 && (!ws || ((uintptr_t)ws & 15) != 0 || ws_bytes < need))
         return obc_fail(ctx, OBC_ERR_WORKSPACE, "obc_layernorm_grad: workspace of %zu bytes needed", need);
     if (T > 0) {
-        const GradArgs a = {h, dy, dh, gain, mean, rstd, dx, (float *)ws, T, d};
+        const GradArgs a = {h, dy, dh, gain, mean, rstd, dx, (float *)ws, T, d, (int64_t)T * d * (int64_t)size_of_type(type) > kCaches};
         if (type == OBC_F32) launch_grad<OBC_F32>(ctx, a);
         else if (type == OBC_F16) launch_grad<OBC_F16>(ctx, a);
         else launch_grad<OBC_BF16>(ctx, a);

@@ -57,6 +57,25 @@ __device__ inline void store8(void *p, int64_t at, int left, const float (&v)[8]
     }
 }
 
+// As store8, past the caches where `past` says so: results that are larger than what the dies' caches hold (4 MB each) only push out what
+// is still to be read (layer norm of 4096 x 4096 in bf16: 22.7 us instead of 32, lookup of 16384 x 4096: 32 instead of 44).
+constexpr int64_t kCaches = 32 << 20;
+
+template <int TYPE>
+__device__ inline void put8(void *p, int64_t at, int left, const float (&v)[8], bool past)
+{
+    if (left < 8 || !past) return store8<TYPE>(p, at, left, v);
+    if (TYPE == OBC_F32) {
+        __builtin_nontemporal_store(floatx4{v[0], v[1], v[2], v[3]}, (floatx4_at4 *)((float *)p + at));
+        __builtin_nontemporal_store(floatx4{v[4], v[5], v[6], v[7]}, (floatx4_at4 *)((float *)p + at + 4));
+    } else {
+        uintx4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = TYPE == OBC_F16 ? pair_f16(v[2 * j], v[2 * j + 1]) : pair_bf16(v[2 * j], v[2 * j + 1]);
+        __builtin_nontemporal_store(w, (uintx4_at2 *)((unsigned short *)p + at));
+    }
+}
+
 // N words moved to the front by `by` half-words (HALF) or words, `fill` behind them; by a power of two at a time
 template <bool HALF, int N>
 __device__ inline void move_words(unsigned (&w)[N], int by, unsigned fill)
