@@ -134,6 +134,9 @@ __device__ inline void sort_keys(Key *keys, int n, int k, OUT out)
     for (int i = tid; i < n && i < k; i += NT) out(i, keys[i]);
 }
 
+// (a - b) c, where a - b may be beyond fp32's end
+__device__ inline float difference(float a, float b, float c) { return 2.f * ((0.5f * a - 0.5f * b) * c); }
+
 // The results of a row; one thread
 __device__ inline void finish(const Args &a, int64_t row, float top, float sum, float dot, float zt, int target)
 {
@@ -142,7 +145,7 @@ __device__ inline void finish(const Args &a, int64_t row, float top, float sum, 
     const float ln = logf(sum);
     if (a.lse) a.lse[row] = none ? -__builtin_inff() : top / a.tau + ln;
     if (a.entropy) a.entropy[row] = none ? 0.f : fmaf(-kLn2, dot / sum, ln);
-    if (a.logp) a.logp[row] = target < 0 ? 0.f : none ? -__builtin_inff() : (zt - top) / a.tau - ln;
+    if (a.logp) a.logp[row] = target < 0 ? 0.f : none ? -__builtin_inff() : 2.f * ((0.5f * zt - 0.5f * top) / a.tau) - ln;
 }
 
 __device__ inline int target_of(const Args &a, int64_t row)
@@ -286,8 +289,8 @@ __global__ __launch_bounds__(NT, NT == 1024 || PIECES <= 512 ? 4 : 3) void score
         s[0] *= f;
     }
     // Numbers that these short ways do not know (NaN, infinities, and beyond 2^100; bf16: nothing but -inf and what is near the type's
-    // lowest to reach the bound): once more, from the caches, for here and below.  Loops over the registers would take some from the
-    // usual way.
+    // lowest to reach the bound, or a temperature so high that a logit the maxima dropped would not make the sum infinite): once more,
+    // from the caches, for here and below.  Loops over the registers would take some from the usual way.
     const int pieces = (n + NT * E - 1) / (NT * E);
     auto all = [&](auto f) {
 #pragma unroll 4
@@ -297,7 +300,7 @@ __global__ __launch_bounds__(NT, NT == 1024 || PIECES <= 512 ? 4 : 3) void score
             f(p, from + (i * NT + tid) * E);
         }
     };
-    const bool known = s[0] < __builtin_inff() && fabsf(off) < 0x1p100f && (TYPE != OBC_BF16 || (fabsf(base) < 0x1p120f && (KEYS == 0 || bound > -0x1p120f)));
+    const bool known = s[0] < __builtin_inff() && fabsf(off) < 0x1p100f && (TYPE != OBC_BF16 || (c2 > 0x1p-100f && fabsf(base) < 0x1p120f && (KEYS == 0 || bound > -0x1p120f)));
     if (!known) {
         own = -__builtin_inff();
         all([&](const Piece<TYPE> &p, int) {
@@ -315,7 +318,7 @@ __global__ __launch_bounds__(NT, NT == 1024 || PIECES <= 512 ? 4 : 3) void score
         all([&](const Piece<TYPE> &p, int) {
 #pragma unroll
             for (int j = 0; j < E; ++j) {
-                const float d = (element(p, j) - base) * c2, e = __builtin_amdgcn_exp2f(d);
+                const float d = difference(element(p, j), base, c2), e = __builtin_amdgcn_exp2f(d);
                 s[0] += e;
                 s[1] = fmaf(e, fmaxf(d, -1e30f), s[1]);
             }
@@ -510,7 +513,7 @@ __global__ __launch_bounds__(256) void score_join_kernel(Args a)
     for (int p = lane; p < a.parts; p += 64) {
         const Stats s = st[p];
         if (s.sum == 0.f) continue;
-        const float d = (s.top - top) * c2, w = __builtin_amdgcn_exp2f(d);
+        const float d = difference(s.top, top, c2), w = __builtin_amdgcn_exp2f(d);
         sum = fmaf(s.sum, w, sum);
         dot = fmaf(fmaf(s.sum, fmaxf(d, -1e30f), s.dot), w, dot);
     }

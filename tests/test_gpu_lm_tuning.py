@@ -933,3 +933,22 @@ def test_refusals_of_plans_and_devices(ctx):
         del graph
         c.close()
     ctx.obc_check()
+
+
+@pytest.mark.parametrize("V", [300, 9000, 40000])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("power", [90, 105, 115, 120, 125])
+def test_score_at_temperatures_as_large_as_the_logits(ctx, power, kind, V):
+    """Logits up to the ends of their types at temperatures that bring them back to a few units: differences of two logits are beyond
+    fp32's end, and every logit counts."""
+    g = _gen(power)
+    end = torch.finfo(TYPES[kind]).max
+    z = (torch.randn(4, V, generator=g, device="cuda") * 2.0 ** min(power, 125)).clamp(-end, end).to(TYPES[kind])
+    z[1, 1::5] = -end
+    z[1, 3] = end
+    z[2, V // 2:] = -INF
+    z[3] = z[3].abs().neg()
+    target = torch.tensor([0, 1, V - 1, 2], dtype=torch.int32, device="cuda")
+    for k in (0, 12, 300):
+        _check_score(ctx.obc_score(z, target, top=k, temperature=2.0 ** power), z, target, k, 2.0 ** power)
+    ctx.obc_check()
