@@ -914,10 +914,10 @@ class Context:
         if plan.ctx is not self:
             raise ValueError("the plan is another context's, whose stream it was laid out on")
         step_at = lr_at = None
+        self._take(grad_scale, *(t for t in (step, lr) if torch.is_tensor(t)))
         if torch.is_tensor(step):
             if step.numel() != 1:
                 raise ValueError("step must be one value")
-            self._take(step)
             step_at, step = _ptr(step, torch.int64), 0
         if torch.is_tensor(lr):
             lr_at, lr = _vector(lr, 1, "lr"), 0.0
