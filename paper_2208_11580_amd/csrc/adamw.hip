@@ -8,7 +8,7 @@
 // zero does not become zero, or the next step would be divided by next to nothing.
 //
 // Memory-bound: 52 million parameters in bf16 with fp32 copies and 8-bit moments, 835 MB, take 156 to 175 us (5.0 TB/s), 26 million in fp32
-// with fp32 moments, 728 MB, 133 us (5.5 TB/s); 50 tensors of 768 values 3.7 us.  With 8 bits the vector instructions, a hundred to a
+// with fp32 moments, 728 MB, 133 us (5.5 TB/s); 50 tensors of 768 values 3.7 us.  With 8 bits the vector instructions, some 80 to a
 // parameter, are busy for most of that time.
 #include <algorithm>
 
