@@ -9,7 +9,7 @@
 // of several parts are joined by a second kernel.
 //
 // Bound by vector issue, with memory close behind: 2048 x 131072 in bf16 with 64 alternatives, 537 MB, takes 123 us a call (4.4 TB/s; plain reads
-// reach 6.0), 117 of them the parts (1500 instructions a wave, half of them for the two sums; vector units active 72 % of the time) and 9
+// reach 6.0), 117 of them the parts (1640 instructions a wave, half of them for the two sums; vector units active 72 % of the time) and 9
 // the join.  One row of 32000 in fp32 with 20 alternatives takes 8.2 us in one launch, 5 without alternatives.  Workgroups that stay and load the
 // next part as they sum this one took 154 us.
 #include <type_traits>
