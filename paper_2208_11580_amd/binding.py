@@ -174,7 +174,7 @@ def _ptr(t, dtype=None):
         raise ValueError("libobc takes contiguous tensors")
     if dtype is not None and t.dtype != dtype:
         raise ValueError("expected %s, got %s" % (dtype, t.dtype))
-    return c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _type_of(t, what, i8=False):
@@ -800,7 +800,7 @@ class Context:
     def obc_layernorm(self, x, gain, bias=None, eps=1e-5, residual=None, quant8=False, want_stats=False, out=None):
         """h = x + residual and its layer norm y.  out may hold h, y, scale (quant8), mean and rstd; without a residual, h is x
         itself."""
-        T, d = x.shape
+        T, d = shape = x.shape
         t = _type_of(x, "x")
         out = {} if out is None else out
         self._take(x, gain, bias, residual, *out.values())
@@ -818,7 +818,7 @@ class Context:
             mean = self._empty((T,), torch.float32, x.device) if mean is None else mean
             rstd = self._empty((T,), torch.float32, x.device) if rstd is None else rstd
         for other in (residual, h, y):
-            if other is not None and other.shape != x.shape:
+            if other is not None and other.shape != shape:
                 raise ValueError("residual, h and y must have x's shape")
         self._ck(self.lib.obc_layernorm(self.h, _ptr(x), _ptr(residual, x.dtype), t, _vector(gain, d, "gain"), _vector(bias, d, "bias"),
                                         float(eps), T, d, _ptr(h, x.dtype), _ptr(y, torch.int8 if quant8 else x.dtype),
@@ -829,7 +829,7 @@ class Context:
     def obc_layernorm_grad(self, h, gain, mean, rstd, dy, dh=None, out=None):
         """Gradients of x (and of the residual), the gain and the bias, from what the forward pass left; out may hold dx, dgain and
         dbias."""
-        T, d = h.shape
+        T, d = shape = h.shape
         t = _type_of(h, "h")
         out = {} if out is None else out
         self._take(h, gain, mean, rstd, dy, dh, *out.values())
@@ -843,7 +843,7 @@ class Context:
         if dbias is None:
             dbias = self._empty((d,), torch.float32, h.device)
         for other in (dy, dh, dx):
-            if other is not None and other.shape != h.shape:
+            if other is not None and other.shape != shape:
                 raise ValueError("dy, dh and dx must have h's shape")
         ws, n, _held = self._need("obc_layernorm_grad_workspace_bytes", T, d)
         self._ck(self.lib.obc_layernorm_grad(self.h, _ptr(h), _vector(gain, d, "gain"), _vector(mean, T, "mean"), _vector(rstd, T, "rstd"),
