@@ -6,9 +6,10 @@
 // waves add up the tokens of a table row, each in its columns, and write them, zeros where there is none.  Rows with more tokens than a
 // stretch of the sorted ones holds are summed by stretches first, in parallel, and then over these.
 //
-// Memory-bound: the lookup of 16384 x 4096 in bf16 takes 31 us (188 MB, 6.1 TB/s: the table partly from the caches).  The gradient of 16384 x 4096 in bf16 into 32000 rows of fp32, 650
-// MB, takes 165 us with fresh inputs, 111 to 123 with inputs that the memory's cache holds: the order 9, the stretches 25, the rows 130 (4.7 TB/s); of
-// 100 x 768 in fp32 into 5000 rows, 15 MB, 10.9 us in two dependent launches.
+// Memory-bound: the lookup of 16384 x 4096 in bf16 takes 31 us (188 MB, 6.1 TB/s: the table partly from the caches).  The gradient of
+// 16384 x 4096 in bf16 into 32000 rows of fp32, 650 MB, takes 165 us with fresh inputs, 111 to 123 with inputs that the memory's cache holds:
+// the order 9, the stretches 25, the rows 130 (4.7 TB/s; both in one launch 154, with 13 more for the long rows); of 100 x 768 in fp32
+// into 5000 rows, 15 MB, 10.9 us in two dependent launches.
 #include <type_traits>
 
 #include "row_io.h"
