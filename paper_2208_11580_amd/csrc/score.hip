@@ -282,15 +282,18 @@ __global__ __launch_bounds__(NT, NT == 1024 || PIECES <= 512 ? 4 : 3) void score
             }
         }
     block_sums<NT, 2>(s, buf2[0]);
+    // the product base c2 was rounded: all exponents are off by this, and the sums are brought back
+    const float r = fmaf(base, c2, -off);
     {
-        // the product base c2 was rounded: all exponents are off by this, and the sums are brought back
-        const float r = fmaf(base, c2, -off), f = __builtin_amdgcn_exp2f(-r);
+        const float f = __builtin_amdgcn_exp2f(-r);
         s[1] = fmaf(-r, s[0], s[1]) * f;
         s[0] *= f;
     }
-    // Numbers that these short ways do not know (NaN, infinities, and beyond 2^100; bf16: nothing but -inf and what is near the type's
-    // lowest to reach the bound, or a temperature so high that a logit the maxima dropped would not make the sum infinite): once more,
-    // from the caches, for here and below.  Loops over the registers would take some from the usual way.
+    // Numbers that these short ways do not know: once more, from the caches, for here and below.  (Loops over the registers would take some
+    // from the usual way.)  They are NaN, infinities, and a maximum of 2^24 temperatures or more, where r may be no small number: the sums lose
+    // the digits that r takes, and from 126 on the instruction's zero for results below 2^-126 makes f or the largest logit's exponential zero.
+    // bf16: nothing but -inf and what is near the type's lowest to reach the bound, or a temperature so high that a logit the maxima dropped
+    // would not make the sum infinite.
     const int pieces = (n + NT * E - 1) / (NT * E);
     auto all = [&](auto f) {
 #pragma unroll 4
@@ -300,7 +303,7 @@ __global__ __launch_bounds__(NT, NT == 1024 || PIECES <= 512 ? 4 : 3) void score
             f(p, from + (i * NT + tid) * E);
         }
     };
-    const bool known = s[0] < __builtin_inff() && fabsf(off) < 0x1p100f && (TYPE != OBC_BF16 || (c2 > 0x1p-100f && fabsf(base) < 0x1p120f && (KEYS == 0 || bound > -0x1p120f)));
+    const bool known = s[0] < __builtin_inff() && fabsf(r) <= 1.f && (TYPE != OBC_BF16 || (c2 > 0x1p-100f && fabsf(base) < 0x1p120f && (KEYS == 0 || bound > -0x1p120f)));
     if (!known) {
         own = -__builtin_inff();
         all([&](const Piece<TYPE> &p, int) {

@@ -1,0 +1,39 @@
+"""Scores, layer norm and AdamW at the ends of what their arguments may be, against plain implementations in 64 bits."""
+import pytest
+import torch
+
+from .test_gpu_lm_tuning import INF, TYPES, _check_score, _gen, ctx  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------------ scores
+@pytest.mark.parametrize("V", [300, 9000, 40000, 70000])
+@pytest.mark.parametrize("kind,top,tau", [
+    ("f32", 22.499048, 1e-8), ("f32", 14.95, 1e-8), ("f32", 15.4825, 1e-8), ("f32", 15.5675, 1e-8), ("f32", 4757779968.0, 1.0),
+    ("f16", 14.9921875, 1e-8), ("f16", 17.234375, 4.196192726624304e-09), ("bf16", 20.125, 1.2176419872389488e-08)])
+def test_score_of_one_logit_at_a_small_temperature(ctx, kind, top, tau, V):
+    """The largest logit over the temperature is about 2^31, so that its product with the reciprocal is rounded by 2^7: by more than
+    the exponents of fp32 hold."""
+    g = _gen(V)
+    tau = float(torch.tensor(tau))
+    z = (torch.randn(3, V, generator=g, device="cuda") + 0.3 * top).clamp_max(0.9 * top).to(TYPES[kind])
+    for row, at in enumerate((0, V // 2, V - 1)):
+        z[row, at] = top
+    target = torch.tensor([0, 1, -1], dtype=torch.int32, device="cuda")
+    for k in (0, 3):
+        _check_score(ctx.obc_score(z, target, top=k, temperature=tau), z, target, k, tau)
+    ctx.obc_check()
+
+
+@pytest.mark.parametrize("T,V", [(700, 300), (60, 40000)])
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("power", range(18, 46, 3))
+def test_score_at_small_temperatures(ctx, power, kind, T, V):
+    """Largest logits of about 2^power temperatures."""
+    g = _gen(power)
+    z = (10.0 + 10.0 * torch.rand(T, V, generator=g, device="cuda")).to(TYPES[kind])
+    target = torch.randint(-1, V, (T,), generator=g, device="cuda", dtype=torch.int32)
+    tau = float(torch.tensor(15.0 * 2.0 ** -power))
+    _check_score(ctx.obc_score(z, target, top=2, temperature=tau), z, target, 2, tau)
+    ctx.obc_check()
