@@ -158,8 +158,12 @@ __device__ inline int target_of(const Args &a, int64_t row)
     return t;
 }
 
+// Clears the mode's IEEE bit (the ninth): a maximum of a number and a NaN is the number then, whatever NaN it is.  With the bit set, a
+// signalling NaN takes the number's place.
+__device__ inline void drop_nans() { __builtin_amdgcn_s_setreg(1 | 9 << 6, 0); }
+
 // The larger halves of two dwords.  bf16 numbers lie in the order of the half-precision ones of the same bits, up to 2^121; beyond
-// (infinities too) those are NaNs, which this drops.
+// (infinities too) those are NaNs, signalling ones up to 2^125, which this drops after drop_nans().
 __device__ inline unsigned larger_halves(unsigned a, unsigned b)
 {
     unsigned r;
@@ -173,6 +177,7 @@ __global__ __launch_bounds__(NT, NT == 1024 || PIECES <= 512 ? 4 : 3) void score
 {
     constexpr int E = Piece<TYPE>::E, WAVES = NT / 64;
     typedef Order<TYPE> O;
+    if (TYPE == OBC_BF16) drop_nans();
     __shared__ float buf1[WAVES], buf2[2][WAVES][2], buf3[WAVES];
     __shared__ int buf4[WAVES], found, queued;
     __shared__ __align__(16) uintx4 queue[PIECES + 1];
@@ -292,8 +297,8 @@ __global__ __launch_bounds__(NT, NT == 1024 || PIECES <= 512 ? 4 : 3) void score
     // Numbers that these short ways do not know: once more, from the caches, for here and below.  (Loops over the registers would take some
     // from the usual way.)  They are NaN, infinities, and a maximum of 2^24 temperatures or more, where r may be no small number: the sums lose
     // the digits that r takes, and from 126 on the instruction's zero for results below 2^-126 makes f or the largest logit's exponential zero.
-    // bf16: nothing but -inf and what is near the type's lowest to reach the bound, or a temperature so high that a logit the maxima dropped
-    // would not make the sum infinite.
+    // bf16: nothing but -inf and what is near the type's lowest, or no more than that to reach the bound, or a temperature so high that a logit
+    // the maxima dropped would not make the sum infinite.
     const int pieces = (n + NT * E - 1) / (NT * E);
     auto all = [&](auto f) {
 #pragma unroll 4
@@ -303,7 +308,17 @@ __global__ __launch_bounds__(NT, NT == 1024 || PIECES <= 512 ? 4 : 3) void score
             f(p, from + (i * NT + tid) * E);
         }
     };
-    const bool known = s[0] < __builtin_inff() && fabsf(r) <= 1.f && (TYPE != OBC_BF16 || (c2 > 0x1p-100f && fabsf(base) < 0x1p120f && (KEYS == 0 || bound > -0x1p120f)));
+    bool nothing = false;      // bf16: -inf alone, which the maxima do not tell from the type's lowest numbers
+    if (TYPE == OBC_BF16 && top == -__builtin_inff()) {
+        bool other = false;
+#pragma unroll
+        for (int i = 0; i <= CH; ++i)
+            if (i < CH ? i < whole : tail)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) other |= x[i].v[j] != 0xff80ff80u;
+        nothing = block_count<NT>(other, buf4) == 0;
+    }
+    const bool known = s[0] < __builtin_inff() && fabsf(r) <= 1.f && (TYPE != OBC_BF16 || nothing || (c2 > 0x1p-100f && fabsf(top) < 0x1p120f && (KEYS == 0 || bound > -0x1p120f)));
     if (!known) {
         own = -__builtin_inff();
         all([&](const Piece<TYPE> &p, int) {

@@ -37,3 +37,33 @@ def test_score_at_small_temperatures(ctx, power, kind, T, V):
     tau = float(torch.tensor(15.0 * 2.0 ** -power))
     _check_score(ctx.obc_score(z, target, top=2, temperature=tau), z, target, 2, tau)
     ctx.obc_check()
+
+
+@pytest.mark.parametrize("low", [-1e37, -2e37, -1e38, -3e38])
+@pytest.mark.parametrize("T,V,k", [(3, 700, 7), (2, 9000, 20), (600, 40000, 64), (3, 40000, 0)])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_score_of_masks_far_below(ctx, kind, T, V, k, low):
+    """Every other logit masked with a large negative number, at random places."""
+    g = _gen(V)
+    z = 3.0 * torch.randn(T, V, generator=g, device="cuda")
+    z = torch.where(torch.rand(T, V, generator=g, device="cuda") < 0.5, low, z).to(TYPES[kind])
+    target = torch.randint(-1, V, (T,), generator=g, device="cuda", dtype=torch.int32)
+    _check_score(ctx.obc_score(z, target, top=k), z, target, k, 1.0)
+    ctx.obc_check()
+
+
+@pytest.mark.parametrize("V", [8, 700, 40000])
+@pytest.mark.parametrize("k", [0, 4])
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+def test_score_of_rows_of_low_numbers_alone(ctx, kind, k, V):
+    """Rows of large negative numbers, which are no rows of -inf: all equal, one of them above the others, and one alone in each of a
+    piece's places."""
+    for low in (torch.finfo(TYPES[kind]).min, -INF if kind == "f16" else -1e37, -1.0):
+        z = torch.full((10, V), low, device="cuda").to(TYPES[kind])
+        z[1, 1] = low / 2
+        z[2:] = -INF
+        for place in range(8):
+            z[2 + place, place] = low
+        target = torch.tensor([V - 1, 1, 0, 1, 2, 3, 4, 5, -1, 0], dtype=torch.int32, device="cuda")
+        _check_score(ctx.obc_score(z, target, top=k), z, target, k, 1.0)
+    ctx.obc_check()
