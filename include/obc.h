@@ -433,8 +433,8 @@ int obc_embed_grad_workspace_bytes(int T, int V, int d, size_t *bytes);
 int obc_embed_grad(obc_ctx *ctx, const int32_t *ids, int T, const void *dy, int type, int64_t lddy, float scale, int V, int d,
                    int accumulate, void *dtable, int dtable_type, int64_t lddt, void *ws, size_t ws_bytes);
 
-/* A tensor of obc_adamw_plan: n elements each, contiguous.  Inputs and outputs may be the same arrays (the usual case) or others that
- * overlap nothing. */
+/* A tensor of obc_adamw_plan: n elements each, contiguous.  Inputs and outputs may be the same arrays (the usual case) or others.  An
+ * output overlaps no other output and no input, but that it may be, from its first byte to its last, an input of the same tensor. */
 typedef struct obc_adamw_tensor {
     const void *p;                  /* parameters, of `type` */
     void *p_out;
@@ -456,7 +456,7 @@ typedef struct obc_adamw_tensor {
  *   bits        of the moments: 32 or 8
  *   plan        obc_adamw_plan_bytes on the device, aligned to 16 bytes, opaque; written on the context's stream
  *   workgroups  HOST out, for obc_adamw.  (2^24 - 1 at most, of 2048 elements of a tensor each.)
- * Arrays that a step writes may not overlap each other, so that a tensor is listed once. */
+ * Overlaps as said above are refused; gradients may be listed more than once. */
 int obc_adamw_plan_bytes(int count, size_t *bytes);
 int obc_adamw_plan(obc_ctx *ctx, const obc_adamw_tensor *tensors, int count, int type, int bits, void *plan, int64_t *workgroups);
 

@@ -257,14 +257,16 @@ __global__ __launch_bounds__(NT, BITS8 ? 5 : 4) void adamw_kernel(Args a)
             p[j] = fmaf(p[j], keep, -rate * m[j] * __builtin_amdgcn_rcpf(fmaf(root[j], c2, a.eps)));
         }
     }
-    if (left > 0) {
+    if (skip && master) {      // the parameters as they were, which need not be the copies rounded (read before the copies are written)
+        if (left > 0) {
+            float old[8];
+            load8<TYPE>(t.p, at, left, old);
+            put8<OBC_F32>(t.master_out, at, left, p, past);
+            put8<TYPE>(t.p_out, at, left, old, past);
+        }
+    } else if (left > 0) {
         if (master) put8<OBC_F32>(t.master_out, at, left, p, past);
-        if (!(skip && master)) put8<TYPE>(t.p_out, at, left, p, past);
-    }
-    if (skip && master && left > 0) {      // the parameters as they were, which need not be the copies rounded
-        float old[8];
-        load8<TYPE>(t.p, at, left, old);
-        put8<TYPE>(t.p_out, at, left, old, past);
+        put8<TYPE>(t.p_out, at, left, p, past);
     }
     if (!BITS8) {
         if (left > 0) {
@@ -362,16 +364,21 @@ void launch(obc_ctx *ctx, const Args &a, unsigned blocks, bool bits8)
 // Memory that a step writes, for the check that no two arrays share any
 struct Span {
     uintptr_t from, to;
+    int tensor;
 };
-inline void put_span(Span *spans, int64_t &n, const void *p, int64_t bytes)
+inline void put_span(Span *spans, int64_t &n, int tensor, const void *p, int64_t bytes)
 {
-    if (p && bytes > 0) spans[n++] = Span{(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes};
+    if (p && bytes > 0) spans[n++] = Span{(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, tensor};
 }
-// An output is its input, or apart from it.
-inline bool apart(const void *in, const void *out, int64_t bytes)
+// Whether an input is apart from all outputs (sorted, apart from each other), or is one of its own tensor's, element for element: a thread reads
+// all inputs of its elements before it writes any.  `out`: its own output, if it has one.
+inline bool apart(const Span *spans, int64_t n, int tensor, const void *in, const void *out, int64_t bytes)
 {
-    const uintptr_t a = (uintptr_t)in, b = (uintptr_t)out;
-    return a == b || a + (uintptr_t)bytes <= b || b + (uintptr_t)bytes <= a;
+    if (!in || bytes == 0 || in == out) return true;
+    const uintptr_t from = (uintptr_t)in, to = from + (uintptr_t)bytes;
+    for (const Span *s = std::lower_bound(spans, spans + n, from, [](const Span &x, uintptr_t f) { return x.to <= f; }); s < spans + n && s->from < to; ++s)
+        if (s->tensor != tensor || s->from != from || s->to != to) return false;
+    return true;
 }
 
 }  // namespace
@@ -414,27 +421,39 @@ int obc_adamw_plan(obc_ctx *ctx, const obc_adamw_tensor *tensors, int count, int
     Span *const spans = new (std::nothrow) Span[(size_t)count * 6 + 1];
     if (!spans) return obc_fail(ctx, OBC_ERR_HIP, "obc_adamw_plan: no host memory");
     int64_t written = 0;
-    int whole = -1;
+    const auto sizes = [&](const obc_adamw_tensor &t, int64_t &p, int64_t &m, int64_t &s) {
+        p = t.n * (int64_t)size_of_type(type);
+        m = t.n * (bits / 8);
+        s = bits == 8 ? (t.n + kScaled - 1) / kScaled * 4 : 0;
+    };
+    int64_t p, m, s;
     for (int i = 0; i < count; ++i) {
         const obc_adamw_tensor &t = tensors[i];
         if (t.n == 0) continue;
-        const int64_t p = t.n * (int64_t)size_of_type(type), m = t.n * (bits / 8), s = bits == 8 ? (t.n + kScaled - 1) / kScaled * 4 : 0;
-        if (!apart(t.p, t.p_out, p) || !apart(t.m, t.m_out, m) || !apart(t.v, t.v_out, m) || !apart(t.master, t.master_out, 4 * t.n) ||
-            !apart(t.m_scale, t.m_scale_out, s) || !apart(t.v_scale, t.v_scale_out, s))
-            whole = i;
-        put_span(spans, written, t.p_out, p);
-        put_span(spans, written, t.m_out, m);
-        put_span(spans, written, t.v_out, m);
-        put_span(spans, written, t.master_out, 4 * t.n);
-        put_span(spans, written, t.m_scale_out, s);
-        put_span(spans, written, t.v_scale_out, s);
+        sizes(t, p, m, s);
+        put_span(spans, written, i, t.p_out, p);
+        put_span(spans, written, i, t.m_out, m);
+        put_span(spans, written, i, t.v_out, m);
+        put_span(spans, written, i, t.master_out, 4 * t.n);
+        put_span(spans, written, i, t.m_scale_out, s);
+        put_span(spans, written, i, t.v_scale_out, s);
     }
     std::sort(spans, spans + written, [](const Span &a, const Span &b) { return a.from < b.from; });
     bool shared = false;
     for (int64_t i = 1; i < written; ++i) shared |= spans[i].from < spans[i - 1].to;
+    int over = -1;
+    for (int i = 0; i < count && !shared && over < 0; ++i) {
+        const obc_adamw_tensor &t = tensors[i];
+        if (t.n == 0) continue;
+        sizes(t, p, m, s);
+        const auto clear = [&](const void *in, const void *out, int64_t bytes) { return apart(spans, written, i, in, out, bytes); };
+        if (!clear(t.p, t.p_out, p) || !clear(t.g, nullptr, p) || !clear(t.m, t.m_out, m) || !clear(t.v, t.v_out, m) ||
+            !clear(t.master, t.master_out, 4 * t.n) || !clear(t.m_scale, t.m_scale_out, s) || !clear(t.v_scale, t.v_scale_out, s))
+            over = i;
+    }
     delete[] spans;
-    if (whole >= 0) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw_plan: tensor %d: an output overlaps its input", whole);
     if (shared) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw_plan: two outputs overlap (is a tensor listed twice?)");
+    if (over >= 0) return obc_fail(ctx, OBC_ERR_BAD_ARG, "obc_adamw_plan: tensor %d: an input overlaps an output that is not these elements", over);
     *workgroups = blocks;
     unsigned first = 0;
     for (int i = 0; i < count; i += kWritten) {

@@ -67,3 +67,47 @@ def test_score_of_rows_of_low_numbers_alone(ctx, kind, k, V):
         target = torch.tensor([V - 1, 1, 0, 1, 2, 3, 4, 5, -1, 0], dtype=torch.int32, device="cuda")
         _check_score(ctx.obc_score(z, target, top=k), z, target, k, 1.0)
     ctx.obc_check()
+
+
+# ------------------------------------------------------------------------------------------------ AdamW
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("master", [True, False])
+def test_adamw_outputs_in_the_place_of_inputs(ctx, bits, master):
+    """Results in the place of the tensor's gradient or of another of its inputs, a gradient that two tensors share: as apart.  What
+    another tensor's step reads is refused."""
+    import paper_2208_11580_amd as pkg
+
+    g = _gen(bits)
+    n = 5000
+
+    def copied(st):
+        return pkg.AdamState(*[None if t is None else t.clone() for t in st])
+
+    p = torch.randn(n, generator=g, device="cuda")
+    grad = torch.randn(n, generator=g, device="cuda")
+    st = ctx.obc_adamw_state(p, bits=bits, master=master)
+    for step in (1, 2):
+        ctx.obc_adamw(ctx.obc_adamw_plan([p], [grad], [st]), step, 1e-2, seed=3)
+    if master:
+        st.master.add_(1e-3)      # (not the parameters' own values)
+    for scale in (0.5, INF):      # (inf: all stays as it was)
+        gs = torch.full((1,), scale, device="cuda")
+        want_p, want = ctx.obc_adamw(ctx.obc_adamw_plan([p], [grad], [st], out=([torch.zeros_like(p)], [pkg.AdamState(
+            *[None if t is None else torch.zeros_like(t) for t in st])])), 3, 1e-2, grad_scale=gs, seed=3)
+        q, gr, su = p.clone(), grad.clone(), copied(st)
+        ctx.obc_adamw(ctx.obc_adamw_plan([q], [gr], [su], out=([gr], [su])), 3, 1e-2, grad_scale=gs, seed=3)
+        assert torch.equal(gr, want_p[0]) and torch.equal(q, p)
+        assert all(a is None or torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(su, want[0]))
+        if master:      # copies and parameters change places
+            q, su = p.clone(), copied(st)
+            new = su._replace(master=q)
+            ctx.obc_adamw(ctx.obc_adamw_plan([q], [grad], [su], out=([su.master], [new])), 3, 1e-2, grad_scale=gs, seed=3)
+            assert torch.equal(su.master, want_p[0]) and torch.equal(q, want[0].master)
+    q, su = p.clone(), copied(st)
+    with pytest.raises(pkg.ObcError):
+        ctx.obc_adamw_plan([p, q], [grad, grad], [st, su], out=([q, p], [st, su]))
+    with pytest.raises(pkg.ObcError):
+        ctx.obc_adamw_plan([p, q], [q, grad], [st, su])
+    with pytest.raises(pkg.ObcError):
+        ctx.obc_adamw_plan([p[:n - 1]], [p[1:]], [ctx.obc_adamw_state(p[1:], bits=bits)])
+    ctx.obc_check()
