@@ -1,8 +1,9 @@
 // obc_layernorm and obc_layernorm_grad: layer norm with the residual's addition, an output in 8 bits, and the backward pass.
 //
 //   mean = sum h / d, var = sum (h - mean)^2 / d, y = (h - mean) rstd gain + bias
-// A row is read once and kept in registers: the mean first, then the squares of what is left, so that a large mean costs the
-// variance no digits; 8 bits take a third reduction, the largest |y|.
+// A row is read once and kept in registers: the mean first, then what is left, c = h - mean, and its squares.  The mean is rounded, which would move
+// all of y alike, so c is summed beside its squares: with e = sum c / d, the mean is off by e, y = (c - e) rstd gain + bias and
+// var = sum c^2 / d - e^2.  A large mean so costs no digits of either.  8 bits take a third reduction, the largest |y|.
 //
 // Memory-bound: 4096 x 8192 in bf16 with residual and sum, 268 MB, takes 52 us with fresh inputs (5.2 TB/s; a large copy reaches 5.2), one row of
 // 768 2.6 us, of which an empty launch is 2.  The backward pass keeps each workgroup's shares of the gain's and the bias's gradient in registers
@@ -60,7 +61,7 @@ struct NormArgs {
 template <int TYPE, bool Q8, int NT, int CH>
 __global__ __launch_bounds__(NT) void layernorm_kernel(NormArgs a)
 {
-    __shared__ float buf[3][NT / 64][1];
+    __shared__ float buf1[NT / 64][1], buf2[NT / 64][2], buf3[NT / 64];
     const int64_t row = blockIdx.x, base = row * a.d;
     float v[CH][8];
     float sum[1] = {0.f};
@@ -79,9 +80,9 @@ __global__ __launch_bounds__(NT) void layernorm_kernel(NormArgs a)
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[0] += v[k][j];      // (zeros beyond the row's end)
     }
-    sums<NT>(sum, buf[0]);
+    sums<NT>(sum, buf1);
     const float mean = sum[0] / (float)a.d;
-    float sq[1] = {0.f};
+    float sq[2] = {0.f, 0.f};      // of c^2, of c
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
         const int left = a.d - (k * NT + (int)threadIdx.x) * 8;
@@ -90,12 +91,16 @@ __global__ __launch_bounds__(NT) void layernorm_kernel(NormArgs a)
         for (int j = 0; j < 8; ++j) {
             v[k][j] = j < left ? v[k][j] - mean : 0.f;
             sq[0] = fmaf(v[k][j], v[k][j], sq[0]);
+            sq[1] += v[k][j];
         }
     }
-    sums<NT>(sq, buf[1]);
-    const float rstd = 1.f / sqrtf(sq[0] / (float)a.d + a.eps);
+    sums<NT>(sq, buf2);
+    const float off = sq[1] / (float)a.d;
+    float var = fmaf(-off, off, sq[0] / (float)a.d);
+    var = var < 0.f ? 0.f : var;      // (rows of one value; a NaN stays one)
+    const float rstd = 1.f / sqrtf(var + a.eps);
     if (threadIdx.x == 0) {
-        if (a.mean) a.mean[row] = mean;
+        if (a.mean) a.mean[row] = mean + off;
         if (a.rstd) a.rstd[row] = rstd;
     }
     float top = 0.f;
@@ -108,13 +113,13 @@ __global__ __launch_bounds__(NT) void layernorm_kernel(NormArgs a)
         if (a.bias) load8<OBC_F32>(a.bias, c, left, b);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            v[k][j] = fmaf(v[k][j] * rstd, g[j], a.bias ? b[j] : 0.f);
+            v[k][j] = fmaf((v[k][j] - off) * rstd, g[j], a.bias ? b[j] : 0.f);
             if (Q8) top = larger(top, v[k][j]);
         }
         if (!Q8) put8<TYPE>(a.y, base + c, left, v[k], a.past);
     }
     if (!Q8) return;
-    top = largest<NT>(top, &buf[2][0][0]);
+    top = largest<NT>(top, buf3);
     // A row whose largest value is next to nothing is scaled up first, so that its reciprocal stays finite.
     const bool lost = !(sq[0] < __builtin_inff()) || !(top < __builtin_inff());
     const float up = top < 1e-30f ? 0x1p90f : 1.f, mul = top > 0.f ? 127.f / (top * up) : 0.f;

@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from .test_gpu_lm_tuning import INF, TYPES, _check_score, _gen, ctx  # noqa: F401
+from .test_gpu_lm_tuning import INF, ROUND, TINY, TYPES, U32, _check_score, _gen, _norm_reference, _within, ctx  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -66,6 +66,49 @@ def test_score_of_rows_of_low_numbers_alone(ctx, kind, k, V):
             z[2 + place, place] = low
         target = torch.tensor([V - 1, 1, 0, 1, 2, 3, 4, 5, -1, 0], dtype=torch.int32, device="cuda")
         _check_score(ctx.obc_score(z, target, top=k), z, target, k, 1.0)
+    ctx.obc_check()
+
+
+# ------------------------------------------------------------------------------------------------ layer norm
+@pytest.mark.parametrize("mean", [3000.0, -30000.0])
+@pytest.mark.parametrize("kind", ["f32", "f16"])
+@pytest.mark.parametrize("T,d", [(4, 1000), (3, 4099), (520, 8192), (2, 16384), (2, 40001)])
+def test_layernorm_of_a_large_mean(ctx, T, d, kind, mean):
+    """Values a few units about a mean of thousands of them.  With n = 90 roundings in a sum the first mean is off by
+    D = n 2^-24 |mean| at most, and its correction by n roundings of the deviations' size; nothing else depends on the mean."""
+    g = _gen(d)
+    x = (mean + 30.0 * torch.randn(T, d, generator=g, device="cuda")).to(TYPES[kind])
+    gain, bias = 1.0 + 0.3 * torch.randn(d, generator=g, device="cuda"), 0.5 * torch.randn(d, generator=g, device="cuda")
+    got = ctx.obc_layernorm(x, gain, bias, want_stats=True)
+    _, m, rstd, y, dm, _, _ = _norm_reference(x, None, gain, bias, 1e-5)
+    n, c = 90, (x.double() - m[:, None]).abs()
+    D = dm[:, None]
+    size = c.mean(1, keepdim=True) + D                                          # of c as the kernel has it
+    e = (n + 3) * U32 * size                                                    # the correction: n roundings, each term's, the quotient's
+    _within(got["mean"], m, U32 * m.abs() + e[:, 0])
+    # c - e: a rounding of c, one of the difference, and e's; the variance's relative error, half of it rstd's: n roundings of its terms, 4 of the
+    # terms' factors and the quotient, over a sum that is larger by D^2
+    r = 0.5 * (n + 6) * U32 * (1 + (D * rstd[:, None]) ** 2) + 3 * U32
+    _within(got["rstd"], rstd, (r[:, 0] + U32) * rstd)
+    bound = gain.double().abs() * rstd[:, None] * (2 * U32 * (c + D) + e + c * (r + 2 * U32)) + U32 * (y.abs() + bias.double().abs())
+    _within(got["y"], y, bound + ROUND[kind] * 1.01 * y.abs() + TINY[kind])
+    ctx.obc_check()
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+def test_layernorm_of_constant_rows(ctx, kind):
+    """The variance is zero, not a little less: y is the bias, and no number is lost at an eps of nearly nothing either."""
+    g = _gen(5)
+    for d in (3, 1000, 4097, 20000):
+        x = (torch.rand(50, 1, generator=g, device="cuda") * 1000).to(TYPES[kind]).expand(50, d).contiguous()
+        gain, bias = torch.rand(d, generator=g, device="cuda"), torch.rand(d, generator=g, device="cuda")
+        got = ctx.obc_layernorm(x, gain, bias, eps=1e-30, want_stats=True)
+        assert torch.isfinite(got["rstd"]).all() and torch.isfinite(got["y"]).all()
+        got = ctx.obc_layernorm(x, gain, bias, eps=1e-5, want_stats=True)
+        # c is one number for all, within 90 roundings of x; its mean is off by as many of it
+        rest = (90 * U32) ** 2 * 1.1 * x.double().abs() * 1e5 ** 0.5
+        _within(got["y"], bias.double().expand(50, d), gain.double() * rest + 2 * U32 + ROUND[kind] * 1.01 * (bias.double() + rest) + TINY[kind])
+        _within(got["mean"], x[:, 0].double(), (U32 + 1.1 * (90 * U32) ** 2) * x[:, 0].double())
     ctx.obc_check()
 
 
