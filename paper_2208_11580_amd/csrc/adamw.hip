@@ -72,6 +72,7 @@ __device__ inline double one_minus_power(double b, int64_t t)
 }
 
 constexpr unsigned kClose = 6;
+constexpr float kSmall = 0x1p-100f;      // of v: its root is taken in another range
 
 // 32 bits from an element's place: odd multipliers (of the fractions of the golden ratio, the root of 2, and pi) and shifts
 __device__ inline unsigned mix(unsigned h)
@@ -253,9 +254,32 @@ __global__ __launch_bounds__(NT, BITS8 ? 5 : 4) void adamw_kernel(Args a)
             } else {
                 v[j] = fmaf(v[j], b2, x * x);
             }
-            root[j] = __builtin_amdgcn_sqrtf(v[j]);      // (to a unit in the last place)
-            p[j] = fmaf(p[j], keep, -rate * m[j] * __builtin_amdgcn_rcpf(fmaf(root[j], c2, a.eps)));
         }
+        if (BITS8) {
+            // Roots down to fp32's least, though their squares are none of its numbers from about 1e-19 on: such ones (zeros too) are formed
+            // from squares that are larger by 2^128, which their wave alone pays for.
+            float least = v[0];
+#pragma unroll
+            for (int j = 1; j < 8; ++j) least = fminf(least, v[j]);
+            if (__any(least < kSmall)) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float x = g[j] * gv * 0x1p64f, old = root[j] * 0x1p64f;
+                    root[j] = v[j] < kSmall ? __builtin_amdgcn_sqrtf(fmaf(old, old, x * x)) * 0x1p-64f : __builtin_amdgcn_sqrtf(v[j]);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) root[j] = __builtin_amdgcn_sqrtf(v[j]);      // (to a unit in the last place)
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {      // (the instruction takes a v below 2^-126 for zero)
+                const bool small = v[j] < kSmall;
+                root[j] = __builtin_amdgcn_sqrtf(small ? v[j] * 0x1p64f : v[j]) * (small ? 0x1p-32f : 1.f);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p[j] = fmaf(p[j], keep, -rate * m[j] * __builtin_amdgcn_rcpf(fmaf(root[j], c2, a.eps)));
     }
     if (skip && master) {      // the parameters as they were, which need not be the copies rounded (read before the copies are written)
         if (left > 0) {

@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from .test_gpu_lm_tuning import INF, ROUND, TINY, TYPES, U32, _check_score, _gen, _norm_reference, _within, ctx  # noqa: F401
+from .test_gpu_lm_tuning import B1, B2, INF, LR, ROUND, TINY, TYPES, U32, _blocks, _check_score, _gen, _norm_reference, _values, _within, ctx  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -153,4 +153,60 @@ def test_adamw_outputs_in_the_place_of_inputs(ctx, bits, master):
         ctx.obc_adamw_plan([p, q], [q, grad], [st, su])
     with pytest.raises(pkg.ObcError):
         ctx.obc_adamw_plan([p[:n - 1]], [p[1:]], [ctx.obc_adamw_state(p[1:], bits=bits)])
+    ctx.obc_check()
+
+
+@pytest.mark.parametrize("n", [300, 5000])
+def test_adamw_of_small_gradients(ctx, n):
+    """Moments in 32 bits whose v is below fp32's smallest normal number, and an eps below their roots."""
+    g, eps = _gen(n), 2.0 ** -110
+    grad = 10.0 ** (-21.0 + 4.0 * torch.rand(n, generator=g, device="cuda"))
+    grad = torch.where(torch.rand(n, generator=g, device="cuda") < 0.5, grad, -grad)
+    grad[::9] = 0.0
+    p = torch.zeros(n, device="cuda")
+    st = ctx.obc_adamw_state(p)
+    m, v = (torch.zeros(n, dtype=torch.float64, device="cuda") for _ in range(2))
+    for step in (1, 2, 3):
+        p.zero_()
+        old_m, old_v = st.m.double(), st.v.double()
+        ctx.obc_adamw(ctx.obc_adamw_plan([p], [grad], [st], decay=0.0), step, LR, B1, B2, eps)
+        m, v = B1 * old_m + (1 - B1) * grad.double(), B2 * old_v + (1 - B2) * grad.double() ** 2
+        _within(st.m, m, 6 * U32 * m.abs())
+        # v: its terms' roundings, and those of the square and of the sum among numbers that lie 2^-149 apart
+        dv = 8 * U32 * v + 2.0 ** -149
+        _within(st.v, v, dv)
+        c1, c2 = 1 / (1 - B1 ** step), (1 - B2 ** step) ** -0.5
+        most, least = (LR * c1 * m.abs() / ((w.clamp_min(0.0)).sqrt() * c2 + eps) for w in (v - dv, v + dv))
+        assert (p.double().abs() <= most * (1 + 24 * U32)).all() and (p.double().abs() >= least * (1 - 24 * U32)).all()
+        assert (torch.sign(p) == -torch.sign(grad)).all()
+    ctx.obc_check()
+
+
+@pytest.mark.parametrize("size", [1e-17, 1e-19, 1e-20, 1e-22, 1e-25, 1e-28])
+@pytest.mark.parametrize("n", [300, 5000])
+def test_adamw_of_8_bit_moments_of_small_gradients(ctx, n, size):
+    """Roots of v down to the smallest that a block may have, and an eps below them, among blocks of ordinary ones: m over the root is what
+    a step moves by, and a root that is not zero does not become zero."""
+    g, eps = _gen(n), 2.0 ** -115
+    grad = size * torch.randn(n, generator=g, device="cuda") * torch.randn(n, generator=g, device="cuda").exp()
+    grad[100:200] = 0.0
+    grad[256:290] = torch.randn(34, generator=g, device="cuda")
+    p = torch.zeros(n, device="cuda")
+    st = ctx.obc_adamw_state(p, bits=8)
+    for step in (1, 2, 3):
+        p.zero_()
+        m, v = _values(st.m, st.m_scale), _values(st.v, st.v_scale) ** 2
+        ctx.obc_adamw(ctx.obc_adamw_plan([p], [grad], [st], decay=0.0), step, LR, B1, B2, eps, seed=2)
+        em = 6 * U32 * (B1 * m.abs() + (1 - B1) * grad.double().abs())
+        m, v = B1 * m + (1 - B1) * grad.double(), B2 * v + (1 - B2) * grad.double() ** 2
+        c1, c2 = 1 / (1 - B1 ** step), (1 - B2 ** step) ** -0.5
+        want = LR * c1 * m / (v.sqrt() * c2 + eps)
+        _within(p, -want, 32 * U32 * want.abs() + LR * c1 * em / (v.sqrt() * c2 + eps))
+        for got, scale, x, e in ((st.m, st.m_scale, m, em), (st.v, st.v_scale, v.sqrt(), 8 * U32 * v.sqrt())):
+            top = _blocks(x.abs()).amax(1)
+            _within(scale, top / 448, _blocks(e).amax(1) / 448 + 2 * U32 * top / 448)
+            s = scale.double().repeat_interleave(256)[:n]
+            # up or down: less than a step, an eighth or 2^-9 of the scale
+            assert ((_values(got, scale) - x).abs() <= torch.maximum(x.abs() / 8, 2.0 ** -9 * s) * (1 + 1e-5) + e).all()
+        assert ((st.v.float() > 0) == (v > 0)).all()
     ctx.obc_check()
