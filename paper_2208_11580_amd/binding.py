@@ -229,7 +229,8 @@ def _no_grad(*tensors):
 
 class AdamPlan:
     """The tensors of obc_adamw, which it keeps, laid out by obc_adamw_plan for the context's stream.  (Their addresses: a tensor that is
-    given other memory needs another plan.  A captured graph needs its plans as long as it is replayed.)"""
+    given other memory needs another plan.  A captured graph needs its plans as long as it is replayed.)  Memory of tensors that go after
+    the plan, or other gradients, took their place is not handed out before the steps queued until then are done."""
 
     def __init__(self, ctx, params, grads, states, decay=0.01, out=None):
         params, states = list(params), list(states)
@@ -248,6 +249,7 @@ class AdamPlan:
         for i in range(count):
             d, p, st, new = self.tensors[i], params[i], states[i], self.new[1][i]
             ctx._take(p, self.new[0][i], *st, *new)
+            self._hold(p, self.new[0][i], *st, *new)
             n = d.n = p.numel()
             d.decay = float(decays[i])
             d.p, d.p_out = self._at(i, p, params[0].dtype, n), self._at(i, self.new[0][i], params[0].dtype, n)
@@ -263,6 +265,12 @@ class AdamPlan:
         self.data = ctx._empty((max(need.value, 16),), torch.uint8, ctx.stream.device)
         self.address = self.data.data_ptr()
         self.use(grads)
+
+    def _hold(self, *tensors):
+        # steps are queued on the context's stream, which need not be the one that a tensor was allocated on
+        for t in tensors:
+            if t is not None:
+                t.record_stream(self.ctx.stream)
 
     @staticmethod
     def _at(i, t, dtype, n):
@@ -280,6 +288,7 @@ class AdamPlan:
             raise ValueError("there must be as many gradients as parameters")
         addresses = [self._at(i, g, self.params[0].dtype, self.params[i].numel()) for i, g in enumerate(grads)]
         self.ctx._take(*grads)
+        self._hold(*grads)
         for t, g in zip(self.tensors, addresses):
             t.g = g
         n = c_int64()
