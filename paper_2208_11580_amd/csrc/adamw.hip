@@ -7,8 +7,8 @@
 // stay where it is, since a step changes it by a thousandth and the nearest 8-bit numbers are an eighth away.  A root that is not
 // zero does not become zero, or the next step would be divided by next to nothing.
 //
-// Memory-bound: 52 million parameters in bf16 with fp32 copies and 8-bit moments, 835 MB, take 156 to 175 us (5.0 TB/s), 26 million in fp32
-// with fp32 moments, 728 MB, 133 us (5.5 TB/s); 50 tensors of 768 values 3.7 us.  With 8 bits the vector instructions, some 80 to a
+// Memory-bound: 52 million parameters in bf16 with fp32 copies and 8-bit moments, 835 MB, take 152 to 174 us (4.8 to 5.5 TB/s), 26 million in fp32
+// with fp32 moments, 728 MB, 132 us (5.5 TB/s); 50 tensors of 768 values 3.9 us.  With 8 bits the vector instructions, some 80 to a
 // parameter, are busy for most of that time.
 #include <algorithm>
 
@@ -71,7 +71,7 @@ __device__ inline double one_minus_power(double b, int64_t t)
     return 1.0 - r;
 }
 
-constexpr unsigned kClose = 6;
+constexpr unsigned kClose = 6;      // units of a float's last place
 constexpr float kSmall = 0x1p-100f;      // of v: its root is taken in another range
 
 // 32 bits from an element's place: odd multipliers (of the fractions of the golden ratio, the root of 2, and pi) and shifts
@@ -326,7 +326,8 @@ __global__ __launch_bounds__(NT, BITS8 ? 5 : 4) void adamw_kernel(Args a)
         }
         // Where a number lies so near to where the dither turns that fp32's roundings would decide (moments are off by a few halves
         // of their last place, mostly), the wave, one in eighty, does it all again in 64 bits: results are those of the
-        // formula, not of an order of roundings.
+        // formula, not of an order of roundings.  (Not so a new m far smaller than its two terms, whose roundings are more of its last places than
+        // that: a few of 16 million codes, small ones: 5e-8 of the norm of m.)
         if (__any(edge < 2 * kClose)) {
             // (one element after the other, the first of arrays that turn: in a loop that is not unrolled, so that the usual way needs no
             // registers for this one -- 119 with eight at once, at which a step of 64 million took 210 us instead of 165)

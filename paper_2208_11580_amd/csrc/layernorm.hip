@@ -6,7 +6,7 @@
 // var = sum c^2 / d - e^2.  A large mean so costs no digits of either.  8 bits take a third reduction, the largest |y|.
 //
 // Memory-bound: 4096 x 8192 in bf16 with residual and sum, 268 MB, takes 52 us with fresh inputs (5.2 TB/s; a large copy reaches 5.2), one row of
-// 768 2.6 us, of which an empty launch is 2.  The backward pass keeps each workgroup's shares of the gain's and the bias's gradient in registers
+// 768 2.8 us in a graph, of which an empty launch is 2.  The backward pass keeps each workgroup's shares of the gain's and the bias's gradient in registers
 // over its rows: 4096 x 4096 in bf16 with the residual's gradient, 134 MB, takes 29 to 37 us (fresh inputs), 24 to 31 of them the
 // rows and 5 the sum of 512 shares.
 #include "row_io.h"

@@ -8,9 +8,9 @@
 // reach it (equal logits, mostly), the k-th largest is found exactly, by bisection, and equal ones are taken in their order.  Rows
 // of several parts are joined by a second kernel.
 //
-// Bound by vector issue, with memory close behind: 2048 x 131072 in bf16 with 64 alternatives, 537 MB, takes 123 us a call (4.4 TB/s; plain reads
-// reach 6.0), 117 of them the parts (1640 instructions a wave, half of them for the two sums; vector units active 72 % of the time) and 9
-// the join.  One row of 32000 in fp32 with 20 alternatives takes 8.2 us in one launch, 5 without alternatives.  Workgroups that stay and load the
+// Bound by vector issue, with memory close behind: 2048 x 131072 in bf16 with 64 alternatives, 537 MB, takes 125 us a call (4.3 TB/s; plain reads
+// reach 6.0).  Traced one by one the parts take 122 (1645 instructions a wave, half of them for the two sums; vector units active three quarters of the
+// time) and the join 10; half of each row at -inf 128 a call.  One row of 32000 in fp32 with 20 alternatives takes 8.2 us in one launch, 5 without alternatives.  Workgroups that stay and load the
 // next part as they sum this one took 154 us.
 #include <type_traits>
 
