@@ -470,8 +470,8 @@ int obc_adamw_plan(obc_ctx *ctx, const obc_adamw_tensor *tensors, int count, int
  *   grad_scale  device, nullable (1): a loss scale's reciprocal or a clipping factor.  Infinite or NaN: all values stay as they are.
  * Moments of 8 bits: m and sqrt(v) are divided by their block's scale, its largest magnitude / 448, and rounded up or down with the
  * chances that keep them on average, by a hash of seed, step, the tensor's place in the list and the element's in the tensor (in 64
- * bits where fp32 is within 6 units of its last place of deciding otherwise); sqrt(v) > 0 is never rounded to 0.  A block whose largest is below 1e-30 becomes zeros.  A
- * block with a NaN or an infinity gets scale NaN.
+ * bits where fp32 is within 6 units of its last place of deciding otherwise); sqrt(v) > 0 is never rounded to 0.  A block whose
+ * largest is below 1e-30 becomes zeros.  A block with a NaN or an infinity gets scale NaN.
  * 0 <= beta < 1, eps >= 2^-120.  (Moments of 32 bits: a v that fp32's least number, 2^-149, does not reach is zero.)  Results do not depend on
  * how tensors are listed, but for the hash. */
 int obc_adamw(obc_ctx *ctx, const void *plan, int count, int64_t workgroups, int type, int bits, int64_t step, const int64_t *step_at,

@@ -229,8 +229,8 @@ def _no_grad(*tensors):
 
 class AdamPlan:
     """The tensors of obc_adamw, which it keeps, laid out by obc_adamw_plan for the context's stream.  (Their addresses: a tensor that is
-    given other memory needs another plan.  A captured graph needs its plans as long as it is replayed.)  Memory of tensors that go after
-    the plan, or other gradients, took their place is not handed out before the steps queued until then are done."""
+    given other memory needs another plan.  A captured graph needs its plans as long as it is replayed.)  The memory of its
+    tensors is not handed out for anything else before the steps that are queued when they go are done."""
 
     def __init__(self, ctx, params, grads, states, decay=0.01, out=None):
         params, states = list(params), list(states)

@@ -9,9 +9,9 @@
 // of several parts are joined by a second kernel.
 //
 // Bound by vector issue, with memory close behind: 2048 x 131072 in bf16 with 64 alternatives, 537 MB, takes 125 us a call (4.3 TB/s; plain reads
-// reach 6.0).  Traced one by one the parts take 122 (1645 instructions a wave, half of them for the two sums; vector units active three quarters of the
-// time) and the join 10; half of each row at -inf 128 a call.  One row of 32000 in fp32 with 20 alternatives takes 8.2 us in one launch, 5 without alternatives.  Workgroups that stay and load the
-// next part as they sum this one took 154 us.
+// reach 6.0).  Traced one by one the parts take 122 (1645 instructions a wave, half of them for the two sums; vector units active three
+// quarters of the time) and the join 10; with half of each row at -inf a call takes 128.  One row of 32000 in fp32 with 20 alternatives takes 8.2 us
+// in one launch, 5 without alternatives.  Workgroups that stay and load the next part as they sum this one took 154 us.
 #include <type_traits>
 
 #include "row_io.h"
@@ -294,11 +294,11 @@ __global__ __launch_bounds__(NT, NT == 1024 || PIECES <= 512 ? 4 : 3) void score
         s[1] = fmaf(-r, s[0], s[1]) * f;
         s[0] *= f;
     }
-    // Numbers that these short ways do not know: once more, from the caches, for here and below.  (Loops over the registers would take some
-    // from the usual way.)  They are NaN, infinities, and a maximum of 2^24 temperatures or more, where r may be no small number: the sums lose
-    // the digits that r takes, and from 126 on the instruction's zero for results below 2^-126 makes f or the largest logit's exponential zero.
-    // bf16: nothing but -inf and what is near the type's lowest, or no more than that to reach the bound, or a temperature so high that a logit
-    // the maxima dropped would not make the sum infinite.
+    // Numbers that these short ways do not know: once more, from the caches.  (Loops over the registers would take some from the usual way.)
+    //  - The sums of NaN and infinities, and of a maximum of 2^24 temperatures or more, where r may be no small number: they lose the digits
+    //    that r takes, and from 126 on the instruction's zero for results below 2^-126 makes f or the largest logit's exponential zero.
+    //  - In bf16 the maximum, where it is none of the numbers in order, or one that the maxima dropped need not have made the sum infinite, at high
+    //    temperatures; and the largest, where no more than the type's lowest may reach the bound.
     const int pieces = (n + NT * E - 1) / (NT * E);
     auto all = [&](auto f) {
 #pragma unroll 4
@@ -318,20 +318,26 @@ __global__ __launch_bounds__(NT, NT == 1024 || PIECES <= 512 ? 4 : 3) void score
                 for (int j = 0; j < 4; ++j) other |= x[i].v[j] != 0xff80ff80u;
         nothing = block_count<NT>(other, buf4) == 0;
     }
-    const bool known = s[0] < __builtin_inff() && fabsf(r) <= 1.f && (TYPE != OBC_BF16 || nothing || (c2 > 0x1p-100f && fabsf(top) < 0x1p120f && (KEYS == 0 || bound > -0x1p120f)));
-    if (!known) {
-        own = -__builtin_inff();
-        all([&](const Piece<TYPE> &p, int) {
+    // whether the maximum is right, the bound too, and the sums
+    const bool sure = TYPE != OBC_BF16 ? top < __builtin_inff() : nothing || (s[0] < __builtin_inff() && c2 > 0x1p-100f && fabsf(top) < 0x1p120f);
+    bool ranked = sure && (TYPE != OBC_BF16 || KEYS == 0 || nothing || bound > -0x1p120f);
+    if (!sure || !(s[0] < __builtin_inff()) || !(fabsf(r) <= 1.f)) {
+        if (!sure) {
+            const float quick = top;
+            own = -__builtin_inff();
+            all([&](const Piece<TYPE> &p, int) {
 #pragma unroll
-            for (int j = 0; j < E; ++j) own = fmaxf(own, element(p, j));
-        });
-        own = join_lanes(own, fmaxf_of);
-        if (lane == 0) buf1[wave] = own;
-        __syncthreads();
-        top = buf1[0];
+                for (int j = 0; j < E; ++j) own = fmaxf(own, element(p, j));
+            });
+            own = join_lanes(own, fmaxf_of);
+            if (lane == 0) buf1[wave] = own;
+            __syncthreads();
+            top = buf1[0];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) top = fmaxf(top, buf1[w]);
-        base = top == -__builtin_inff() ? 0.f : top;
+            for (int w = 1; w < WAVES; ++w) top = fmaxf(top, buf1[w]);
+            base = top == -__builtin_inff() ? 0.f : top;
+            ranked = top == quick && fabsf(top) < 0x1p120f && bound > -0x1p120f;      // (fp32 and fp16: +inf, a lost row)
+        }
         s[0] = s[1] = 0.f;
         all([&](const Piece<TYPE> &p, int) {
 #pragma unroll
@@ -399,7 +405,7 @@ __global__ __launch_bounds__(NT, NT == 1024 || PIECES <= 512 ? 4 : 3) void score
         return queued <= PIECES && found <= KEYS;
     };
     const float least = O::bound(O::of(-__builtin_inff()) + 1);      // above -inf
-    const bool room = known && collect(fmaxf(bound, least));
+    const bool room = ranked && collect(fmaxf(bound, least));
     int have = found;
     __syncthreads();      // (found is set again below)
     if (!room) {
@@ -412,7 +418,7 @@ __global__ __launch_bounds__(NT, NT == 1024 || PIECES <= 512 ? 4 : 3) void score
             });
             return block_count<NT>(c, buf4);
         };
-        unsigned lo = __builtin_amdgcn_readfirstlane(O::of(known ? fmaxf(bound, least) : least)), hi = __builtin_amdgcn_readfirstlane(O::of(top));
+        unsigned lo = __builtin_amdgcn_readfirstlane(O::of(ranked ? fmaxf(bound, least) : least)), hi = __builtin_amdgcn_readfirstlane(O::of(top));
         const unsigned highest = hi;
         const int finite = count(least);
         int need = min(a.k, finite);
